@@ -1,0 +1,363 @@
+"""Performance cases of the dense operators: what a training or serving loop asks of them between the mini-batch and the loss.
+
+The operators run on the rows that a mini-batch leaves on the device (features and neighbor means of a frontier, then hidden
+layers): `linear` is a product with bias, activation, dropout and residual behind it, with its gradients and a form for 8-bit
+operands; `dropout` draws its mask from a counter and stores none; `norm` is the root-mean-square norm with the residual's
+addition in front and, where asked, an 8-bit result behind, with its gradients.
+
+`own` chooses between the plain forms below (elementary torch operations in 32 bits, rounded once) and the library's kernels.
+`exact` has the same values in 64 bits from the definitions.  Feature widths are those of the benchmark's workloads (100, 128,
+256, 600); hidden widths and class counts are generic."""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16, "f8": torch.float8_e4m3fn}
+SIZE = {"f32": 4, "bf16": 2, "f16": 2, "f8": 1}
+MAX8 = 448.0  # largest finite value of the 8-bit type
+
+
+def _linear(name, dtype, rows, k, n, **more):
+    return {"name": name, "op": "linear", "dtype": dtype, "rows": rows, "in": k, "out": n, "act": "none", "p": 0.0, "residual": False,
+            "save": False, "count": 0, "pad": 0, **more}
+
+
+def _norm(name, dtype, rows, cols, **more):
+    return {"name": name, "op": "norm", "dtype": dtype, "rows": rows, "cols": cols, "residual": True, "p": 0.0, "out": "same", "count": 0, "pad": 0, **more}
+
+
+def listed():
+    return [
+        # serving: the class scores of one vertex
+        _linear("linear_one_row", "bf16", 1, 256, 512),
+        # the first layer of a deep mini-batch: [features | neighbor mean] of the innermost frontier as the plan's fused input holds them,
+        # as many rows as the device says, the activation's input kept for the backward pass
+        _linear("linear_first_layer", "f32", 300_000, 256, 256, act="relu", save=True, count=285_127),
+        # a hidden layer of a wide residual network in training
+        _linear("linear_hidden", "bf16", 65_537, 1024, 1024, act="gelu", p=0.1, residual=True, save=True),
+        # the output layer: few and odd classes, an odd width, rows that start anywhere
+        _linear("linear_ragged", "f16", 33_333, 301, 47, pad=2),
+        # inference on 8-bit operands, the operands' scales by row, the result in bf16
+        _linear("linear_8bit", "f8", 65_536, 1024, 2048, act="silu"),
+        # gradients of a first layer's shape (features of 2 x 100 columns), weights and bias and input
+        _linear("linear_gradients_f32", "f32", 100_000, 200, 256, op="linear_backward", act="relu"),
+        # gradients of the hidden layer
+        _linear("linear_gradients_bf16", "bf16", 65_536, 1024, 1024, op="linear_backward", act="silu", p=0.2),
+        # dropout of a hidden layer's rows, the mask by global vertex id
+        {"name": "dropout_large", "op": "dropout", "dtype": "bf16", "rows": 285_127, "cols": 512, "p": 0.5, "residual": False, "ids": True, "pad": 0},
+        # dropout and addition on a batch of seeds with an odd width, rows that start anywhere
+        {"name": "dropout_ragged", "op": "dropout", "dtype": "f32", "rows": 4_096, "cols": 601, "p": 0.1, "residual": True, "ids": False, "pad": 1},
+        # serving: norm of a few rows, result in 8 bits
+        _norm("norm_few_rows", "bf16", 16, 1024, out="f8"),
+        # norm in front of a hidden layer in training: residual and dropout in the same pass, fewer rows than the buffers hold
+        _norm("norm_hidden", "bf16", 131_072, 1024, p=0.1, count=120_001),
+        # its gradients
+        _norm("norm_gradients", "bf16", 131_072, 1024, op="norm_backward"),
+    ]
+
+
+def draw(rng):
+    def log(lo, hi):
+        return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi + 1)))))))
+
+    op = rng.choice(["linear", "linear", "linear_backward", "linear_backward", "dropout", "norm", "norm_backward"])
+    rows, p = log(1, 262_144), rng.choice([0.0, 0.1, 0.25, 0.5])
+    count = rng.choice([0, 0, rng.randint(0, rows)])
+    if op in ("linear", "linear_backward"):
+        dtype = rng.choice(["f32", "bf16", "f16", "f8"] if op == "linear" else ["f32", "bf16", "f16"])
+        case = {"op": op, "dtype": dtype, "rows": rows, "in": log(1, 2048), "out": log(1, 2048), "act": rng.choice(["none", "relu", "silu", "gelu"]),
+                "p": p, "residual": op == "linear" and rng.random() < 0.5, "save": op == "linear" and dtype != "f8" and rng.random() < 0.5,
+                "count": count, "pad": rng.choice([0, 0, 1, 8])}
+    elif op == "dropout":
+        case = {"op": op, "dtype": rng.choice(["f32", "bf16", "f16"]), "rows": rows, "cols": log(1, 4096), "p": rng.choice([0.1, 0.25, 0.5]),
+                "residual": rng.random() < 0.5, "ids": rng.random() < 0.5, "pad": rng.choice([0, 0, 1, 8])}
+    else:
+        case = {"op": op, "dtype": rng.choice(["f32", "bf16", "f16"]), "rows": rows, "cols": log(2, 8192), "residual": rng.random() < 0.7, "p": p,
+                "out": rng.choice(["same", "f8"]) if op == "norm" else "same", "count": count, "pad": rng.choice([0, 0, 1, 8])}
+    most = max(_cost(c) for c in listed() if c["op"] == op)  # a drawn case costs no more than the largest one of its operator
+    while _cost(case) > most:
+        case["rows"] -= -(-case["rows"] // 8)
+        case["count"] = min(case["count"], case["rows"])
+    return case
+
+
+def _summed(case):
+    """Whether the norm's input is a sum of its own, which the backward pass needs: a residual was added or x went through dropout."""
+    return case["residual"] or case["p"] > 0
+
+
+def work(case):
+    rows, e = case.get("count") or case["rows"], SIZE[case["dtype"]]
+    if case["op"] == "linear":
+        k, n, ey = case["in"], case["out"], 2 if case["dtype"] == "f8" else e
+        scales = 4 * (rows + n) if case["dtype"] == "f8" else 0
+        return {"bytes": e * (rows * k + n * k) + 4 * n + scales + ey * rows * n * (1 + case["residual"] + case["save"]), "flops": 2.0 * rows * k * n}
+    if case["op"] == "linear_backward":
+        k, n = case["in"], case["out"]
+        return {"bytes": e * (2 * rows * k + 2 * n * k + rows * n * (1 + (case["act"] != "none"))) + 4 * n, "flops": 4.0 * rows * k * n}
+    cells = rows * case["cols"]
+    if case["op"] == "dropout":
+        return {"bytes": e * cells * (2 + case["residual"]) + 4 * rows * case["ids"], "flops": 1.0 * cells}
+    if case["op"] == "norm":  # x (+ residual) in, (the sum and) the result out
+        out8 = case["out"] == "f8"
+        return {"bytes": cells * (e * (1 + case["residual"] + _summed(case)) + (1 if out8 else e)) + 4 * rows * (1 + out8) + 4 * case["cols"], "flops": 4.0 * cells}
+    # gradients: dy, dh and h in, one gradient out, two where the branch was dropped
+    return {"bytes": e * cells * (3 + case["residual"] + (case["residual"] and case["p"] > 0)) + 4 * rows + 8 * case["cols"], "flops": 8.0 * cells}
+
+
+def _cost(case):
+    w = work(case)
+    return max(w["bytes"], w["flops"] / 50)
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    op, rows, pad = case["op"], case["rows"], case["pad"]
+    dtype = TYPES[case["dtype"]]
+    wide = torch.bfloat16 if case["dtype"] == "f8" else dtype
+
+    def normal(r, c, scale=1.0, kind=wide):  # rows inside wider rows where the case says so
+        return (torch.randn(r, c + pad, device="cuda", generator=gen) * scale).to(kind)[:, :c]
+
+    s = {"case": case, "key": seed * 0x9E3779B97F4A7C15 % 2**63, "layer": seed % 7, "rows": None, "ids": None}
+    if case.get("count"):
+        s["rows"] = torch.tensor([case["count"]], dtype=torch.int32, device="cuda")
+    if case.get("ids"):
+        s["ids"] = torch.randint(0, 110_000_000, (rows,), device="cuda", generator=gen, dtype=torch.int32)
+    live = 0 if s["rows"] is None else 1  # buffers that hold more rows than there are: zeros where nobody writes
+
+    def buffer(c, kind=wide):
+        return torch.zeros(rows, c, dtype=kind, device="cuda") if live else None
+
+    if op in ("linear", "linear_backward"):
+        k, n = case["in"], case["out"]
+        if case["dtype"] == "f8":  # what a norm with an 8-bit result and weights laid out once are: full range in every row, and the rows' scales
+            for name, r, scale in (("a", rows, 1.0), ("w", n, k ** -0.5)):
+                v = torch.randn(r, k, device="cuda", generator=gen) * scale
+                top = v.abs().amax(1).clamp_min(1e-12) / MAX8
+                s[name], s["scale_" + name] = (v / top[:, None]).to(dtype), top
+        else:
+            a = torch.randn(rows, k + pad, device="cuda", generator=gen)
+            s["a"] = (a if case["dtype"] == "f32" else a.relu()).to(dtype)[:, :k]  # features, or a hidden layer's output
+            s["w"] = normal(n, k, k ** -0.5)
+        s["bias"] = torch.randn(n, device="cuda", generator=gen) * 0.1
+        if op == "linear":
+            s["residual"] = normal(rows, n) if case["residual"] else None
+            s["y"], s["z"] = buffer(n), buffer(n) if case["save"] else None
+        else:
+            s["dy"], s["z"] = normal(rows, n, 1.0 / math.sqrt(rows)), normal(rows, n)
+            s["da"] = buffer(k)
+    elif op == "dropout":
+        s["x"], s["residual"] = normal(rows, case["cols"]), normal(rows, case["cols"]) if case["residual"] else None
+    else:
+        cols = case["cols"]
+        s["gain"] = 1.0 + 0.1 * torch.randn(cols, device="cuda", generator=gen)
+        if op == "norm":
+            s["x"], s["residual"] = normal(rows, cols), normal(rows, cols, 2.0) if case["residual"] else None
+            s["y"] = buffer(cols, TYPES["f8"] if case["out"] == "f8" else wide)
+            s["h"] = buffer(cols) if _summed(case) else None
+            s["rstd"] = torch.zeros(rows, device="cuda") if live else None
+            s["scale"] = torch.zeros(rows, device="cuda") if live and case["out"] == "f8" else None
+        else:
+            s["h"], s["dy"] = normal(rows, cols, 2.0), normal(rows, cols, 1.0 / math.sqrt(rows))
+            s["dh"] = normal(rows, cols, 1.0 / math.sqrt(rows)) if case["residual"] else None
+            s["rstd"] = s["h"].float().square().mean(1).add(1e-6).rsqrt()
+            s["dx"] = buffer(cols)
+            s["dr"] = buffer(cols) if case["residual"] and case["p"] > 0 else None
+    return s
+
+
+# ---- the plain forms ------------------------------------------------------------------------------------------------------------
+
+def _words(key, layer, ids, rows, cols):
+    """Philox4x32-10 words of a [rows, cols] mask, int64: word c % 4 of counter (id of the row, c / 4, layer, 1)."""
+    low = 0xFFFFFFFF
+    row = (torch.arange(rows, device="cuda") if ids is None else ids.long())[:, None] & low
+    c0, c1 = torch.broadcast_tensors(row, torch.arange(-(-cols // 4), device="cuda")[None, :])
+    c2, c3 = torch.full_like(c0, layer), torch.full_like(c0, 1)
+    k0, k1 = key & low, key >> 32 & low
+    for _ in range(10):
+        m0, m1 = c0 * 0xD2511F53, c2 * 0xCD9E8D57
+        c0, c1, c2, c3 = (m1 >> 32 & low) ^ c1 ^ k0, m1 & low, (m0 >> 32 & low) ^ c3 ^ k1, m0 & low
+        k0, k1 = k0 + 0x9E3779B9 & low, k1 + 0xBB67AE85 & low
+    return torch.stack((c0, c1, c2, c3), 2).reshape(rows, -1)[:, :cols]
+
+
+def _dropped(x, s):
+    p = s["case"]["p"]
+    if p == 0:
+        return x
+    keep = _words(s["key"], s["layer"], s["ids"], x.shape[0], x.shape[1]) >= int(p * 2**32)
+    return torch.where(keep, x * (1.0 / (1.0 - p)), 0.0)
+
+
+def _act(z, act):
+    if act == "relu":
+        return torch.where(z > 0, z, 0.0)
+    if act == "silu":
+        return z / (1 + torch.exp(-z))
+    if act == "gelu":
+        return 0.5 * z * (1 + torch.erf(z * 0.5**0.5))
+    return z
+
+
+def _slope(z, act):
+    if act == "relu":
+        return torch.where(z > 0, 1.0, 0.0)
+    if act == "silu":
+        g = 1 / (1 + torch.exp(-z))
+        return g * (1 + z * (1 - g))
+    if act == "gelu":
+        return 0.5 * (1 + torch.erf(z * 0.5**0.5)) + z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+    return torch.ones_like(z)
+
+
+def _live(v, s):
+    """Zeros in the rows that the device's count leaves out."""
+    if s["rows"] is None:
+        return v
+    here = torch.arange(v.shape[0], device="cuda") < s["rows"]
+    return torch.where(here if v.dim() == 1 else here[:, None], v, 0.0)
+
+
+def _plain(s):
+    case, op = s["case"], s["case"]["op"]
+    kind = torch.bfloat16 if case["dtype"] == "f8" else TYPES[case["dtype"]]
+    if op == "linear":
+        a, w = s["a"].float(), s["w"].float()
+        if case["dtype"] == "f8":
+            a, w = a * s["scale_a"][:, None], w * s["scale_w"][:, None]
+        z = torch.matmul(a, w.t()) + s["bias"]
+        y = _dropped(_act(z, case["act"]), s)
+        y = y + s["residual"].float() if case["residual"] else y
+        out = {"y": _live(y, s).to(kind)}
+        return {**out, "z": _live(z, s).to(kind)} if case["save"] else out
+    if op == "linear_backward":
+        dz = _dropped(s["dy"].float(), s) * _slope(s["z"].float(), case["act"])
+        dz = _live(dz, s)
+        return {"da": torch.matmul(dz, s["w"].float()).to(kind), "dw": torch.matmul(dz.t(), _live(s["a"].float(), s)).to(kind), "dbias": dz.sum(0)}
+    if op == "dropout":
+        y = _dropped(s["x"].float(), s)
+        return {"y": (y + s["residual"].float() if case["residual"] else y).to(kind)}
+    if op == "norm":
+        h = _dropped(s["x"].float(), s)
+        h = h + s["residual"].float() if case["residual"] else h
+        rstd = torch.rsqrt((h * h).mean(1) + 1e-6)
+        y = h * rstd[:, None] * s["gain"]
+        out = {"rstd": _live(rstd, s)}
+        if _summed(case):
+            out["h"] = _live(h, s).to(kind)
+        if case["out"] == "f8":
+            scale = y.abs().amax(1) / MAX8
+            scale = torch.where(scale > 0, scale, 1.0)
+            return {**out, "y": _live((y / scale[:, None]).clamp(-MAX8, MAX8), s).to(TYPES["f8"]), "scale": _live(scale, s)}
+        return {**out, "y": _live(y, s).to(kind)}
+    h, dy, rstd = s["h"].float(), s["dy"].float(), s["rstd"][:, None]
+    g = dy * s["gain"]
+    dh = rstd * (g - h * (rstd * rstd * (g * h).mean(1, keepdim=True)))
+    dh = dh + s["dh"].float() if case["residual"] else dh
+    out = {"dx": _live(_dropped(dh, s), s).to(kind), "dgain": _live(dy * h * rstd, s).sum(0)}
+    return {**out, "dr": _live(dh, s).to(kind)} if case["residual"] and case["p"] > 0 else out
+
+
+# ---- the library's operators ----------------------------------------------------------------------------------------------------
+
+def _kernels(s):
+    from paper_2605_29346_amd import layers
+    case, op, rows = s["case"], s["case"]["op"], s["rows"]
+    drop = layers.Dropout(case["p"], s["key"], s["layer"], s["ids"]) if case["p"] > 0 else None
+    if op == "linear":
+        eight = {"scale_a": s["scale_a"], "scale_w": s["scale_w"], "out_dtype": torch.bfloat16} if case["dtype"] == "f8" else {}
+        r = layers.linear(s["a"], s["w"], bias=s["bias"], act=case["act"], dropout=drop, residual=s["residual"], rows=rows,
+                          save=case["save"], out=s["y"], preact=s["z"], **eight)
+        return {"y": r[0], "z": r[1]} if case["save"] else {"y": r}
+    if op == "linear_backward":
+        da, dw, db = layers.linear_backward(s["dy"], s["a"], s["w"], preact=s["z"] if case["act"] != "none" else None, act=case["act"], dropout=drop, rows=rows, da=s["da"])
+        return {"da": da, "dw": dw, "dbias": db}
+    if op == "dropout":
+        return {"y": layers.dropout(s["x"], drop, residual=s["residual"])}
+    if op == "norm":
+        r = layers.rms_norm(s["x"], gain=s["gain"], eps=1e-6, residual=s["residual"], dropout=drop, rows=rows,
+                            out_dtype=TYPES["f8"] if case["out"] == "f8" else None, y=s["y"], h=s["h"], rstd=s["rstd"], scale=s["scale"])
+        out = {"rstd": r.rstd, "y": r.y}
+        if _summed(case):
+            out["h"] = r.h
+        return {**out, "scale": r.scale} if case["out"] == "f8" else out
+    dx, dr, dgain = layers.rms_norm_backward(s["dy"], s["h"], s["rstd"], gain=s["gain"], dh=s["dh"], dropout=drop, rows=rows, need_dr=case["residual"], dx=s["dx"], dr=s["dr"])
+    out = {"dx": dx, "dgain": dgain}
+    return {**out, "dr": dr} if case["residual"] and case["p"] > 0 else out
+
+
+def run(state):
+    return _kernels(state) if own else _plain(state)
+
+
+# ---- the definitions in 64 bits -------------------------------------------------------------------------------------------------
+
+def _kept(key, layer, ids, rows, cols, p):
+    """The mask as booleans, from Philox4x32-10 on 64-bit words of the host."""
+    u, mask = np.uint64, np.uint64(0xFFFFFFFF)
+    who = np.arange(rows, dtype=u) if ids is None else ids.cpu().numpy().astype(np.uint32).astype(u)
+    x = [np.repeat(who, -(-cols // 4)), np.tile(np.arange(-(-cols // 4), dtype=u), rows), u(layer), u(1)]
+    for r in range(10):
+        k0, k1 = u((key + r * 0x9E3779B9) & 0xFFFFFFFF), u(((key >> 32) + r * 0xBB67AE85) & 0xFFFFFFFF)
+        a, b = x[0] * u(0xD2511F53), x[2] * u(0xCD9E8D57)
+        x = [(b >> u(32)) ^ x[1] ^ k0, b & mask, (a >> u(32)) ^ x[3] ^ k1, a & mask]
+    words = np.stack(x, 1).reshape(rows, -1)[:, :cols]
+    return torch.from_numpy(words >= u(int(p * 2**32))).cuda()
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    op, act, p, rows = case["op"], case.get("act"), case["p"], case["rows"]
+    n = case.get("count") or rows
+    wide = case["out"] if op in ("linear", "linear_backward") else case["cols"]
+    keep = _kept(s["key"], s["layer"], s["ids"], rows, wide, p) if p > 0 else None
+
+    def d(t):
+        return t.double()
+
+    def drop(t):
+        return t if keep is None else t.masked_fill(~keep, 0) / (1 - p)
+
+    def cut(t):
+        t = t.clone()
+        t[n:] = 0
+        return t
+
+    def bend(z):
+        f = {"none": lambda v: v, "relu": torch.relu, "silu": lambda v: v * torch.sigmoid(v), "gelu": lambda v: v * torch.special.ndtr(v)}
+        return f[act](z)
+
+    if op == "linear":
+        a, w = d(s["a"]), d(s["w"])
+        if case["dtype"] == "f8":
+            a, w = d(s["scale_a"])[:, None] * a, d(s["scale_w"])[:, None] * w
+        z = torch.addmm(d(s["bias"]), a, w.t())
+        y = drop(bend(z)) + (d(s["residual"]) if case["residual"] else 0)
+        return {"y": cut(y), "z": cut(z)} if case["save"] else {"y": cut(y)}
+    if op == "linear_backward":  # the chain rule from the activation's input on, by differentiation
+        z = d(s["z"]).requires_grad_()
+        dz, = torch.autograd.grad(drop(bend(z)), z, d(s["dy"]))
+        return {"da": cut(dz @ d(s["w"])), "dw": dz[:n].t() @ d(s["a"])[:n], "dbias": dz[:n].sum(0)}
+    if op == "dropout":
+        return {"y": drop(d(s["x"])) + (d(s["residual"]) if case["residual"] else 0)}
+    if op == "norm":
+        h = drop(d(s["x"])) + (d(s["residual"]) if case["residual"] else 0)
+        rstd = (h.pow(2).sum(1) / wide + 1e-6) ** -0.5
+        y = h * d(s["gain"]) * rstd[:, None]
+        out = {"rstd": cut(rstd)}
+        if _summed(case):
+            out["h"] = cut(h)
+        if case["out"] == "f8":  # before the rounding to 8 bits
+            top = y.abs().max(1).values / MAX8
+            return {**out, "y": cut(y / top.clamp_min(1e-300)[:, None]), "scale": cut(torch.where(top > 0, top, 1.0))}
+        return {**out, "y": cut(y)}
+    h, rstd, g = d(s["h"]), d(s["rstd"])[:, None], d(s["gain"])
+    dy = d(s["dy"])
+    dh = dy * g * rstd - h * rstd**3 * ((dy * g * h).sum(1, keepdim=True) / wide) + (d(s["dh"]) if case["residual"] else 0)
+    out = {"dx": cut(drop(dh)), "dgain": (dy * h * rstd)[:n].sum(0)}
+    return {**out, "dr": cut(dh)} if case["residual"] and p > 0 else out
