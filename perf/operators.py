@@ -172,26 +172,33 @@ def prepare(case, seed):
 
 # ---- the plain forms ------------------------------------------------------------------------------------------------------------
 
-def _words(key, layer, ids, rows, cols):
-    """Philox4x32-10 words of a [rows, cols] mask, int64: word c % 4 of counter (id of the row, c / 4, layer, 1)."""
+def _halves(key, layer, ids, rows, cols):
+    """16 random bits for each cell of a [rows, cols] mask, int64: the low, then the high half of word c / 2 % 4 of Philox4x32-10 with
+    counter (id of the row, c / 8, layer, 1)."""
     low = 0xFFFFFFFF
     row = (torch.arange(rows, device="cuda") if ids is None else ids.long())[:, None] & low
-    c0, c1 = torch.broadcast_tensors(row, torch.arange(-(-cols // 4), device="cuda")[None, :])
+    c0, c1 = torch.broadcast_tensors(row, torch.arange(-(-cols // 8), device="cuda")[None, :])
     c2, c3 = torch.full_like(c0, layer), torch.full_like(c0, 1)
     k0, k1 = key & low, key >> 32 & low
     for _ in range(10):
         m0, m1 = c0 * 0xD2511F53, c2 * 0xCD9E8D57
         c0, c1, c2, c3 = (m1 >> 32 & low) ^ c1 ^ k0, m1 & low, (m0 >> 32 & low) ^ c3 ^ k1, m0 & low
         k0, k1 = k0 + 0x9E3779B9 & low, k1 + 0xBB67AE85 & low
-    return torch.stack((c0, c1, c2, c3), 2).reshape(rows, -1)[:, :cols]
+    words = torch.stack((c0, c1, c2, c3), 2).unsqueeze(3)
+    return torch.cat((words & 0xFFFF, words >> 16), 3).reshape(rows, -1)[:, :cols]
+
+
+def _cut(p):
+    """A cell is dropped where its 16 bits are below this: p is taken to a multiple of 2^-16."""
+    return math.floor(p * 65536 + 0.5)
 
 
 def _dropped(x, s):
     p = s["case"]["p"]
     if p == 0:
         return x
-    keep = _words(s["key"], s["layer"], s["ids"], x.shape[0], x.shape[1]) >= int(p * 2**32)
-    return torch.where(keep, x * (1.0 / (1.0 - p)), 0.0)
+    keep = _halves(s["key"], s["layer"], s["ids"], x.shape[0], x.shape[1]) >= _cut(p)
+    return torch.where(keep, x * (65536 / (65536 - _cut(p))), 0.0)
 
 
 def _act(z, act):
@@ -299,15 +306,15 @@ def run(state):
 
 def _kept(key, layer, ids, rows, cols, p):
     """The mask as booleans, from Philox4x32-10 on 64-bit words of the host."""
-    u, mask = np.uint64, np.uint64(0xFFFFFFFF)
+    u, mask, groups = np.uint64, np.uint64(0xFFFFFFFF), -(-cols // 8)
     who = np.arange(rows, dtype=u) if ids is None else ids.cpu().numpy().astype(np.uint32).astype(u)
-    x = [np.repeat(who, -(-cols // 4)), np.tile(np.arange(-(-cols // 4), dtype=u), rows), u(layer), u(1)]
+    x = [np.repeat(who, groups), np.tile(np.arange(groups, dtype=u), rows), u(layer), u(1)]
     for r in range(10):
         k0, k1 = u((key + r * 0x9E3779B9) & 0xFFFFFFFF), u(((key >> 32) + r * 0xBB67AE85) & 0xFFFFFFFF)
         a, b = x[0] * u(0xD2511F53), x[2] * u(0xCD9E8D57)
         x = [(b >> u(32)) ^ x[1] ^ k0, b & mask, (a >> u(32)) ^ x[3] ^ k1, a & mask]
-    words = np.stack(x, 1).reshape(rows, -1)[:, :cols]
-    return torch.from_numpy(words >= u(int(p * 2**32))).cuda()
+    bits = np.stack(x, 1).astype("<u4").view("<u2").reshape(rows, -1)[:, :cols]
+    return torch.from_numpy(bits >= round(p * 65536)).cuda()
 
 
 def exact(case, seed):
@@ -316,6 +323,7 @@ def exact(case, seed):
     n = case.get("count") or rows
     wide = case["out"] if op in ("linear", "linear_backward") else case["cols"]
     keep = _kept(s["key"], s["layer"], s["ids"], rows, wide, p) if p > 0 else None
+    p = round(p * 65536) / 65536
 
     def d(t):
         return t.double()
