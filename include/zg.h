@@ -45,7 +45,14 @@ typedef struct zg_graph_s zg_graph_t;
 typedef struct zg_plan_s zg_plan_t;
 
 enum zg_status { ZG_OK = 0, ZG_EINVAL = -1, ZG_ENOMEM = -2, ZG_EHIP = -3, ZG_ESTATE = -4 };
-enum zg_dtype { ZG_I32 = 0, ZG_I64 = 1 };
+enum zg_dtype {
+    ZG_I32 = 0,
+    ZG_I64 = 1,
+    ZG_F32 = 2,
+    ZG_F16 = 3,
+    ZG_BF16 = 4,
+    ZG_F8 = 5 /* 8-bit floats of 4 exponent and 3 mantissa bits, largest value 448, no infinities */
+};
 
 /* zg_graph_create flags */
 #define ZG_GRAPH_VALIDATE 1u /* synchronising check: indices in range, rows ascending (hence duplicate-free) */
@@ -328,6 +335,175 @@ int zg_overflow_flag(const zg_plan_t *p, const uint32_t **d_flag);
 /* Clears the sticky word with a one-lane kernel on `stream` (no memset node: safe under graph capture). */
 int zg_overflow_clear(zg_plan_t *p, void *stream);
 
+
+/* ---- dense operators on the rows of a mini-batch --------------------------------------------------
+ * What a layer does with the rows that a step leaves on the device: a product with bias, activation, dropout and residual
+ * behind it, dropout alone, and the root-mean-square norm with the residual's addition in front of it; each with its
+ * gradients.  Conventions of this section:
+ *  - Matrices are row-major with a row stride (ld_*, in elements, >= the width); rows may start at any multiple of the
+ *    element size.  Rows and widths: 0 <= rows < 2^31, 1 <= width <= ZG_MAX_WIDTH (norms: ZG_MAX_NORM_WIDTH).
+ *  - `rows` is a capacity.  d_rows (NULL: all rows) is the device's own count, read when the kernels run, as zg_outputs.d_n
+ *    holds it: min(*d_rows, rows) rows are read and written, the others are left alone and take no part in any sum.
+ *  - Types: ZG_F32, ZG_F16, ZG_BF16 (and ZG_F8 where it says so).  Vectors (bias, gain, scales, their gradients) and the
+ *    norm's statistics are fp32.  Sums, activations and everything in between are fp32; a result is rounded to its type once,
+ *    to nearest even.  One rounding more where a gradient of ZG_F16 or ZG_BF16 passes through an activation: see zg_linear_backward.
+ *  - The calls enqueue kernels on `stream` (default-priority, under capture or not) and nothing else: no allocation, no memset
+ *    node, no synchronisation.  They use the current device.  Results do not depend on the launch: no atomics add them up.
+ *  - Outputs must not overlap inputs or each other, except where a call says that one may be the other (same address, same stride).
+ *  - Structs start from zero: a field that is not needed is 0 / NULL.
+ * Errors: ZG_EINVAL (null pointers, widths, strides, types), ZG_ENOMEM (workspace too small), ZG_EHIP (a launch failed). */
+#define ZG_MAX_WIDTH 32768
+#define ZG_MAX_NORM_WIDTH 16384 /* of zg_rms_norm and its gradients, which hold a row in one workgroup's registers */
+
+enum zg_act {
+    ZG_ACT_NONE = 0,
+    ZG_ACT_RELU = 1, /* max(z, 0), slope 0 at z = 0 */
+    ZG_ACT_SILU = 2, /* z / (1 + exp(-z)) */
+    ZG_ACT_GELU = 3  /* z (1 + erf(z / sqrt 2)) / 2 */
+};
+
+/* Dropout whose mask is never stored: whether cell (row, c) is dropped is a function of (key, layer, id of the row, c) alone, so
+ * the backward pass, another layout of the rows or another machine finds the same mask.  Cell (row, c) takes 16 bits: the low half
+ * (c even) or the high half (c odd) of word (c / 2) % 4 of Philox4x32-10 with counter (id, c / 8, layer, 1) and key (low, high word
+ * of `key`); it is dropped where they are below t = floor(65536 p + 1/2).  What is kept is multiplied by 65536 / (65536 - t) (p is
+ * taken to a multiple of 2^-16, and the mean stays); what is dropped is 0 whatever it was.  The last counter word keeps these draws
+ * apart from the sampler's (whose last word is 0) under the same key.  id = d_ids[row] (e.g. the plan's d_S: the mask then belongs
+ * to the vertex), or the row itself where d_ids is NULL.  p = 0: no dropout; 0 <= p <= 1. */
+typedef struct {
+    double p;
+    uint64_t key;
+    uint32_t layer;
+    uint32_t reserved;
+    const int32_t *d_ids; /* [rows] or NULL */
+} zg_drop;
+
+/* Z = A W^T + bias,  Y = drop(act(Z)) + R.
+ * A: [rows, in], W: [out, in] (as a linear layer keeps it), both of type `dtype`; bias: [out]; R, Y, Z: [rows, out] of type
+ * `out_dtype`.  dtype = ZG_F8 takes the operands' scales, which multiply whole rows: A[i,:] stands for scale_A[i] A[i,:], W[j,:]
+ * for scale_W[j] W[j,:] (NULL: 1).  Z (optional) is what zg_linear_backward needs of the forward pass.  Y may be R.
+ * out_dtype: ZG_F32, ZG_F16 or ZG_BF16, whatever dtype is. */
+typedef struct {
+    int64_t rows;
+    const uint32_t *d_rows;
+    int32_t in, out;
+    int32_t dtype, out_dtype;
+    int32_t act, reserved;
+    const void *d_A;
+    int64_t ld_A;
+    const float *d_scale_A;
+    const void *d_W;
+    int64_t ld_W;
+    const float *d_scale_W;
+    const float *d_bias;
+    const void *d_R;
+    int64_t ld_R;
+    void *d_Y;
+    int64_t ld_Y;
+    void *d_Z;
+    int64_t ld_Z;
+    zg_drop drop;
+} zg_linear_args;
+int zg_linear(const zg_linear_args *a, void *stream);
+
+/* Gradients of zg_linear: with dZ = drop(dY) act'(Z),  dA = dZ W,  dW = dZ^T A,  dbias = sum of dZ over the rows (dR is dY itself).
+ * dtype is the type of A, W, dA and dW, out_dtype that of dY and Z; Z may be NULL where act is ZG_ACT_NONE.  d_dA, d_dW and d_dbias
+ * may be NULL: that gradient is not wanted (d_W is not needed without d_dA, d_A not without d_dW).  dZ is held in `dtype` (the
+ * products' operand; exact where the slope is 0 or 1, as of ZG_ACT_NONE and ZG_ACT_RELU: dropout's factor is applied behind the
+ * products), dbias is summed from its fp32 values. */
+typedef struct {
+    int64_t rows;
+    const uint32_t *d_rows;
+    int32_t in, out;
+    int32_t dtype, out_dtype;
+    int32_t act, reserved;
+    const void *d_dY;
+    int64_t ld_dY;
+    const void *d_Z;
+    int64_t ld_Z;
+    const void *d_A;
+    int64_t ld_A;
+    const void *d_W;
+    int64_t ld_W;
+    void *d_dA;
+    int64_t ld_dA;
+    void *d_dW;
+    int64_t ld_dW;
+    float *d_dbias;
+    zg_drop drop;
+} zg_linear_grad_args;
+/* Workspace bytes of the call, 256-byte aligned device memory that is free again when the call's kernels are done.  Host only. */
+int zg_linear_backward_workspace(const zg_linear_grad_args *a, size_t *bytes);
+int zg_linear_backward(const zg_linear_grad_args *a, void *d_workspace, size_t workspace_bytes, void *stream);
+
+/* y = drop(x) + r (r may be NULL; y may be x or r); [rows, cols] of type dtype.  Its gradient is the same call on the gradient of y
+ * (with r = NULL); that of r is the gradient of y itself. */
+typedef struct {
+    int64_t rows;
+    const uint32_t *d_rows;
+    int32_t cols;
+    int32_t dtype;
+    const void *d_x;
+    int64_t ld_x;
+    const void *d_r;
+    int64_t ld_r;
+    void *d_y;
+    int64_t ld_y;
+    zg_drop drop;
+} zg_dropout_args;
+int zg_dropout(const zg_dropout_args *a, void *stream);
+
+/* h = drop(x) + r,  rstd = 1 / sqrt(mean over the row of h^2 + eps),  y = h rstd gain.
+ * x, r, h: [rows, cols] of type dtype (r NULL: no residual; h NULL: not wanted; h may be r or x); gain: [cols] or NULL (ones);
+ * rstd: [rows] or NULL.  y is of type out_dtype; the statistics and y are made from the fp32 sums, not from h as it is rounded.
+ * out_dtype = ZG_F8: scale[i] = max over the row of |y| / 448 (1 where that is 0 or not a number) and y holds y / scale to nearest
+ * even - the operand of a zg_linear of type ZG_F8, with d_scale_A = scale. */
+typedef struct {
+    int64_t rows;
+    const uint32_t *d_rows;
+    int32_t cols;
+    int32_t dtype, out_dtype;
+    float eps; /* >= 0 */
+    const void *d_x;
+    int64_t ld_x;
+    const void *d_r;
+    int64_t ld_r;
+    const float *d_gain;
+    void *d_h;
+    int64_t ld_h;
+    void *d_y;
+    int64_t ld_y;
+    float *d_scale; /* [rows], ZG_F8 only */
+    float *d_rstd;
+    zg_drop drop;
+} zg_norm_args;
+int zg_rms_norm(const zg_norm_args *a, void *stream);
+
+/* Gradients of zg_rms_norm (out_dtype = dtype) from dy, h and rstd, and dh, the gradient that reaches h from elsewhere (NULL: none):
+ *   dr = dh + rstd (gain dy - h rstd^2 mean over the row of (gain dy h)),  dx = drop(dr),  dgain = sum over the rows of dy h rstd.
+ * dr (the gradient of the residual and of h) may be NULL; dx may be NULL where dr is not; without dropout they are the same values.
+ * dx or dr may be dh or dy.  dgain may be NULL: then no workspace is needed. */
+typedef struct {
+    int64_t rows;
+    const uint32_t *d_rows;
+    int32_t cols;
+    int32_t dtype;
+    const void *d_dy;
+    int64_t ld_dy;
+    const void *d_h;
+    int64_t ld_h;
+    const float *d_rstd;
+    const float *d_gain;
+    const void *d_dh;
+    int64_t ld_dh;
+    void *d_dx;
+    int64_t ld_dx;
+    void *d_dr;
+    int64_t ld_dr;
+    float *d_dgain;
+    zg_drop drop;
+} zg_norm_grad_args;
+int zg_rms_norm_backward_workspace(const zg_norm_grad_args *a, size_t *bytes);
+int zg_rms_norm_backward(const zg_norm_grad_args *a, void *d_workspace, size_t workspace_bytes, void *stream);
 
 /* ---- measurement helpers ----------------------------------------------------------------------
  * Identifier of the sources the library was built from (a hash the build step passes in); lets a caller

@@ -5,14 +5,16 @@ import hashlib
 import os
 import shutil
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 from typing import Optional
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libzg.so")
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("zg_host.cpp", "zg_device.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("zg_host.cpp", "zg_device.hip", "zg_rows.hip", "zg_linear.hip")]
 HEADERS = [os.path.join(HERE, "csrc", "zg_internal.h"), os.path.join(HERE, "csrc", "zg_floyd.h"),
-           os.path.join(ROOT, "include", "zg.h")]
+           os.path.join(HERE, "csrc", "zg_dense.h"), os.path.join(ROOT, "include", "zg.h")]
 
 
 def hipcc() -> Optional[str]:
@@ -45,14 +47,19 @@ def build(force: bool = True, verbose: bool = False) -> str:
     if cc is None:
         raise RuntimeError("hipcc not found: cannot build libzg.so")
     sid = source_id()
-    cmd = [cc, "-x", "hip", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           "-ffp-contract=off", "-Wall", "-Wno-unused-function", f'-DZG_BUILD_ID="{sid}"',
-           "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"),
-           "-o", LIB] + SOURCES
-    if verbose:
-        print(" ".join(cmd))
-    subprocess.run(cmd, check=True)
+    flags = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+             "-ffp-contract=off", "-Wall", "-Wno-unused-function", f'-DZG_BUILD_ID="{sid}"',
+             "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(f) + ".o") for f in SOURCES]
+        steps = [[cc, "-x", "hip"] + flags + ["-c", f, "-o", o] for f, o in zip(SOURCES, objects)]
+        link = [cc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objects
+        if verbose:
+            print("\n".join(" ".join(c) for c in steps + [link]))
+        with ThreadPoolExecutor(len(steps)) as pool:  # one compiler per source
+            list(pool.map(lambda c: subprocess.run(c, check=True), steps))
+        subprocess.run(link, check=True)
     with open(LIB + ".id", "w") as fh:
         fh.write(sid + "\n")
     return LIB

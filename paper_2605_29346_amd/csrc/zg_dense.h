@@ -1,0 +1,218 @@
+// What the dense operators share: types and their wide accesses, the dropout mask, activations, argument checks, launches.
+#pragma once
+
+#include "zg_internal.h"
+
+#include <cmath>
+#include <cstring>
+#include <tuple>
+
+namespace zg {
+
+// ---- host side ------------------------------------------------------------------------------------------------------------------
+
+constexpr int64_t kMaxRows = 0x7FFFFFFF;
+
+inline size_t type_size(int32_t t) { return t == ZG_F32 ? 4 : t == ZG_F16 || t == ZG_BF16 ? 2 : t == ZG_F8 ? 1 : 0; }
+inline bool wide_type(int32_t t) { return t == ZG_F32 || t == ZG_F16 || t == ZG_BF16; }
+
+// Nothing of C++ leaves a C entry point.
+template <class F> int entry(F &&body) noexcept
+{
+    try {
+        return body();
+    } catch (...) {
+        return ZG_ENOMEM; // (the only thing that can throw is a message's string)
+    }
+}
+
+template <class... P, class... A> int launch(hipStream_t st, void (*kernel)(P...), dim3 grid, unsigned block, const A &...given)
+{
+    if (grid.x == 0 || grid.y == 0 || grid.z == 0) return ZG_OK;
+    std::tuple<P...> a{given...};
+    void *args[sizeof...(P)];
+    std::apply([&](auto &...v) { int i = 0; ((args[i++] = const_cast<void *>(static_cast<const void *>(&v))), ...); }, a);
+    // (what the launch returned, and not hipGetLastError: that may be an earlier error of the caller's own)
+    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(block), args, 0, st);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();
+        return fail(ZG_EHIP, std::string("hipLaunchKernel: ") + hipGetErrorString(e));
+    }
+    return ZG_OK;
+}
+
+inline int check_rows(int64_t rows)
+{
+    return rows < 0 || rows > kMaxRows ? fail(ZG_EINVAL, "rows outside 0..2^31-1") : ZG_OK;
+}
+
+inline int check_width(int32_t width, int32_t most = ZG_MAX_WIDTH)
+{
+    return width < 1 || width > most ? fail(ZG_EINVAL, "a width outside 1.." + std::to_string(most)) : ZG_OK;
+}
+
+inline int check_matrix(const char *what, const void *p, int64_t ld, int32_t width, int32_t type)
+{
+    if (!p) return fail(ZG_EINVAL, std::string(what) + " is null");
+    if (ld < width || ld > (int64_t(1) << 40)) return fail(ZG_EINVAL, std::string("the row stride of ") + what + " is below its width, or above 2^40");
+    if (reinterpret_cast<uintptr_t>(p) % type_size(type)) return fail(ZG_EINVAL, std::string(what) + " is not aligned to its elements");
+    return ZG_OK;
+}
+
+// fp32 and int32 vectors
+inline int check_vector(const char *what, const void *p)
+{
+    return reinterpret_cast<uintptr_t>(p) % 4 ? fail(ZG_EINVAL, std::string(what) + " is not aligned to its elements") : ZG_OK;
+}
+
+inline int check_drop(const zg_drop &d)
+{
+    if (!(d.p >= 0.0 && d.p <= 1.0)) return fail(ZG_EINVAL, "the dropout probability is outside 0..1");
+    return check_vector("the dropout's d_ids", d.d_ids);
+}
+
+inline int check_workspace(const void *p, size_t have, size_t need)
+{
+    if (need == 0) return ZG_OK;
+    if (!p || reinterpret_cast<uintptr_t>(p) % 256) return fail(ZG_EINVAL, "the workspace is null or not 256-byte aligned");
+    return have < need ? fail(ZG_ENOMEM, "the workspace is smaller than the call needs") : ZG_OK;
+}
+
+#define ZG_TRY(call)                                                                                         \
+    do {                                                                                                     \
+        const int s_ = (call);                                                                               \
+        if (s_ != ZG_OK) return s_;                                                                          \
+    } while (0)
+
+// ---- the dropout mask -----------------------------------------------------------------------------------------------------------
+
+struct Drop {
+    uint32_t cut; // a cell is dropped where its 16 bits are below this; 0: no dropout
+    float scale;  // 65536 / (65536 - cut)
+    uint32_t key_lo, key_hi, layer;
+    const int32_t *ids;
+};
+
+inline Drop make_drop(const zg_drop &d)
+{
+    Drop r{};
+    r.cut = (uint32_t)std::floor(d.p * 65536.0 + 0.5);
+    r.scale = r.cut < 65536u ? (float)(65536.0 / (65536.0 - r.cut)) : 0.0f;
+    r.key_lo = (uint32_t)d.key;
+    r.key_hi = (uint32_t)(d.key >> 32);
+    r.layer = d.layer;
+    r.ids = d.d_ids;
+    return r;
+}
+
+struct Rows {
+    const uint32_t *d_rows;
+    uint32_t cap;
+    __device__ __forceinline__ uint32_t live() const { return d_rows ? min(*d_rows, cap) : cap; }
+};
+
+#ifdef __HIPCC__
+
+__device__ __forceinline__ uint64_t mask_product(uint32_t a, uint32_t b)
+{
+    uint64_t p;
+    asm("v_mad_u64_u32 %0, vcc, %1, %2, 0" : "=v"(p) : "v"(a), "s"(b) : "vcc");
+    return p;
+}
+
+// Philox4x32-10 (Salmon et al., SC'11) with counter (id, group, layer, 1): the 16 bits of the eight cells 8 group .. 8 group + 7 of a row, two to
+// a word.  20 whole products and 20 three-way xors.
+__device__ __forceinline__ void mask_bits(const Drop &d, uint32_t id, uint32_t group, uint32_t (&w)[4])
+{
+    uint32_t c0 = id, c1 = group, c2 = d.layer, c3 = 1u, k0 = d.key_lo, k1 = d.key_hi;
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t p0 = mask_product(c0, 0xD2511F53u);
+        const uint64_t p1 = r == 0 ? (uint64_t)0xCD9E8D57u * c2 : mask_product(c2, 0xCD9E8D57u); // (the first one is the layer's: a scalar)
+        c0 = __builtin_amdgcn_bitop3_b32((uint32_t)(p1 >> 32), c1, k0, 0x96);
+        c1 = (uint32_t)p1;
+        c2 = __builtin_amdgcn_bitop3_b32((uint32_t)(p0 >> 32), c3, k1, 0x96);
+        c3 = (uint32_t)p0;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    w[0] = c0, w[1] = c1, w[2] = c2, w[3] = c3;
+}
+
+__device__ __forceinline__ bool mask_keeps(const Drop &d, const uint32_t (&w)[4], int cell)
+{
+    return (cell & 1 ? w[cell >> 1] >> 16 : w[cell >> 1] & 0xFFFFu) >= d.cut;
+}
+
+__device__ __forceinline__ uint32_t mask_id(const Drop &d, uint32_t row) { return d.ids ? (uint32_t)d.ids[row] : row; }
+
+// eight cells of a row at column 8 group: dropped ones become 0 whatever they are, the others are multiplied by `scale`
+__device__ __forceinline__ void mask8(const Drop &d, uint32_t id, uint32_t group, float scale, float (&v)[8])
+{
+    uint32_t w[4];
+    mask_bits(d, id, group, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = mask_keeps(d, w, i) ? v[i] * scale : 0.0f;
+}
+
+// ---- eight consecutive elements -------------------------------------------------------------------------------------------------
+// Rows may start at any element: wide accesses at any alignment are what global memory on this chip takes.
+
+template <class T> __device__ __forceinline__ void load8(const T *p, float (&v)[8])
+{
+    T t[8];
+    __builtin_memcpy(t, p, sizeof t);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)t[i];
+}
+
+// the first `n` of eight elements; 0 for the others
+template <class T> __device__ __forceinline__ void load8(const T *p, int n, float (&v)[8])
+{
+    if (n >= 8) {
+        load8(p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
+    }
+}
+
+template <class T> __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])
+{
+    T t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = (T)v[i];
+    if (n >= 8) {
+        __builtin_memcpy(p, t, sizeof t);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = t[i];
+    }
+}
+
+// ---- activations, fp32 ----------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ float act_of(int act, float z)
+{
+    if (act == ZG_ACT_RELU) return z > 0.0f ? z : z != z ? z : 0.0f; // (not a number stays that)
+    if (act == ZG_ACT_SILU) return z / (1.0f + expf(-z));
+    if (act == ZG_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    return z;
+}
+
+__device__ __forceinline__ float act_slope(int act, float z)
+{
+    if (act == ZG_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if (act == ZG_ACT_SILU) {
+        const float g = 1.0f / (1.0f + expf(-z));
+        return g * (1.0f + z * (1.0f - g));
+    }
+    if (act == ZG_ACT_GELU)
+        return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+    return 1.0f;
+}
+
+#endif
+
+} // namespace zg

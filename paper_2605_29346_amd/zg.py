@@ -17,6 +17,9 @@ LOG_STRIDE = 32
 
 OK, EINVAL, ENOMEM, EHIP, ESTATE = 0, -1, -2, -3, -4
 I32, I64 = 0, 1
+F32, F16, BF16, F8 = 2, 3, 4, 5
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
+MAX_WIDTH, MAX_NORM_WIDTH = 32768, 16384
 GRAPH_VALIDATE = 1
 PLAN_EAGER, PLAN_REPLACE, PLAN_SAFE_TWIN, PLAN_FUSED_INPUT, PLAN_AUTO_FALLBACK = 1, 2, 4, 8, 16
 PLAN_X_ONE_PASS, PLAN_X_TWO_PASS = 32, 64
@@ -36,7 +39,9 @@ EXPORTS = ["zg_strerror", "zg_last_error", "zg_graph_create", "zg_graph_create_s
            "zg_plan_destroy", "zg_plan_bind_features", "zg_plan_outputs", "zg_step", "zg_gather",
            "zg_aggregate_mean", "zg_overflow_flag", "zg_overflow_clear", "zg_step_safe", "zg_plan_outputs_safe",
            "zg_step_status", "zg_envelope_model_graph", "zg_envelope_from_pilot", "zg_pilot_update", "zg_build_id",
-           "zg_calibration_copy", "zg_envelope_model_graph_static", "zg_plan_replay_features", "zg_step_timed"]
+           "zg_calibration_copy", "zg_envelope_model_graph_static", "zg_plan_replay_features", "zg_step_timed",
+           "zg_linear", "zg_linear_backward_workspace", "zg_linear_backward", "zg_dropout", "zg_rms_norm",
+           "zg_rms_norm_backward_workspace", "zg_rms_norm_backward"]
 
 
 class Envelope(C.Structure):
@@ -69,6 +74,42 @@ class Outputs(C.Structure):
                 ("d_X", C.c_void_p), ("ldx", C.c_int64), ("d_agg", C.c_void_p), ("ld_agg", C.c_int64),
                 ("d_log", C.c_void_p), ("log_capacity", C.c_int32), ("d_epoch", C.c_void_p), ("x_row_cap", C.c_int64),
                 ("d_active", C.c_void_p), ("x_one_pass", C.c_int32), ("reserved", C.c_int32)]
+
+
+class Drop(C.Structure):
+    _fields_ = [("p", C.c_double), ("key", C.c_uint64), ("layer", C.c_uint32), ("reserved", C.c_uint32), ("d_ids", C.c_void_p)]
+
+
+def _matrices(*names):
+    return [f for n in names for f in (("d_" + n, C.c_void_p), ("ld_" + n, C.c_int64))]
+
+
+_ROWS = [("rows", C.c_int64), ("d_rows", C.c_void_p)]
+
+
+class LinearArgs(C.Structure):
+    _fields_ = _ROWS + [("in_", C.c_int32), ("out", C.c_int32), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("act", C.c_int32),
+                        ("reserved", C.c_int32)] + _matrices("A") + [("d_scale_A", C.c_void_p)] + _matrices("W") + [
+                            ("d_scale_W", C.c_void_p), ("d_bias", C.c_void_p)] + _matrices("R", "Y", "Z") + [("drop", Drop)]
+
+
+class LinearGradArgs(C.Structure):
+    _fields_ = _ROWS + [("in_", C.c_int32), ("out", C.c_int32), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("act", C.c_int32),
+                        ("reserved", C.c_int32)] + _matrices("dY", "Z", "A", "W", "dA", "dW") + [("d_dbias", C.c_void_p), ("drop", Drop)]
+
+
+class DropoutArgs(C.Structure):
+    _fields_ = _ROWS + [("cols", C.c_int32), ("dtype", C.c_int32)] + _matrices("x", "r", "y") + [("drop", Drop)]
+
+
+class NormArgs(C.Structure):
+    _fields_ = _ROWS + [("cols", C.c_int32), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("eps", C.c_float)] + _matrices(
+        "x", "r") + [("d_gain", C.c_void_p)] + _matrices("h", "y") + [("d_scale", C.c_void_p), ("d_rstd", C.c_void_p), ("drop", Drop)]
+
+
+class NormGradArgs(C.Structure):
+    _fields_ = _ROWS + [("cols", C.c_int32), ("dtype", C.c_int32)] + _matrices("dy", "h") + [
+        ("d_rstd", C.c_void_p), ("d_gain", C.c_void_p)] + _matrices("dh", "dx", "dr") + [("d_dgain", C.c_void_p), ("drop", Drop)]
 
 
 _lib = None
@@ -125,6 +166,13 @@ def lib() -> C.CDLL:
         L.zg_calibration_copy.argtypes = [vp, vp, C.c_size_t, vp]
         L.zg_plan_replay_features.argtypes = [vp, i32, vp]
         L.zg_step_timed.argtypes = [vp, vp, u64, vp, vp, vp]
+        L.zg_linear.argtypes = [P(LinearArgs), vp]
+        L.zg_linear_backward_workspace.argtypes = [P(LinearGradArgs), P(C.c_size_t)]
+        L.zg_linear_backward.argtypes = [P(LinearGradArgs), vp, C.c_size_t, vp]
+        L.zg_dropout.argtypes = [P(DropoutArgs), vp]
+        L.zg_rms_norm.argtypes = [P(NormArgs), vp]
+        L.zg_rms_norm_backward_workspace.argtypes = [P(NormGradArgs), P(C.c_size_t)]
+        L.zg_rms_norm_backward.argtypes = [P(NormGradArgs), vp, C.c_size_t, vp]
         for name in EXPORTS:
             if name not in ("zg_strerror", "zg_last_error", "zg_normal_quantile", "zg_build_id"):
                 getattr(L, name).restype = C.c_int
