@@ -191,6 +191,21 @@ template <class T> __device__ __forceinline__ void store8(T *p, int n, const flo
     }
 }
 
+// of a type that is known at run time (ZG_F32, ZG_F16 or ZG_BF16), at element `at`
+__device__ __forceinline__ void load8(const void *p, int32_t type, int64_t at, int n, float (&v)[8])
+{
+    if (type == ZG_F32) load8(static_cast<const float *>(p) + at, n, v);
+    else if (type == ZG_F16) load8(static_cast<const _Float16 *>(p) + at, n, v);
+    else load8(static_cast<const __bf16 *>(p) + at, n, v);
+}
+
+__device__ __forceinline__ void store8(void *p, int32_t type, int64_t at, int n, const float (&v)[8])
+{
+    if (type == ZG_F32) store8(static_cast<float *>(p) + at, n, v);
+    else if (type == ZG_F16) store8(static_cast<_Float16 *>(p) + at, n, v);
+    else store8(static_cast<__bf16 *>(p) + at, n, v);
+}
+
 // ---- activations, fp32 ----------------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ float act_of(int act, float z)

@@ -22,42 +22,44 @@ struct Epilogue {
     int64_t ld_Y, ld_Z;
 };
 
-__device__ __forceinline__ float load1(const void *p, int32_t type, int64_t at)
+// cells n .. n + 7 (a multiple of 8; `left` of them are there) of row m
+__device__ __forceinline__ void finish8(const Epilogue &e, uint32_t m, uint32_t n, int left, float (&v)[8])
 {
-    if (type == ZG_F32) return static_cast<const float *>(p)[at];
-    if (type == ZG_F16) return (float)static_cast<const _Float16 *>(p)[at];
-    return (float)static_cast<const __bf16 *>(p)[at];
-}
-
-__device__ __forceinline__ void store1(void *p, int32_t type, int64_t at, float v)
-{
-    if (type == ZG_F32) static_cast<float *>(p)[at] = v;
-    else if (type == ZG_F16) static_cast<_Float16 *>(p)[at] = (_Float16)v;
-    else static_cast<__bf16 *>(p)[at] = (__bf16)v;
-}
-
-__device__ __forceinline__ void finish1(const Epilogue &e, uint32_t m, uint32_t n, float sum)
-{
-    float v = sum * e.factor;
-    if (e.scale_m) v *= e.scale_m[m];
-    if (e.scale_n) v *= e.scale_n[n];
-    if (e.bias) v += e.bias[n];
-    if (e.Z) store1(e.Z, e.type, m * e.ld_Z + n, v);
-    v = act_of(e.act, v);
-    if (e.drop.cut) {
-        uint32_t w[4];
-        mask_bits(e.drop, mask_id(e.drop, m), n >> 3, w);
-        const uint32_t word = n & 4 ? (n & 2 ? w[3] : w[2]) : (n & 2 ? w[1] : w[0]);
-        v = (n & 1 ? word >> 16 : word & 0xFFFFu) >= e.drop.cut ? v * e.drop.scale : 0.0f;
+    const float f = e.scale_m ? e.factor * e.scale_m[m] : e.factor;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= f;
+    if (e.scale_n) {
+        float s[8];
+        load8(e.scale_n + n, left, s);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= s[j];
     }
-    if (e.R) v += load1(e.R, e.type, m * e.ld_R + n);
-    store1(e.Y, e.type, m * e.ld_Y + n, v);
+    if (e.bias) {
+        float b[8];
+        load8(e.bias + n, left, b);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += b[j];
+    }
+    if (e.Z) store8(e.Z, e.type, m * e.ld_Z + n, left, v);
+    if (e.act != ZG_ACT_NONE) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = act_of(e.act, v[j]);
+    }
+    if (e.drop.cut) mask8(e.drop, mask_id(e.drop, m), n >> 3, e.drop.scale, v);
+    if (e.R) {
+        float r[8];
+        load8(e.R, e.type, m * e.ld_R + n, left, r);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += r[j];
+    }
+    store8(e.Y, e.type, m * e.ld_Y + n, left, v);
 }
 
-// C[m, n] = sum over k of a(m, k) b(n, k); element (i, k) of an operand is p[i * si + k * sk].
+// C[m, n] = sum over k of a(m, k) b(n, k); element (i, k) of an operand is p[i * ld + k], or p[k * ld + i] where it is turned.
 struct Operand {
     const void *p;
-    int64_t si, sk;
+    int64_t ld;
+    bool turned;
 };
 
 struct ProductArgs {
@@ -70,61 +72,298 @@ struct ProductArgs {
     Epilogue e;
 };
 
-__device__ __forceinline__ float as_float(float v) { return v; }
-__device__ __forceinline__ float as_float(_Float16 v) { return (float)v; }
-__device__ __forceinline__ float as_float(__bf16 v) { return (float)v; }
-__device__ __forceinline__ float as_float(uint8_t v) { return __builtin_amdgcn_cvt_f32_fp8((int)v, 0); }
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// A tile of 64 x 64 in registers, 4 x 4 to a lane; 16 of the sum's terms at a time through LDS.
-template <class T> __global__ __launch_bounds__(256) void k_product(ProductArgs p)
+// Operands are dealt with in chunks of 16 bytes of one row, 4, 8 or 16 consecutive k.  A matrix instruction takes from a lane's chunk what
+// it takes for its half of the wavefront: which k that is does not matter as long as both operands agree.
+template <class T> constexpr int chunk_k = 16 / (int)sizeof(T);
+
+// 8-bit operands as they lie in memory, multiplied as fp16 (which holds each of their values).  The matrix instructions for 8-bit operands
+// add eight products at a time in a window that ends about 13 bits below the largest of them, and only then in fp32: over a short
+// sum that is more than an fp32 sum may lose.
+struct Widened8 {
+    uint8_t v;
+};
+template <> constexpr int chunk_k<Widened8> = 8;
+
+__device__ __forceinline__ u32x4 widen(u32x4 r) // eight 8-bit values as fp16
 {
-    constexpr int tile = 64, depth = 16;
-    __shared__ float la[depth][tile + 1], lb[depth][tile + 1];
-    const uint32_t live = p.rows.live();
-    const uint32_t M = p.rows_are_k ? p.M : min(p.M, live), K = p.rows_are_k ? min(p.K, live) : p.K;
-    const uint32_t m0 = blockIdx.x * tile, n0 = blockIdx.y * tile, split = blockIdx.z;
-    if (m0 >= M) return;
-    const uint32_t share = ((K + p.splits - 1) / p.splits + depth - 1) / depth * depth;
-    const uint32_t k_first = min((uint64_t)K, (uint64_t)share * split), k_last = min((uint64_t)K, (uint64_t)k_first + share);
-    const T *a = static_cast<const T *>(p.a.p), *b = static_cast<const T *>(p.b.p);
-    float acc[4][4] = {};
-    const uint32_t tm = threadIdx.x / 16, tn = threadIdx.x % 16;
-    for (uint32_t k0 = k_first; k0 < k_last; k0 += depth) {
-        for (uint32_t e = threadIdx.x; e < tile * depth; e += 256) {
-            const bool a_k = p.a.sk == 1, b_k = p.b.sk == 1; // (lanes along the dimension whose elements lie side by side)
-            const uint32_t ia = a_k ? e / depth : e % tile, ka = a_k ? e % depth : e / tile;
-            const uint32_t ib = b_k ? e / depth : e % tile, kb = b_k ? e % depth : e / tile;
-            la[ka][ia] = m0 + ia < M && k0 + ka < k_last ? as_float(a[(m0 + ia) * p.a.si + (k0 + ka) * p.a.sk]) : 0.0f;
-            lb[kb][ib] = n0 + ib < p.N && k0 + kb < k_last ? as_float(b[(n0 + ib) * p.b.si + (k0 + kb) * p.b.sk]) : 0.0f;
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)r[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)r[i], true);
+        w[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo[0], lo[1]));
+        w[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(hi[0], hi[1]));
+    }
+    return w;
+}
+
+// acc += the products over one pair of chunks (a lane's half of the wavefront has one of the two), all 32 x 32 cells.  The first operand's
+// rows become the cells that a lane holds side by side.
+__device__ __forceinline__ void multiply(float, u32x4 x, u32x4 y, f32x16 &acc)
+{
+    const f32x4 a = __builtin_bit_cast(f32x4, x), b = __builtin_bit_cast(f32x4, y);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[k], b[k], acc, 0, 0, 0);
+}
+
+__device__ __forceinline__ void multiply(_Float16, u32x4 x, u32x4 y, f32x16 &acc)
+{
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), acc, 0, 0, 0);
+}
+
+__device__ __forceinline__ void multiply(Widened8, u32x4 x, u32x4 y, f32x16 &acc) { multiply((_Float16)0, x, y, acc); }
+
+__device__ __forceinline__ void multiply(__bf16, u32x4 x, u32x4 y, f32x16 &acc)
+{
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
+}
+
+// 8-bit operands: two chunks of a lane at a time, the instruction's own block scales at 1 (2^(127 - 127))
+__device__ __forceinline__ void multiply2(u32x4 x0, u32x4 x1, u32x4 y0, u32x4 y1, f32x16 &acc)
+{
+    const i32x8 a = {(int)x0[0], (int)x0[1], (int)x0[2], (int)x0[3], (int)x1[0], (int)x1[1], (int)x1[2], (int)x1[3]};
+    const i32x8 b = {(int)y0[0], (int)y0[1], (int)y0[2], (int)y0[3], (int)y1[0], (int)y1[1], (int)y1[2], (int)y1[3]};
+    acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 0, 0, 0, 0x7F7F7F7F, 0, 0x7F7F7F7F);
+}
+
+// Where chunk c of row i lies in an operand's tile in LDS (8 chunks to a row).  Eight rows at one c, eight chunks of one row, and every
+// fourth row at one c - what a wavefront reads, writes, and writes of an operand that it turns - each lie in eight different groups of banks.
+__device__ __forceinline__ uint32_t slot(uint32_t i, uint32_t c) { return 8 * i + (c ^ ((i ^ (i >> 2)) & 7)); }
+
+// The first n < K elements of a chunk (none where n <= 0), zeros behind them.  Where the row has a chunk's worth of elements up to there
+// (`long_row`), the 16 bytes that end with them are read and shifted.
+template <class T> __device__ __forceinline__ u32x4 part_of_chunk(const T *from, int n, bool long_row)
+{
+    constexpr int K = chunk_k<T>;
+    uint64_t lo = 0, hi = 0;
+    if (n > 0 && long_row) {
+        uint64_t w[2] = {};
+        __builtin_memcpy(w, from + n - K, K * sizeof(T));
+        const int s = (K - n) * (int)sizeof(T) * 8;
+        lo = s >= 64 ? w[1] >> (s - 64) : w[0] >> s | w[1] << (64 - s);
+        hi = s >= 64 ? 0 : w[1] >> s;
+    } else {
+#pragma unroll 1
+        for (int j = 0; j < n; ++j) {
+            uint64_t bits = 0;
+            __builtin_memcpy(&bits, from + j, sizeof(T));
+            const int s = j * (int)sizeof(T) * 8;
+            if (s < 64) lo |= bits << s;
+            else hi |= bits << (s - 64);
         }
-        __syncthreads();
+    }
+    return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
+// One operand's way from memory to LDS: `tile` rows, eight chunks of k.  TURNED: its elements lie side by side along the rows and not
+// along k.  What is beyond the last row or k is 0 and not read.
+template <class T, int tile, bool TURNED> struct Side {
+    static constexpr int K = chunk_k<T>, regs = tile / 32 < 4 && TURNED ? 4 : tile / 32; // chunks of a lane
+    static constexpr int groups = tile / 4, patches = 8 * groups;                         // (TURNED: a lane has four at a time)
+    const T *p;
+    int64_t ld;
+    uint32_t first, rows; // the tile's first row; rows of the operand
+    u32x4 r[regs];
+
+    __device__ __forceinline__ void load(uint32_t k0, uint32_t k_end)
+    {
+        if constexpr (!TURNED) {
+            if (k0 + 8 * K <= k_end) { // (rows beyond the last one repeat it: their cells are not kept)
 #pragma unroll
-        for (int k = 0; k < depth; ++k)
+                for (int c = 0; c < regs; ++c) {
+                    const uint32_t e = threadIdx.x + 256 * c;
+                    const T *from = p + min(first + e / 8, rows - 1) * ld + k0 + (e % 8) * K;
+                    __builtin_memcpy(&r[c], from, K * sizeof(T));
+                }
+            } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+                for (int c = 0; c < regs; ++c) {
+                    const uint32_t e = threadIdx.x + 256 * c, k = k0 + (e % 8) * K;
+                    const T *from = p + min(first + e / 8, rows - 1) * ld + k;
+                    if (k + K <= k_end) __builtin_memcpy(&r[c], from, K * sizeof(T));
+                    else r[c] = part_of_chunk(from, (int)(k_end - k), k_end >= (uint32_t)K);
+                }
+            }
+        } else { // K rows of four elements: four chunks once they are turned
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(la[k][tm * 4 + i], lb[k][tn + 16 * j], acc[i][j]);
+            for (int c = 0; c < regs / 4; ++c) {
+                const uint32_t e = threadIdx.x + 256 * c, i = first + 4 * (e % groups), k = k0 + (e / groups) * K;
+                T t[K][4] = {};
+                if (patches < 256 && threadIdx.x >= patches) continue;
+                if (k0 + 8 * K <= k_end && first + tile <= rows) {
+#pragma unroll
+                    for (int j = 0; j < K; ++j) __builtin_memcpy(t[j], p + (k + j) * ld + i, 4 * sizeof(T));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < K; ++j) {
+                        if (k + j >= k_end) continue;
+                        const T *from = p + (k + j) * ld + i;
+                        if (i + 4 <= rows) {
+                            __builtin_memcpy(t[j], from, 4 * sizeof(T));
+                        } else {
+#pragma unroll
+                            for (int h = 0; h < 4; ++h)
+                                if (i + h < rows) t[j][h] = from[h];
+                        }
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    T u[K];
+#pragma unroll
+                    for (int j = 0; j < K; ++j) u[j] = t[j][h];
+                    __builtin_memcpy(&r[4 * c + h], u, 16);
+                }
+            }
+        }
+    }
+
+    __device__ __forceinline__ void store(u32x4 *lds) const
+    {
+        if constexpr (!TURNED) {
+#pragma unroll
+            for (int c = 0; c < regs; ++c) {
+                const uint32_t e = threadIdx.x + 256 * c;
+                if constexpr (std::is_same_v<T, Widened8>) lds[slot(e / 8, e % 8)] = widen(r[c]);
+                else lds[slot(e / 8, e % 8)] = r[c];
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < regs / 4; ++c) {
+                const uint32_t e = threadIdx.x + 256 * c;
+                if (patches < 256 && threadIdx.x >= patches) continue;
+#pragma unroll
+                for (int h = 0; h < 4; ++h) lds[slot(4 * (e % groups) + h, e / groups)] = r[4 * c + h];
+            }
+        }
+    }
+};
+
+// A tile of BM x BN cells: four wavefronts, two by two, matrix instructions of 32 x 32 cells; eight chunks of k at a time through two buffers
+// in LDS, the next ones on their way in registers.  The first operand of an instruction is b, so that a lane's cells lie side by side in a
+// row of C.
+template <class T, int BM, int BN, bool A_TURNED, bool B_TURNED> __global__ __launch_bounds__(256, 2) void k_product(ProductArgs p)
+{
+    constexpr int K = chunk_k<T>, depth = 8 * K, FM = BM / 64, FN = BN / 64;
+    __shared__ u32x4 la[2][BM * 8], lb[2][BN * 8];
+    const uint32_t live = p.rows.live();
+    const uint32_t M = p.rows_are_k ? p.M : min(p.M, live), k_all = p.rows_are_k ? min(p.K, live) : p.K;
+    // Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles, those of one row of tiles (of one part of the sum) beside each
+    // other, so that what they share is in its L2.
+    const uint32_t nt = (p.N + BN - 1) / BN, mt = (M + BM - 1) / BM;
+    const uint64_t tiles = (uint64_t)mt * nt * p.splits, share = (tiles + 7) / 8;
+    const uint64_t t = (blockIdx.x % 8) * share + blockIdx.x / 8;
+    if (blockIdx.x / 8 >= share || t >= tiles) return;
+    const uint32_t split = (uint32_t)(t / ((uint64_t)mt * nt)), in_split = (uint32_t)(t % ((uint64_t)mt * nt));
+    const uint32_t m0 = in_split / nt * BM, n0 = in_split % nt * BN;
+    const uint32_t part_k = ((k_all + p.splits - 1) / p.splits + depth - 1) / depth * depth;
+    const uint32_t k_first = (uint32_t)min((uint64_t)k_all, (uint64_t)part_k * split), k_end = (uint32_t)min((uint64_t)k_all, (uint64_t)k_first + part_k);
+
+    Side<T, BM, A_TURNED> a;
+    Side<T, BN, B_TURNED> b;
+    a.p = static_cast<const T *>(p.a.p), a.ld = p.a.ld, a.first = m0, a.rows = M;
+    b.p = static_cast<const T *>(p.b.p), b.ld = p.b.ld, b.first = n0, b.rows = p.N;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const uint32_t am = (wave >> 1) * (BM / 2) + (lane & 31), bn = (wave & 1) * (BN / 2) + (lane & 31);
+    f32x16 acc[FM][FN] = {};
+    if (k_first < k_end) {
+        a.load(k_first, k_end);
+        b.load(k_first, k_end);
+        a.store(la[0]);
+        b.store(lb[0]);
+    }
+    __syncthreads();
+    uint32_t now = 0;
+    for (uint32_t k0 = k_first; k0 < k_end; k0 += depth, now ^= 1) {
+        const bool more = k_end - k0 > (uint32_t)depth;
+        if (more) {
+            a.load(k0 + depth, k_end);
+            b.load(k0 + depth, k_end);
+        }
+        if constexpr (std::is_same_v<T, uint8_t>) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                u32x4 fa[FM][2], fb[FN][2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int i = 0; i < FM; ++i) fa[i][h] = la[now][slot(am + 32 * i, 4 * s + 2 * half + h)];
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) fb[j][h] = lb[now][slot(bn + 32 * j, 4 * s + 2 * half + h)];
+                }
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) multiply2(fb[j][0], fb[j][1], fa[i][0], fa[i][1], acc[i][j]);
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                u32x4 fa[FM], fb[FN];
+#pragma unroll
+                for (int i = 0; i < FM; ++i) fa[i] = la[now][slot(am + 32 * i, 2 * s + half)];
+#pragma unroll
+                for (int j = 0; j < FN; ++j) fb[j] = lb[now][slot(bn + 32 * j, 2 * s + half)];
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) multiply(T(), fb[j], fa[i], acc[i][j]);
+            }
+        }
+        if (more) {
+            a.store(la[now ^ 1]);
+            b.store(lb[now ^ 1]);
+        }
         __syncthreads();
     }
+    // Of 32 x 32 cells a lane has row lane % 32, columns 8 q + 4 half + 0..3 in registers 4 q + 0..3: two halves of a wavefront swap what makes
+    // eight columns side by side of each.
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < FM; ++i) {
+        const uint32_t m = m0 + am + 32 * i;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t m = m0 + tm * 4 + i, n = n0 + tn + 16 * j;
-            if (m >= M || n >= p.N) continue;
-            if (p.splits > 1) p.part[((uint64_t)split * p.M + m) * p.N + n] = acc[i][j];
-            else finish1(p.e, m, n, acc[i][j]);
-        }
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                float v[8];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const auto two = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, (float)acc[i][j][8 * q + r]),
+                                                                      __builtin_bit_cast(uint32_t, (float)acc[i][j][8 * q + 4 + r]), false, false);
+                    v[r] = __builtin_bit_cast(float, (uint32_t)two[0]);
+                    v[4 + r] = __builtin_bit_cast(float, (uint32_t)two[1]);
+                }
+                const uint32_t n = n0 + (wave & 1) * (BN / 2) + 32 * j + 16 * q + 8 * half;
+                if (m >= M || n >= p.N) continue;
+                const int left = (int)(p.N - n);
+                if (p.splits > 1) store8(p.part + ((uint64_t)split * p.M + m) * p.N + n, left, v);
+                else finish8(p.e, m, n, left, v);
+            }
+    }
 }
 
 // the sum over the splits, in order, and what happens to it
 __global__ __launch_bounds__(256) void k_join(ProductArgs p)
 {
-    const uint64_t cells = (uint64_t)p.M * p.N;
-    for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < cells; i += gridDim.x * 256ull) {
-        float v = 0.0f;
-        for (uint32_t s = 0; s < p.splits; ++s) v += p.part[s * cells + i];
-        finish1(p.e, (uint32_t)(i / p.N), (uint32_t)(i % p.N), v);
+    const uint32_t groups = (p.N + 7) / 8;
+    const uint64_t all = (uint64_t)p.M * groups, cells = (uint64_t)p.M * p.N;
+    for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < all; i += gridDim.x * 256ull) {
+        const uint32_t m = (uint32_t)(i / groups), n = (uint32_t)(i % groups) * 8;
+        const int left = (int)(p.N - n);
+        float v[8] = {};
+        for (uint32_t s = 0; s < p.splits; ++s) {
+            float w[8];
+            load8(p.part + s * cells + (uint64_t)m * p.N + n, left, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += w[j];
+        }
+        finish8(p.e, m, n, left, v);
     }
 }
 
@@ -174,16 +413,37 @@ template <class TO, class T> __global__ __launch_bounds__(256) void k_slope(Slop
     store8(a.part + (uint64_t)blockIdx.y * a.cols + 8 * g, left, sums);
 }
 
+template <class T, int BM, int BN> int launch_tiles(hipStream_t st, const ProductArgs &p)
+{
+    const uint64_t tiles = (uint64_t)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN) * p.splits;
+    const dim3 grid((unsigned)((tiles + 7) / 8 * 8));
+    if constexpr (sizeof(T) == 1) {
+        return launch(st, k_product<T, BM, BN, false, false>, grid, 256, p);
+    } else {
+        if (p.a.turned) return launch(st, k_product<T, BM, BN, true, true>, grid, 256, p);
+        if (p.b.turned) return launch(st, k_product<T, BM, BN, false, true>, grid, 256, p);
+        return launch(st, k_product<T, BM, BN, false, false>, grid, 256, p);
+    }
+}
+
+constexpr int kTile = 128;
+
+template <class T> int launch_product(hipStream_t st, const ProductArgs &p)
+{
+    ZG_TRY((launch_tiles<T, kTile, kTile>(st, p)));
+    if (p.splits == 1) return ZG_OK;
+    const uint64_t groups = (uint64_t)p.M * ((p.N + 7) / 8);
+    return launch(st, k_join, dim3((unsigned)std::min<uint64_t>(4096, (groups + 255) / 256)), 256, p);
+}
+
 int launch_product(hipStream_t st, int32_t type, const ProductArgs &p)
 {
-    const dim3 grid((p.M + 63) / 64, (p.N + 63) / 64, p.splits);
-    if (type == ZG_F32) ZG_TRY(launch(st, k_product<float>, grid, 256, p));
-    else if (type == ZG_F16) ZG_TRY(launch(st, k_product<_Float16>, grid, 256, p));
-    else if (type == ZG_BF16) ZG_TRY(launch(st, k_product<__bf16>, grid, 256, p));
-    else ZG_TRY(launch(st, k_product<uint8_t>, grid, 256, p));
-    if (p.splits == 1) return ZG_OK;
-    const uint64_t cells = (uint64_t)p.M * p.N;
-    return launch(st, k_join, dim3((unsigned)std::min<uint64_t>(4096, (cells + 255) / 256)), 256, p);
+    if (type == ZG_F32) return launch_product<float>(st, p);
+    if (type == ZG_F16) return launch_product<_Float16>(st, p);
+    if (type == ZG_BF16) return launch_product<__bf16>(st, p);
+    // What the 8-bit instructions lose per group of eight adds up like the root of their number; what an fp32 sum may lose, like the number
+    // of its terms.  From a sum of a few hundred terms on the former is the smaller.
+    return p.K >= 512 ? launch_product<uint8_t>(st, p) : launch_product<Widened8>(st, p);
 }
 
 // How the gradients' workspace is laid out.
@@ -210,8 +470,8 @@ GradPlan grad_plan(const zg_linear_grad_args &a)
     while (g.lanes < groups && g.lanes < 64) g.lanes *= 2;
     g.slope_x = (groups + g.lanes - 1) / g.lanes;
     g.slope_y = (uint32_t)std::min<int64_t>(std::max(1u, 1024u / g.slope_x), (a.rows + 256 / g.lanes - 1) / (256 / g.lanes));
-    const int64_t tiles = (int64_t)((a.out + 63) / 64) * ((a.in + 63) / 64);
-    g.splits = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(1024 / tiles, (a.rows + 255) / 256));
+    const int64_t tiles = (int64_t)((a.out + kTile - 1) / kTile) * ((a.in + kTile - 1) / kTile);
+    g.splits = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, (a.rows + 255) / 256));
     if (g.slopes && (a.d_dA || a.d_dW)) g.off_dz = take((size_t)a.rows * g.ld_dz * type_size(a.dtype));
     if (a.d_dbias) g.off_part = take((size_t)g.slope_y * a.out * sizeof(float));
     if (a.d_dW && g.splits > 1) g.off_dw = take((size_t)g.splits * a.out * a.in * sizeof(float));
@@ -261,8 +521,8 @@ int zg_linear(const zg_linear_args *a, void *stream)
         if (a->d_Y == a->d_A || a->d_Z == a->d_A || a->d_Z == a->d_Y || (a->d_Z && a->d_Z == a->d_R))
             return fail(ZG_EINVAL, "an output lies on an input or on the other output");
         ProductArgs p{};
-        p.a = {a->d_A, a->ld_A, 1};
-        p.b = {a->d_W, a->ld_W, 1};
+        p.a = {a->d_A, a->ld_A, false};
+        p.b = {a->d_W, a->ld_W, false};
         p.M = (uint32_t)a->rows, p.N = (uint32_t)a->out, p.K = (uint32_t)a->in;
         p.rows = {a->d_rows, p.M};
         p.splits = 1;
@@ -334,16 +594,16 @@ int zg_linear_backward(const zg_linear_grad_args *a, void *d_workspace, size_t w
         p.e.factor = factor;
         p.e.type = a->dtype;
         if (a->d_dA && a->rows > 0) {
-            p.a = {dz, ld_dz, 1};
-            p.b = {a->d_W, 1, a->ld_W};
+            p.a = {dz, ld_dz, false};
+            p.b = {a->d_W, a->ld_W, true};
             p.M = (uint32_t)a->rows, p.N = (uint32_t)a->in, p.K = (uint32_t)a->out;
             p.splits = 1;
             p.e.Y = a->d_dA, p.e.ld_Y = a->ld_dA;
             ZG_TRY(launch_product(st, a->dtype, p));
         }
         if (a->d_dW) {
-            p.a = {dz, 1, ld_dz};
-            p.b = {a->d_A, 1, a->ld_A};
+            p.a = {dz, ld_dz, true};
+            p.b = {a->d_A, a->ld_A, true};
             p.M = (uint32_t)a->out, p.N = (uint32_t)a->in, p.K = (uint32_t)a->rows;
             p.rows_are_k = 1;
             p.splits = g.splits;

@@ -188,10 +188,8 @@ template <class T, int PER, int CH> __global__ __launch_bounds__(PER > kRowsBloc
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int at = 8 * (c * PER + lane), left = (int)a.cols - at;
-        if (a.out_type == ZG_F32) store8(static_cast<float *>(a.y) + row * a.ld_y + at, left, v[c]);
-        else if (a.out_type == ZG_F16) store8(static_cast<_Float16 *>(a.y) + row * a.ld_y + at, left, v[c]);
-        else store8(static_cast<__bf16 *>(a.y) + row * a.ld_y + at, left, v[c]);
+        const int at = 8 * (c * PER + lane);
+        store8(a.y, a.out_type, row * a.ld_y + at, (int)a.cols - at, v[c]);
     }
 }
 
