@@ -245,107 +245,205 @@ template <class T, int tile, bool TURNED> struct Side {
     }
 };
 
+// What a wavefront does with its 32 FM x 64 cells' sums.  Of 32 x 32 cells a lane has row lane % 32, columns 8 q + 4 half + 0..3 in registers
+// 4 q + 0..3: they go through LDS (`mine`: 16 KB of the wavefront's own, free from here on), 64 rows at a time, so that eight lanes have 64 columns of a row
+// and memory sees whole lines.  Places are 16 bytes, 16 to a row, turned by the row so that neither way meets in a bank.
+template <int FM> __device__ __forceinline__ void hand_over(const ProductArgs &p, f32x16 (&acc)[FM][2], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t split)
+{
+    const uint32_t lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31;
+#pragma unroll
+    for (int h = 0; h < FM; h += 2) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t at = (32 * i + row) * 16 + ((8 * j + 2 * q + half) ^ (row & 15));
+                    mine[at] = f32x4{acc[h + i][j][4 * q], acc[h + i][j][4 * q + 1], acc[h + i][j][4 * q + 2], acc[h + i][j][4 * q + 3]};
+                }
+        const uint32_t n = n_wave + 8 * (lane & 7);
+        const int left = (int)(p.N - n);
+        if (n < p.N) { // (a wavefront's LDS accesses are in order)
+#pragma unroll 1
+            for (uint32_t r = lane >> 3; r < 64; r += 8) {
+                const uint32_t m = m_wave + 32 * h + r;
+                if (m >= M) break;
+                const f32x4 lo = mine[r * 16 + ((2 * (lane & 7)) ^ (r & 15))], hi = mine[r * 16 + ((2 * (lane & 7) + 1) ^ (r & 15))];
+                float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                if (p.splits > 1) store8(p.part + ((uint64_t)split * p.M + m) * p.N + n, left, v);
+                else finish8(p.e, m, n, left, v);
+            }
+        }
+    }
+}
+
+// Which tile, and which part of the sum, a workgroup has.  Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles, those of
+// one row of tiles (of one part of the sum) beside each other, so that what they share is in its L2.
+struct Place {
+    uint32_t M, m0, n0, split, k_first, k_end;
+};
+
+template <int BM, int BN> __device__ __forceinline__ bool place_of(const ProductArgs &p, uint32_t depth, Place &w)
+{
+    const uint32_t live = p.rows.live();
+    w.M = p.rows_are_k ? p.M : min(p.M, live);
+    const uint32_t k_all = p.rows_are_k ? min(p.K, live) : p.K;
+    const uint32_t nt = (p.N + BN - 1) / BN, mt = (w.M + BM - 1) / BM;
+    const uint64_t in_part = (uint64_t)mt * nt, tiles = in_part * p.splits, share = (tiles + 7) / 8;
+    const uint64_t t = (blockIdx.x % 8) * share + blockIdx.x / 8;
+    if (blockIdx.x / 8 >= share || t >= tiles) return false;
+    w.split = p.splits > 1 ? (uint32_t)(t / in_part) : 0u;
+    const uint32_t in_split = (uint32_t)(t - w.split * in_part);
+    w.m0 = in_split / nt * BM;
+    w.n0 = in_split % nt * BN;
+    const uint32_t part_k = ((k_all + p.splits - 1) / p.splits + depth - 1) / depth * depth;
+    w.k_first = (uint32_t)min((uint64_t)k_all, (uint64_t)part_k * w.split);
+    w.k_end = (uint32_t)min((uint64_t)k_all, (uint64_t)w.k_first + part_k);
+    return true;
+}
+
 // A tile of BM x BN cells: four wavefronts, two by two, matrix instructions of 32 x 32 cells; eight chunks of k at a time through two buffers
 // in LDS, the next ones on their way in registers.  The first operand of an instruction is b, so that a lane's cells lie side by side in a
-// row of C.
+// row of C.  For operands that lie anyhow.
 template <class T, int BM, int BN, bool A_TURNED, bool B_TURNED> __global__ __launch_bounds__(256, 2) void k_product(ProductArgs p)
 {
     constexpr int K = chunk_k<T>, depth = 8 * K, FM = BM / 64, FN = BN / 64;
-    __shared__ u32x4 la[2][BM * 8], lb[2][BN * 8];
-    const uint32_t live = p.rows.live();
-    const uint32_t M = p.rows_are_k ? p.M : min(p.M, live), k_all = p.rows_are_k ? min(p.K, live) : p.K;
-    // Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles, those of one row of tiles (of one part of the sum) beside each
-    // other, so that what they share is in its L2.
-    const uint32_t nt = (p.N + BN - 1) / BN, mt = (M + BM - 1) / BM;
-    const uint64_t tiles = (uint64_t)mt * nt * p.splits, share = (tiles + 7) / 8;
-    const uint64_t t = (blockIdx.x % 8) * share + blockIdx.x / 8;
-    if (blockIdx.x / 8 >= share || t >= tiles) return;
-    const uint32_t split = (uint32_t)(t / ((uint64_t)mt * nt)), in_split = (uint32_t)(t % ((uint64_t)mt * nt));
-    const uint32_t m0 = in_split / nt * BM, n0 = in_split % nt * BN;
-    const uint32_t part_k = ((k_all + p.splits - 1) / p.splits + depth - 1) / depth * depth;
-    const uint32_t k_first = (uint32_t)min((uint64_t)k_all, (uint64_t)part_k * split), k_end = (uint32_t)min((uint64_t)k_all, (uint64_t)k_first + part_k);
-
+    __shared__ u32x4 lds[2][(BM + BN) * 8];
+    Place w;
+    if (!place_of<BM, BN>(p, depth, w)) return;
+    const uint32_t k_end = w.k_end;
     Side<T, BM, A_TURNED> a;
     Side<T, BN, B_TURNED> b;
-    a.p = static_cast<const T *>(p.a.p), a.ld = p.a.ld, a.first = m0, a.rows = M;
-    b.p = static_cast<const T *>(p.b.p), b.ld = p.b.ld, b.first = n0, b.rows = p.N;
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-    const uint32_t am = (wave >> 1) * (BM / 2) + (lane & 31), bn = (wave & 1) * (BN / 2) + (lane & 31);
+    a.p = static_cast<const T *>(p.a.p), a.ld = p.a.ld, a.first = w.m0, a.rows = w.M;
+    b.p = static_cast<const T *>(p.b.p), b.ld = p.b.ld, b.first = w.n0, b.rows = p.N;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const uint32_t wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2), am = wm + (lane & 31), bn = wn + (lane & 31);
     f32x16 acc[FM][FN] = {};
-    if (k_first < k_end) {
-        a.load(k_first, k_end);
-        b.load(k_first, k_end);
-        a.store(la[0]);
-        b.store(lb[0]);
+    if (w.k_first < k_end) {
+        a.load(w.k_first, k_end);
+        b.load(w.k_first, k_end);
+        a.store(lds[0]);
+        b.store(lds[0] + BM * 8);
     }
     __syncthreads();
     uint32_t now = 0;
-    for (uint32_t k0 = k_first; k0 < k_end; k0 += depth, now ^= 1) {
+    for (uint32_t k0 = w.k_first; k0 < k_end; k0 += depth, now ^= 1) {
         const bool more = k_end - k0 > (uint32_t)depth;
         if (more) {
             a.load(k0 + depth, k_end);
             b.load(k0 + depth, k_end);
         }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            u32x4 fa[FM], fb[FN];
+#pragma unroll
+            for (int i = 0; i < FM; ++i) fa[i] = lds[now][slot(am + 32 * i, 2 * s + half)];
+#pragma unroll
+            for (int j = 0; j < FN; ++j) fb[j] = lds[now][BM * 8 + slot(bn + 32 * j, 2 * s + half)];
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) multiply(T(), fb[j], fa[i], acc[i][j]);
+        }
+        if (more) {
+            a.store(lds[now ^ 1]);
+            b.store(lds[now ^ 1] + BM * 8);
+        }
+        __syncthreads();
+    }
+    hand_over(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 1024, w.m0 + wm, w.n0 + wn, w.M, w.split);
+}
+
+// ---- operands in whole chunks ---------------------------------------------------------------------------------------------------
+// Where both operands' rows start on 16-byte boundaries and are whole chunks long, chunks go from memory to LDS without passing through
+// registers, two steps ahead of the one that is multiplied: three buffers of four chunks (64 bytes) of k for every row of the tile.  A
+// wavefront has 128 x 64 cells of a workgroup's 256 x 128.
+
+__device__ __forceinline__ uint32_t slot4(uint32_t i, uint32_t c) { return (i >> 1) * 8 + (i & 1) * 4 + (c ^ ((i >> 1) & 3)); }
+
+constexpr uint32_t kReach = 0x80000000u; // bytes that a tile's rows may span: offsets from here on read zeros
+
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+
+template <int n> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory"); }
+
+template <class T, int BM, int BN> __global__ __launch_bounds__(256, 2) void k_chunks(ProductArgs p)
+{
+    constexpr int K = 16 / (int)sizeof(T), depth = 4 * K, FM = BM / 64, FN = BN / 64, stages = 3;
+    constexpr int loads_a = BM * 4 / 256, loads_b = BN * 4 / 256, loads = loads_a + loads_b; // of a lane for a step
+    __shared__ u32x4 lds[stages][(BM + BN) * 4];
+    Place w;
+    if (!place_of<BM, BN>(p, depth, w)) return;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const uint32_t wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2), am = wm + (lane & 31), bn = wn + (lane & 31);
+    const T *const a0 = static_cast<const T *>(p.a.p) + (int64_t)w.m0 * p.a.ld, *const b0 = static_cast<const T *>(p.b.p) + (int64_t)w.n0 * p.b.ld;
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(a0), 0, kReach, 0x00027000);
+    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(b0), 0, kReach, 0x00027000);
+    // where this lane's chunks are: 64 consecutive places of LDS are filled by one instruction of a wavefront
+    uint32_t from[loads], chunk = 0;
+#pragma unroll
+    for (int l = 0; l < loads; ++l) {
+        const bool is_a = l < loads_a;
+        const uint32_t s = (wave * (is_a ? loads_a : loads_b) + (is_a ? l : l - loads_a)) * 64 + lane, pair = s / 8, i = 2 * pair + ((s >> 2) & 1);
+        chunk = (s & 3) ^ (pair & 3); // (the same for every l: 64 places are 8 pairs)
+        const uint32_t rows = is_a ? w.M - w.m0 : p.N - w.n0;
+        from[l] = i < rows ? i * (uint32_t)((is_a ? p.a.ld : p.b.ld) * sizeof(T)) + chunk * 16 : kReach;
+    }
+    const auto fetch = [&](uint32_t k0, int stage) {
+        const uint32_t beyond = k0 + (chunk + 1) * K <= w.k_end ? 0 : kReach;
+        const int at = (int)(k0 * sizeof(T));
+#pragma unroll
+        for (int l = 0; l < loads; ++l) {
+            const bool is_a = l < loads_a;
+            u32x4 *to = &lds[stage][is_a ? (wave * loads_a + l) * 64 : BM * 4 + (wave * loads_b + l - loads_a) * 64];
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? ra : rb, (lds_u32x4 *)to, 16, (int)(from[l] | beyond), at, 0, 0);
+        }
+    };
+    f32x16 acc[FM][FN] = {};
+    const uint32_t steps = (w.k_end - w.k_first + depth - 1) / depth;
+    if (steps > 0) fetch(w.k_first, 0);
+    if (steps > 1) fetch(w.k_first + depth, 1);
+    int now = 0, next = 2;
+    for (uint32_t t = 0; t < steps; ++t) {
+        if (t + 1 < steps) wait_loads<loads>();
+        else wait_loads<0>();
+        __builtin_amdgcn_s_barrier(); // every wavefront's chunks of this step are there, and the step before is multiplied
+        asm volatile("" ::: "memory");
+        if (t + 2 < steps) fetch(w.k_first + (t + 2) * depth, next);
+        const u32x4 *la = lds[now], *lb = lds[now] + BM * 4;
         if constexpr (std::is_same_v<T, uint8_t>) {
+            u32x4 fa[FM][2], fb[FN][2];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                u32x4 fa[FM][2], fb[FN][2];
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int i = 0; i < FM; ++i) fa[i][h] = la[slot4(am + 32 * i, 2 * half + h)];
 #pragma unroll
-                    for (int i = 0; i < FM; ++i) fa[i][h] = la[now][slot(am + 32 * i, 4 * s + 2 * half + h)];
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) fb[j][h] = lb[now][slot(bn + 32 * j, 4 * s + 2 * half + h)];
-                }
-#pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) multiply2(fb[j][0], fb[j][1], fa[i][0], fa[i][1], acc[i][j]);
+                for (int j = 0; j < FN; ++j) fb[j][h] = lb[slot4(bn + 32 * j, 2 * half + h)];
             }
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) multiply2(fb[j][0], fb[j][1], fa[i][0], fa[i][1], acc[i][j]);
         } else {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
+            for (int s = 0; s < 2; ++s) {
                 u32x4 fa[FM], fb[FN];
 #pragma unroll
-                for (int i = 0; i < FM; ++i) fa[i] = la[now][slot(am + 32 * i, 2 * s + half)];
+                for (int i = 0; i < FM; ++i) fa[i] = la[slot4(am + 32 * i, 2 * s + half)];
 #pragma unroll
-                for (int j = 0; j < FN; ++j) fb[j] = lb[now][slot(bn + 32 * j, 2 * s + half)];
+                for (int j = 0; j < FN; ++j) fb[j] = lb[slot4(bn + 32 * j, 2 * s + half)];
 #pragma unroll
                 for (int i = 0; i < FM; ++i)
 #pragma unroll
                     for (int j = 0; j < FN; ++j) multiply(T(), fb[j], fa[i], acc[i][j]);
             }
         }
-        if (more) {
-            a.store(la[now ^ 1]);
-            b.store(lb[now ^ 1]);
-        }
-        __syncthreads();
+        now = now == stages - 1 ? 0 : now + 1;
+        next = next == stages - 1 ? 0 : next + 1;
     }
-    // Of 32 x 32 cells a lane has row lane % 32, columns 8 q + 4 half + 0..3 in registers 4 q + 0..3: two halves of a wavefront swap what makes
-    // eight columns side by side of each.
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const uint32_t m = m0 + am + 32 * i;
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                float v[8];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const auto two = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, (float)acc[i][j][8 * q + r]),
-                                                                      __builtin_bit_cast(uint32_t, (float)acc[i][j][8 * q + 4 + r]), false, false);
-                    v[r] = __builtin_bit_cast(float, (uint32_t)two[0]);
-                    v[4 + r] = __builtin_bit_cast(float, (uint32_t)two[1]);
-                }
-                const uint32_t n = n0 + (wave & 1) * (BN / 2) + 32 * j + 16 * q + 8 * half;
-                if (m >= M || n >= p.N) continue;
-                const int left = (int)(p.N - n);
-                if (p.splits > 1) store8(p.part + ((uint64_t)split * p.M + m) * p.N + n, left, v);
-                else finish8(p.e, m, n, left, v);
-            }
-    }
+    __syncthreads(); // the buffers are free
+    hand_over(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 1024, w.m0 + wm, w.n0 + wn, w.M, w.split);
 }
 
 // the sum over the splits, in order, and what happens to it
@@ -413,24 +511,36 @@ template <class TO, class T> __global__ __launch_bounds__(256) void k_slope(Slop
     store8(a.part + (uint64_t)blockIdx.y * a.cols + 8 * g, left, sums);
 }
 
-template <class T, int BM, int BN> int launch_tiles(hipStream_t st, const ProductArgs &p)
+constexpr int kTile = 128;
+
+template <int BM, int BN> dim3 tile_grid(const ProductArgs &p)
 {
     const uint64_t tiles = (uint64_t)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN) * p.splits;
-    const dim3 grid((unsigned)((tiles + 7) / 8 * 8));
-    if constexpr (sizeof(T) == 1) {
-        return launch(st, k_product<T, BM, BN, false, false>, grid, 256, p);
-    } else {
-        if (p.a.turned) return launch(st, k_product<T, BM, BN, true, true>, grid, 256, p);
-        if (p.b.turned) return launch(st, k_product<T, BM, BN, false, true>, grid, 256, p);
-        return launch(st, k_product<T, BM, BN, false, false>, grid, 256, p);
-    }
+    return dim3((unsigned)((tiles + 7) / 8 * 8));
 }
 
-constexpr int kTile = 128;
+// whether an operand's rows are whole chunks on 16-byte boundaries, and those of a tile near enough to each other
+template <class T> bool in_chunks(const Operand &o, uint32_t K, int rows)
+{
+    const uint64_t ld = (uint64_t)o.ld * sizeof(T);
+    return !o.turned && reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && ld % 16 == 0 && K * sizeof(T) % 16 == 0 && ld * rows + K * sizeof(T) < kReach;
+}
 
 template <class T> int launch_product(hipStream_t st, const ProductArgs &p)
 {
-    ZG_TRY((launch_tiles<T, kTile, kTile>(st, p)));
+    constexpr int BM = 256, BN = 128;
+    if constexpr (std::is_same_v<T, Widened8>) {
+        ZG_TRY(launch(st, k_product<T, kTile, kTile, false, false>, tile_grid<kTile, kTile>(p), 256, p));
+    } else {
+        if (in_chunks<T>(p.a, p.K, BM) && in_chunks<T>(p.b, p.K, BN)) {
+            ZG_TRY(launch(st, k_chunks<T, BM, BN>, tile_grid<BM, BN>(p), 256, p));
+        } else if constexpr (std::is_same_v<T, uint8_t>) {
+            return launch_product<Widened8>(st, p);
+        } else {
+            const auto kernel = p.a.turned ? k_product<T, kTile, kTile, true, true> : p.b.turned ? k_product<T, kTile, kTile, false, true> : k_product<T, kTile, kTile, false, false>;
+            ZG_TRY(launch(st, kernel, tile_grid<kTile, kTile>(p), 256, p));
+        }
+    }
     if (p.splits == 1) return ZG_OK;
     const uint64_t groups = (uint64_t)p.M * ((p.N + 7) / 8);
     return launch(st, k_join, dim3((unsigned)std::min<uint64_t>(4096, (groups + 255) / 256)), 256, p);
