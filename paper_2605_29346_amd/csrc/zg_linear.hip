@@ -10,7 +10,7 @@ int launch_column_sums(hipStream_t st, const float *part, uint32_t n, uint32_t c
 
 namespace {
 
-// What happens to a product's sums: v = scale_m scale_n sum, z = v + bias, y = R + drop(act(z)).
+// What happens to a product's sums: v = factor scale_m scale_n sum, z = v + bias, y = R + drop(act(z)).
 struct Epilogue {
     float factor;
     const float *scale_m, *scale_n, *bias;
@@ -20,39 +20,100 @@ struct Epilogue {
     int64_t ld_R;
     void *Y, *Z;
     int64_t ld_Y, ld_Z;
+    int64_t part; // elements between the parts of a sum that is made in parts (all else is left out then)
 };
 
-// cells n .. n + 7 (a multiple of 8; `left` of them are there) of row m
-__device__ __forceinline__ void finish8(const Epilogue &e, uint32_t m, uint32_t n, int left, float (&v)[8])
+struct AnyType {}; // the type of R, Y and Z is looked up in the epilogue
+
+template <class O> struct Eight {
+    O t[8];
+};
+template <> struct Eight<AnyType> {
+    float t[8];
+};
+
+template <class O> __device__ __forceinline__ Eight<O> get8(const void *p, int32_t type, int64_t at, int n)
 {
-    const float f = e.scale_m ? e.factor * e.scale_m[m] : e.factor;
+    Eight<O> r;
+    if constexpr (std::is_same_v<O, AnyType>) {
+        load8(p, type, at, n, r.t);
+    } else {
+        const O *from = static_cast<const O *>(p) + at;
+        if (n >= 8) {
+            __builtin_memcpy(r.t, from, sizeof r.t);
+        } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= f;
-    if (e.scale_n) {
-        float s[8];
-        load8(e.scale_n + n, left, s);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= s[j];
+            for (int j = 0; j < 8; ++j) r.t[j] = j < n ? from[j] : (O)0.0f;
+        }
     }
-    if (e.bias) {
-        float b[8];
-        load8(e.bias + n, left, b);
+    return r;
+}
+
+template <class O> __device__ __forceinline__ void put8(void *p, int32_t type, int64_t at, int n, const float (&v)[8])
+{
+    if constexpr (std::is_same_v<O, AnyType>) store8(p, type, at, n, v);
+    else store8(static_cast<O *>(p) + at, n, v);
+}
+
+// what the epilogue has of eight columns, whatever the row
+struct Columns {
+    uint32_t n;
+    int left; // of the eight
+    float scale[8], bias[8];
+};
+
+__device__ __forceinline__ Columns columns_of(const Epilogue &e, uint32_t n, uint32_t N)
+{
+    Columns c;
+    c.n = n;
+    c.left = (int)(N - n);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += b[j];
+    for (int j = 0; j < 8; ++j) c.scale[j] = 1.0f, c.bias[j] = 0.0f;
+    if (n < N) {
+        if (e.scale_n) load8(e.scale_n + n, c.left, c.scale);
+        if (e.bias) load8(e.bias + n, c.left, c.bias);
     }
-    if (e.Z) store8(e.Z, e.type, m * e.ld_Z + n, left, v);
-    if (e.act != ZG_ACT_NONE) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = act_of(e.act, v[j]);
-    }
-    if (e.drop.cut) mask8(e.drop, mask_id(e.drop, m), n >> 3, e.drop.scale, v);
-    if (e.R) {
-        float r[8];
-        load8(e.R, e.type, m * e.ld_R + n, left, r);
+    for (int j = 0; j < 8; ++j) c.scale[j] *= e.factor;
+    return c;
+}
+
+// Eight columns of ROWS rows, `step` apart: what the rows need from memory is asked for first, for all of them.
+template <class O, int ROWS, class F> __device__ __forceinline__ void finish(const Epilogue &e, const Columns &c, uint32_t m0, uint32_t step, uint32_t M, F &&sums)
+{
+    Eight<O> r[ROWS];
+    uint32_t id[ROWS];
+    float scale[ROWS];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += r[j];
+    for (int u = 0; u < ROWS; ++u) {
+        const uint32_t m = m0 + u * step;
+        id[u] = m;
+        scale[u] = 1.0f;
+        if (m >= M) continue;
+        if (e.R) r[u] = get8<O>(e.R, e.type, m * e.ld_R + c.n, c.left);
+        if (e.drop.ids) id[u] = (uint32_t)e.drop.ids[m];
+        if (e.scale_m) scale[u] = e.scale_m[m];
     }
-    store8(e.Y, e.type, m * e.ld_Y + n, left, v);
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+        const uint32_t m = m0 + u * step;
+        if (m >= M) continue;
+        float v[8];
+        sums(u, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = fmaf(v[j], scale[u] * c.scale[j], c.bias[j]);
+        if (e.Z) put8<O>(e.Z, e.type, m * e.ld_Z + c.n, c.left, v);
+        if (e.act != ZG_ACT_NONE) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = act_of(e.act, v[j]);
+        }
+        if (e.drop.cut) mask8(e.drop, id[u], c.n >> 3, e.drop.scale, v);
+        if (e.R) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += (float)r[u].t[j];
+        }
+        put8<O>(e.Y, e.type, m * e.ld_Y + c.n, c.left, v);
+    }
 }
 
 // C[m, n] = sum over k of a(m, k) b(n, k); element (i, k) of an operand is p[i * ld + k], or p[k * ld + i] where it is turned.
@@ -67,8 +128,7 @@ struct ProductArgs {
     uint32_t M, N, K;
     Rows rows;
     int32_t rows_are_k; // the device's count bounds K, else M
-    uint32_t splits;    // > 1: parts of the sum to part[split][M][N] in place of the epilogue
-    float *part;
+    uint32_t splits;    // parts that the sum is made in
     Epilogue e;
 };
 
@@ -248,9 +308,12 @@ template <class T, int tile, bool TURNED> struct Side {
 // What a wavefront does with its 32 FM x 64 cells' sums.  Of 32 x 32 cells a lane has row lane % 32, columns 8 q + 4 half + 0..3 in registers
 // 4 q + 0..3: they go through LDS (`mine`: 16 KB of the wavefront's own, free from here on), 64 rows at a time, so that eight lanes have 64 columns of a row
 // and memory sees whole lines.  Places are 16 bytes, 16 to a row, turned by the row so that neither way meets in a bank.
-template <int FM> __device__ __forceinline__ void hand_over(const ProductArgs &p, f32x16 (&acc)[FM][2], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t split)
+template <class O, int FM> __device__ __forceinline__ void hand_over(const ProductArgs &p, f32x16 (&acc)[FM][2], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t split)
 {
-    const uint32_t lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31;
+    const uint32_t lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31, g = lane & 7;
+    const Columns c = columns_of(p.e, n_wave + 8 * g, p.N);
+    Epilogue e = p.e;
+    if (split) e.Y = static_cast<float *>(e.Y) + split * e.part;
 #pragma unroll
     for (int h = 0; h < FM; h += 2) {
 #pragma unroll
@@ -262,19 +325,15 @@ template <int FM> __device__ __forceinline__ void hand_over(const ProductArgs &p
                     const uint32_t at = (32 * i + row) * 16 + ((8 * j + 2 * q + half) ^ (row & 15));
                     mine[at] = f32x4{acc[h + i][j][4 * q], acc[h + i][j][4 * q + 1], acc[h + i][j][4 * q + 2], acc[h + i][j][4 * q + 3]};
                 }
-        const uint32_t n = n_wave + 8 * (lane & 7);
-        const int left = (int)(p.N - n);
-        if (n < p.N) { // (a wavefront's LDS accesses are in order)
+        if (c.left <= 0) continue; // (a wavefront's LDS accesses are in order)
 #pragma unroll 1
-            for (uint32_t r = lane >> 3; r < 64; r += 8) {
-                const uint32_t m = m_wave + 32 * h + r;
-                if (m >= M) break;
-                const f32x4 lo = mine[r * 16 + ((2 * (lane & 7)) ^ (r & 15))], hi = mine[r * 16 + ((2 * (lane & 7) + 1) ^ (r & 15))];
-                float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                if (p.splits > 1) store8(p.part + ((uint64_t)split * p.M + m) * p.N + n, left, v);
-                else finish8(p.e, m, n, left, v);
-            }
-        }
+        for (uint32_t r0 = lane >> 3; r0 < 64; r0 += 32)
+            finish<O, 4>(e, c, m_wave + 32 * h + r0, 8, M, [&](int u, float (&v)[8]) {
+                const uint32_t r = r0 + 8 * u;
+                const f32x4 lo = mine[r * 16 + ((2 * g) ^ (r & 15))], hi = mine[r * 16 + ((2 * g + 1) ^ (r & 15))];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = lo[j], v[4 + j] = hi[j];
+            });
     }
 }
 
@@ -352,53 +411,129 @@ template <class T, int BM, int BN, bool A_TURNED, bool B_TURNED> __global__ __la
         }
         __syncthreads();
     }
-    hand_over(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 1024, w.m0 + wm, w.n0 + wn, w.M, w.split);
+    hand_over<AnyType>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 1024, w.m0 + wm, w.n0 + wn, w.M, w.split);
 }
 
 // ---- operands in whole chunks ---------------------------------------------------------------------------------------------------
 // Where both operands' rows start on 16-byte boundaries and are whole chunks long, chunks go from memory to LDS without passing through
-// registers, two steps ahead of the one that is multiplied: three buffers of four chunks (64 bytes) of k for every row of the tile.  A
-// wavefront has 128 x 64 cells of a workgroup's 256 x 128.
+// registers, two steps ahead of the one that is multiplied: three buffers, a step being four chunks (64 bytes) of k for every row of the
+// tile.  A wavefront has 128 x 64 cells of a workgroup's 256 x 128.
 
-__device__ __forceinline__ uint32_t slot4(uint32_t i, uint32_t c) { return (i >> 1) * 8 + (i & 1) * 4 + (c ^ ((i >> 1) & 3)); }
-
-constexpr uint32_t kReach = 0x80000000u; // bytes that a tile's rows may span: offsets from here on read zeros
+constexpr uint32_t kReach = 0x80000000u; // bytes that what a tile reads in a step may span: offsets from here on read zeros
 
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 template <int n> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory"); }
 
-template <class T, int BM, int BN> __global__ __launch_bounds__(256, 2) void k_chunks(ProductArgs p)
+// One operand's buffer in LDS, 4 `tile` places of 16 bytes, and its way there: 64 places side by side are filled by one instruction of a
+// wavefront, each lane's from where it says.
+template <class T, int tile, bool TURNED> struct Feed;
+
+// Along k in memory: place (row i, chunk c) is 8 (i / 2) + 4 (i % 2) + (c ^ (i / 2) % 4), so that eight rows at one c lie in eight groups of banks.
+template <class T, int tile> struct Feed<T, tile, false> {
+    static constexpr int K = 16 / (int)sizeof(T), loads = tile * 4 / 256;
+    const char *p;
+    uint32_t from[loads], chunk;
+
+    __device__ __forceinline__ void start(const Operand &o, uint32_t first, uint32_t rows, uint32_t wave, uint32_t lane)
+    {
+        const uint64_t ld = (uint64_t)o.ld * sizeof(T);
+        p = static_cast<const char *>(o.p) + first * ld;
+#pragma unroll
+        for (int l = 0; l < loads; ++l) {
+            const uint32_t s = (wave * loads + l) * 64 + lane, i = s / 4;
+            chunk = (s & 3) ^ ((s / 8) & 3); // (the same for every l: 64 places are 8 pairs of rows)
+            from[l] = first + i < rows ? (uint32_t)(i * ld) + chunk * 16 : kReach;
+        }
+    }
+    // k0 .. k0 + 4 K - 1, zeros from k_end on
+    __device__ __forceinline__ void fetch(uint32_t k0, uint32_t k_end, u32x4 *buffer, uint32_t wave) const
+    {
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p) + (uint64_t)k0 * sizeof(T), 0, kReach, 0x00027000);
+        const uint32_t beyond = k0 + (chunk + 1) * K <= k_end ? 0u : kReach;
+#pragma unroll
+        for (int l = 0; l < loads; ++l)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u32x4 *)(buffer + (wave * loads + l) * 64), 16, (int)(from[l] | beyond), 0, 0, 0);
+    }
+    // chunk c of row i
+    __device__ __forceinline__ static u32x4 chunk_of(const u32x4 *buffer, uint32_t i, uint32_t c)
+    {
+        return buffer[(i >> 1) * 8 + (i & 1) * 4 + (c ^ ((i >> 1) & 3))];
+    }
+};
+
+// Along the rows in memory: the buffer holds a row of the tile's `tile` rows for each k, and a lane's chunk is put together as it is read.
+template <class T, int tile> struct Feed<T, tile, true> {
+    static constexpr int K = 16 / (int)sizeof(T), loads = tile * 4 / 256, row = tile / K; // places of one k
+    const char *p;
+    uint64_t ld;
+    uint32_t from[loads], k_of[loads];
+
+    // 16-bit rows of four k that are read together start 64 bytes apart in the banks
+    __device__ __forceinline__ static uint32_t turn(uint32_t k) { return sizeof(T) == 2 ? (k & 3) << 2 : 0; }
+
+    __device__ __forceinline__ void start(const Operand &o, uint32_t first, uint32_t rows, uint32_t wave, uint32_t lane)
+    {
+        ld = (uint64_t)o.ld * sizeof(T);
+        p = static_cast<const char *>(o.p) + (uint64_t)first * sizeof(T);
+#pragma unroll
+        for (int l = 0; l < loads; ++l) {
+            const uint32_t s = (wave * loads + l) * 64 + lane, i = ((s % row) ^ turn(s / row)) * K;
+            k_of[l] = s / row;
+            from[l] = first + i < rows ? (uint32_t)(k_of[l] * ld) + i * (uint32_t)sizeof(T) : kReach;
+        }
+    }
+    __device__ __forceinline__ void fetch(uint32_t k0, uint32_t k_end, u32x4 *buffer, uint32_t wave) const
+    {
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p) + k0 * ld, 0, kReach, 0x00027000);
+#pragma unroll
+        for (int l = 0; l < loads; ++l)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u32x4 *)(buffer + (wave * loads + l) * 64), 16, (int)(from[l] | (k0 + k_of[l] < k_end ? 0u : kReach)), 0, 0, 0);
+    }
+    // 16-bit: a group of 16 lanes reads four k of 16 rows, four rows to a lane, and each gets its row's four k (lane 4 k + r / 4 has
+    // rows r .. r + 3 of the k-th); i = the lane's row.  fp32: four reads.
+    __device__ __forceinline__ static u32x4 chunk_of(const u32x4 *buffer, uint32_t i, uint32_t c)
+    {
+        if constexpr (sizeof(T) == 2) {
+            const uint32_t lane = threadIdx.x & 15, r = (i & ~15u) + 4 * (lane & 3);
+            u32x4 v;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t k = 8 * c + 4 * h + (lane >> 2);
+                const auto *at = reinterpret_cast<const uint16_t *>(buffer + k * row + ((r / 8) ^ turn(k))) + (r & 4);
+                const s16x4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
+                const uint64_t two = __builtin_bit_cast(uint64_t, t);
+                v[2 * h] = (uint32_t)two, v[2 * h + 1] = (uint32_t)(two >> 32);
+            }
+            return v;
+        } else {
+            u32x4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = reinterpret_cast<const uint32_t *>(buffer)[(4 * c + j) * tile + i];
+            return v;
+        }
+    }
+};
+
+template <class T, class O, int BM, int BN, bool A_TURNED, bool B_TURNED> __global__ __launch_bounds__(256, 2) void k_chunks(ProductArgs p)
 {
-    constexpr int K = 16 / (int)sizeof(T), depth = 4 * K, FM = BM / 64, FN = BN / 64, stages = 3;
-    constexpr int loads_a = BM * 4 / 256, loads_b = BN * 4 / 256, loads = loads_a + loads_b; // of a lane for a step
+    using A = Feed<T, BM, A_TURNED>;
+    using B = Feed<T, BN, B_TURNED>;
+    constexpr int depth = 4 * A::K, FM = BM / 64, FN = BN / 64, stages = 3;
     __shared__ u32x4 lds[stages][(BM + BN) * 4];
     Place w;
     if (!place_of<BM, BN>(p, depth, w)) return;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const uint32_t wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2), am = wm + (lane & 31), bn = wn + (lane & 31);
-    const T *const a0 = static_cast<const T *>(p.a.p) + (int64_t)w.m0 * p.a.ld, *const b0 = static_cast<const T *>(p.b.p) + (int64_t)w.n0 * p.b.ld;
-    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(a0), 0, kReach, 0x00027000);
-    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(b0), 0, kReach, 0x00027000);
-    // where this lane's chunks are: 64 consecutive places of LDS are filled by one instruction of a wavefront
-    uint32_t from[loads], chunk = 0;
-#pragma unroll
-    for (int l = 0; l < loads; ++l) {
-        const bool is_a = l < loads_a;
-        const uint32_t s = (wave * (is_a ? loads_a : loads_b) + (is_a ? l : l - loads_a)) * 64 + lane, pair = s / 8, i = 2 * pair + ((s >> 2) & 1);
-        chunk = (s & 3) ^ (pair & 3); // (the same for every l: 64 places are 8 pairs)
-        const uint32_t rows = is_a ? w.M - w.m0 : p.N - w.n0;
-        from[l] = i < rows ? i * (uint32_t)((is_a ? p.a.ld : p.b.ld) * sizeof(T)) + chunk * 16 : kReach;
-    }
+    A a;
+    B b;
+    a.start(p.a, w.m0, w.M, wave, lane);
+    b.start(p.b, w.n0, p.N, wave, lane);
     const auto fetch = [&](uint32_t k0, int stage) {
-        const uint32_t beyond = k0 + (chunk + 1) * K <= w.k_end ? 0 : kReach;
-        const int at = (int)(k0 * sizeof(T));
-#pragma unroll
-        for (int l = 0; l < loads; ++l) {
-            const bool is_a = l < loads_a;
-            u32x4 *to = &lds[stage][is_a ? (wave * loads_a + l) * 64 : BM * 4 + (wave * loads_b + l - loads_a) * 64];
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? ra : rb, (lds_u32x4 *)to, 16, (int)(from[l] | beyond), at, 0, 0);
-        }
+        a.fetch(k0, w.k_end, lds[stage], wave);
+        b.fetch(k0, w.k_end, lds[stage] + BM * 4, wave);
     };
     f32x16 acc[FM][FN] = {};
     const uint32_t steps = (w.k_end - w.k_first + depth - 1) / depth;
@@ -406,7 +541,7 @@ template <class T, int BM, int BN> __global__ __launch_bounds__(256, 2) void k_c
     if (steps > 1) fetch(w.k_first + depth, 1);
     int now = 0, next = 2;
     for (uint32_t t = 0; t < steps; ++t) {
-        if (t + 1 < steps) wait_loads<loads>();
+        if (t + 1 < steps) wait_loads<A::loads + B::loads>();
         else wait_loads<0>();
         __builtin_amdgcn_s_barrier(); // every wavefront's chunks of this step are there, and the step before is multiplied
         asm volatile("" ::: "memory");
@@ -417,9 +552,9 @@ template <class T, int BM, int BN> __global__ __launch_bounds__(256, 2) void k_c
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                for (int i = 0; i < FM; ++i) fa[i][h] = la[slot4(am + 32 * i, 2 * half + h)];
+                for (int i = 0; i < FM; ++i) fa[i][h] = A::chunk_of(la, am + 32 * i, 2 * half + h);
 #pragma unroll
-                for (int j = 0; j < FN; ++j) fb[j][h] = lb[slot4(bn + 32 * j, 2 * half + h)];
+                for (int j = 0; j < FN; ++j) fb[j][h] = B::chunk_of(lb, bn + 32 * j, 2 * half + h);
             }
 #pragma unroll
             for (int i = 0; i < FM; ++i)
@@ -430,9 +565,9 @@ template <class T, int BM, int BN> __global__ __launch_bounds__(256, 2) void k_c
             for (int s = 0; s < 2; ++s) {
                 u32x4 fa[FM], fb[FN];
 #pragma unroll
-                for (int i = 0; i < FM; ++i) fa[i] = la[slot4(am + 32 * i, 2 * s + half)];
+                for (int i = 0; i < FM; ++i) fa[i] = A::chunk_of(la, am + 32 * i, 2 * s + half);
 #pragma unroll
-                for (int j = 0; j < FN; ++j) fb[j] = lb[slot4(bn + 32 * j, 2 * s + half)];
+                for (int j = 0; j < FN; ++j) fb[j] = B::chunk_of(lb, bn + 32 * j, 2 * s + half);
 #pragma unroll
                 for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -443,26 +578,42 @@ template <class T, int BM, int BN> __global__ __launch_bounds__(256, 2) void k_c
         next = next == stages - 1 ? 0 : next + 1;
     }
     __syncthreads(); // the buffers are free
-    hand_over(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 1024, w.m0 + wm, w.n0 + wn, w.M, w.split);
+    hand_over<O>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 1024, w.m0 + wm, w.n0 + wn, w.M, w.split);
 }
 
-// the sum over the splits, in order, and what happens to it
-__global__ __launch_bounds__(256) void k_join(ProductArgs p)
+// The sum over the parts, and what happens to it: eight groups of eight cells to a workgroup, every 32nd part to a lane, then the lanes in order.
+struct JoinArgs {
+    const float *part;
+    uint32_t M, N, splits;
+    Epilogue e;
+};
+
+__global__ __launch_bounds__(256) void k_join(JoinArgs p)
 {
-    const uint32_t groups = (p.N + 7) / 8;
-    const uint64_t all = (uint64_t)p.M * groups, cells = (uint64_t)p.M * p.N;
-    for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < all; i += gridDim.x * 256ull) {
-        const uint32_t m = (uint32_t)(i / groups), n = (uint32_t)(i % groups) * 8;
-        const int left = (int)(p.N - n);
-        float v[8] = {};
-        for (uint32_t s = 0; s < p.splits; ++s) {
+    __shared__ float lds[32][8][8 + 1];
+    const uint32_t groups = (p.N + 7) / 8, g = threadIdx.x & 7, lane = threadIdx.x >> 3;
+    const uint64_t i = blockIdx.x * 8ull + g, cells = (uint64_t)p.M * p.N;
+    const bool there = i < (uint64_t)p.M * groups;
+    const uint32_t m = there ? (uint32_t)(i / groups) : 0u, n = there ? (uint32_t)(i % groups) * 8 : 0u;
+    float v[8] = {};
+    if (there)
+        for (uint32_t s = lane; s < p.splits; s += 32) {
             float w[8];
-            load8(p.part + s * cells + (uint64_t)m * p.N + n, left, w);
+            load8(p.part + s * cells + (uint64_t)m * p.N + n, (int)(p.N - n), w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += w[j];
         }
-        finish8(p.e, m, n, left, v);
-    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) lds[lane][g][j] = v[j];
+    __syncthreads();
+    if (lane || !there) return;
+    finish<AnyType, 1>(p.e, columns_of(p.e, n, p.N), m, 1, p.M, [&](int, float(&sum)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+        for (uint32_t s = 0; s < min(p.splits, 32u); ++s)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += lds[s][g][j];
+    });
 }
 
 // dZ without dropout's factor (dropped cells 0), and the sums of dZ over a workgroup's rows.  A lane has eight columns.
@@ -511,7 +662,7 @@ template <class TO, class T> __global__ __launch_bounds__(256) void k_slope(Slop
     store8(a.part + (uint64_t)blockIdx.y * a.cols + 8 * g, left, sums);
 }
 
-constexpr int kTile = 128;
+constexpr int kTile = 128, kTileM = 256, kTileN = 128; // of operands that lie anyhow, and of those in chunks
 
 template <int BM, int BN> dim3 tile_grid(const ProductArgs &p)
 {
@@ -519,41 +670,67 @@ template <int BM, int BN> dim3 tile_grid(const ProductArgs &p)
     return dim3((unsigned)((tiles + 7) / 8 * 8));
 }
 
-// whether an operand's rows are whole chunks on 16-byte boundaries, and those of a tile near enough to each other
-template <class T> bool in_chunks(const Operand &o, uint32_t K, int rows)
+// Whether an operand's rows (a tile has `tile` of them) start on 16-byte boundaries, are whole chunks long, and near enough to each other.
+template <class T> bool in_chunks(const Operand &o, uint32_t rows, uint32_t K, int tile)
 {
-    const uint64_t ld = (uint64_t)o.ld * sizeof(T);
-    return !o.turned && reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && ld % 16 == 0 && K * sizeof(T) % 16 == 0 && ld * rows + K * sizeof(T) < kReach;
+    const uint64_t ld = (uint64_t)o.ld * sizeof(T), along = (uint64_t)(o.turned ? rows : K) * sizeof(T);
+    const uint64_t span = o.turned ? ld * (64 / sizeof(T)) + tile * sizeof(T) : ld * tile + 64;
+    return reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && ld % 16 == 0 && along % 16 == 0 && span < kReach;
 }
 
-template <class T> int launch_product(hipStream_t st, const ProductArgs &p)
+template <class T, class O, bool A_TURNED, bool B_TURNED> int launch_chunks(hipStream_t st, const ProductArgs &p)
 {
-    constexpr int BM = 256, BN = 128;
-    if constexpr (std::is_same_v<T, Widened8>) {
-        ZG_TRY(launch(st, k_product<T, kTile, kTile, false, false>, tile_grid<kTile, kTile>(p), 256, p));
-    } else {
-        if (in_chunks<T>(p.a, p.K, BM) && in_chunks<T>(p.b, p.K, BN)) {
-            ZG_TRY(launch(st, k_chunks<T, BM, BN>, tile_grid<BM, BN>(p), 256, p));
-        } else if constexpr (std::is_same_v<T, uint8_t>) {
-            return launch_product<Widened8>(st, p);
-        } else {
-            const auto kernel = p.a.turned ? k_product<T, kTile, kTile, true, true> : p.b.turned ? k_product<T, kTile, kTile, false, true> : k_product<T, kTile, kTile, false, false>;
-            ZG_TRY(launch(st, kernel, tile_grid<kTile, kTile>(p), 256, p));
+    return launch(st, k_chunks<T, O, kTileM, kTileN, A_TURNED, B_TURNED>, tile_grid<kTileM, kTileN>(p), 256, p);
+}
+
+// the tiles of one product, or of the parts of one, whose results are of type p.e.type
+template <class T> int launch_tiles(hipStream_t st, const ProductArgs &p)
+{
+    if constexpr (!std::is_same_v<T, Widened8>) {
+        if (in_chunks<T>(p.a, p.M, p.K, kTileM) && in_chunks<T>(p.b, p.N, p.K, kTileN)) {
+            if constexpr (!std::is_same_v<T, uint8_t>) {
+                if (p.a.turned) return p.e.type == ZG_F32 ? launch_chunks<T, float, true, true>(st, p) : launch_chunks<T, T, true, true>(st, p);
+                if (p.b.turned) return launch_chunks<T, T, false, true>(st, p);
+            }
+            if (p.e.type == ZG_F32) return launch_chunks<T, float, false, false>(st, p);
+            if (p.e.type == ZG_F16) return launch_chunks<T, _Float16, false, false>(st, p);
+            return launch_chunks<T, __bf16, false, false>(st, p);
         }
     }
-    if (p.splits == 1) return ZG_OK;
-    const uint64_t groups = (uint64_t)p.M * ((p.N + 7) / 8);
-    return launch(st, k_join, dim3((unsigned)std::min<uint64_t>(4096, (groups + 255) / 256)), 256, p);
+    if constexpr (std::is_same_v<T, uint8_t>) {
+        return launch_tiles<Widened8>(st, p);
+    } else {
+        const dim3 grid = tile_grid<kTile, kTile>(p);
+        if constexpr (!std::is_same_v<T, Widened8>) {
+            if (p.a.turned) return launch(st, k_product<T, kTile, kTile, true, true>, grid, 256, p);
+            if (p.b.turned) return launch(st, k_product<T, kTile, kTile, false, true>, grid, 256, p);
+        }
+        return launch(st, k_product<T, kTile, kTile, false, false>, grid, 256, p);
+    }
 }
 
-int launch_product(hipStream_t st, int32_t type, const ProductArgs &p)
+// `part`: room for splits x M x N sums where there are parts
+template <class T> int launch_product(hipStream_t st, const ProductArgs &p, float *part)
 {
-    if (type == ZG_F32) return launch_product<float>(st, p);
-    if (type == ZG_F16) return launch_product<_Float16>(st, p);
-    if (type == ZG_BF16) return launch_product<__bf16>(st, p);
+    if (p.splits == 1) return launch_tiles<T>(st, p);
+    ProductArgs q = p;
+    q.e = Epilogue{};
+    q.e.factor = 1.0f;
+    q.e.type = ZG_F32;
+    q.e.Y = part, q.e.ld_Y = p.N, q.e.part = (int64_t)p.M * p.N;
+    ZG_TRY(launch_tiles<T>(st, q));
+    const uint64_t groups = (uint64_t)p.M * ((p.N + 7) / 8);
+    return launch(st, k_join, dim3((unsigned)((groups + 7) / 8)), 256, JoinArgs{part, p.M, p.N, p.splits, p.e});
+}
+
+int launch_product(hipStream_t st, int32_t type, const ProductArgs &p, float *part = nullptr)
+{
+    if (type == ZG_F32) return launch_product<float>(st, p, part);
+    if (type == ZG_F16) return launch_product<_Float16>(st, p, part);
+    if (type == ZG_BF16) return launch_product<__bf16>(st, p, part);
     // What the 8-bit instructions lose per group of eight adds up like the root of their number; what an fp32 sum may lose, like the number
     // of its terms.  From a sum of a few hundred terms on the former is the smaller.
-    return p.K >= 512 ? launch_product<uint8_t>(st, p) : launch_product<Widened8>(st, p);
+    return p.K >= 512 ? launch_product<uint8_t>(st, p, part) : launch_product<Widened8>(st, p, part);
 }
 
 // How the gradients' workspace is laid out.
@@ -580,7 +757,7 @@ GradPlan grad_plan(const zg_linear_grad_args &a)
     while (g.lanes < groups && g.lanes < 64) g.lanes *= 2;
     g.slope_x = (groups + g.lanes - 1) / g.lanes;
     g.slope_y = (uint32_t)std::min<int64_t>(std::max(1u, 1024u / g.slope_x), (a.rows + 256 / g.lanes - 1) / (256 / g.lanes));
-    const int64_t tiles = (int64_t)((a.out + kTile - 1) / kTile) * ((a.in + kTile - 1) / kTile);
+    const int64_t tiles = (int64_t)((a.out + kTileM - 1) / kTileM) * ((a.in + kTileN - 1) / kTileN);
     g.splits = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, (a.rows + 255) / 256));
     if (g.slopes && (a.d_dA || a.d_dW)) g.off_dz = take((size_t)a.rows * g.ld_dz * type_size(a.dtype));
     if (a.d_dbias) g.off_part = take((size_t)g.slope_y * a.out * sizeof(float));
@@ -717,9 +894,8 @@ int zg_linear_backward(const zg_linear_grad_args *a, void *d_workspace, size_t w
             p.M = (uint32_t)a->out, p.N = (uint32_t)a->in, p.K = (uint32_t)a->rows;
             p.rows_are_k = 1;
             p.splits = g.splits;
-            p.part = reinterpret_cast<float *>(ws + g.off_dw);
             p.e.Y = a->d_dW, p.e.ld_Y = a->ld_dW;
-            ZG_TRY(launch_product(st, a->dtype, p));
+            ZG_TRY(launch_product(st, a->dtype, p, reinterpret_cast<float *>(ws + g.off_dw)));
         }
         return ZG_OK;
     });
