@@ -581,6 +581,65 @@ template <class T, class O, int BM, int BN, bool A_TURNED, bool B_TURNED> __glob
     hand_over<O>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 1024, w.m0 + wm, w.n0 + wn, w.M, w.split);
 }
 
+// ---- few tiles ------------------------------------------------------------------------------------------------------------------
+// Where tiles of the sizes above would leave most of the chip idle, or be mostly empty: a workgroup has 32 x 32 cells, its four wavefronts
+// every fourth pair of chunks of k each, straight from memory into registers; their sums meet in LDS.  Nothing is shared but what the caches
+// hold, and a call lasts little more than one way to memory and back.  Operands lie along k, anyhow.
+template <class T> struct Along {
+    static constexpr int K = chunk_k<T>;
+    const T *row;
+    uint32_t k_end;
+    __device__ __forceinline__ u32x4 at(uint32_t k) const
+    {
+        u32x4 r = {};
+        if (k + K <= k_end) __builtin_memcpy(&r, row + k, K * sizeof(T));
+        else if (k < k_end) r = part_of_chunk(row + k, (int)(k_end - k), k_end >= (uint32_t)K);
+        if constexpr (std::is_same_v<T, Widened8>) return widen(r);
+        else return r;
+    }
+};
+
+template <class T> __global__ __launch_bounds__(256) void k_few(ProductArgs p)
+{
+    constexpr int K = chunk_k<T>, ahead = 4, stride = 36; // floats to a row of LDS: rows start in different groups of banks
+    __shared__ float lds[4][32 * stride];
+    const uint32_t live = min(p.M, p.rows.live()), nt = (p.N + 31) / 32;
+    const uint32_t m0 = blockIdx.x / nt * 32, n0 = blockIdx.x % nt * 32;
+    if (m0 >= live) return;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    Along<T> a, b;
+    a.row = static_cast<const T *>(p.a.p) + min(m0 + (lane & 31), live - 1) * p.a.ld;
+    b.row = static_cast<const T *>(p.b.p) + min(n0 + (lane & 31), p.N - 1) * p.b.ld;
+    a.k_end = b.k_end = p.K;
+    const uint32_t row = threadIdx.x >> 2, group = threadIdx.x & 3; // of the lanes that hand the sums over
+    const Columns c = columns_of(p.e, n0 + 8 * group, p.N);
+    f32x16 acc = {};
+    for (uint32_t k0 = wave * 2 * K; k0 < p.K; k0 += ahead * 8 * K) {
+        u32x4 x[ahead], y[ahead];
+#pragma unroll
+        for (int i = 0; i < ahead; ++i) {
+            const uint32_t k = k0 + i * 8 * K + half * K;
+            x[i] = a.at(k);
+            y[i] = b.at(k);
+        }
+#pragma unroll
+        for (int i = 0; i < ahead; ++i) multiply(T(), y[i], x[i], acc);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4 *>(&lds[wave][(lane & 31) * stride + 8 * q + 4 * half]) = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    __syncthreads();
+    if (row >= 32 || c.left <= 0) return;
+    finish<AnyType, 1>(p.e, c, m0 + row, 1, live, [&](int, float(&v)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += lds[w][row * stride + 8 * group + j];
+    });
+}
+
 // The sum over the parts, and what happens to it: eight groups of eight cells to a workgroup, every 32nd part to a lane, then the lanes in order.
 struct JoinArgs {
     const float *part;
@@ -678,6 +737,22 @@ template <class T> bool in_chunks(const Operand &o, uint32_t rows, uint32_t K, i
     return reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && ld % 16 == 0 && along % 16 == 0 && span < kReach;
 }
 
+// Whether cells of 32 x 32 (k_few) take less time than large tiles, both as measured on an MI355X.  A large tile alone takes 9 us and 0.5 us
+// for 64 bytes of k (fp32: 2 us, its instructions' own time), 512 of them at a time; k_few 3 us, 1.65 us for a million chunks out of the
+// caches (twice that where rows start anywhere) and 1.3 us for a thousand workgroups.  bf16, large tiles / k_few: 1 x 256 x 512 8.1 / 3.0 us,
+// 256 x 2048 x 512 40 / 9.7, 4096 x 256 x 256 13.6 / 6.6, 8192 x 256 x 256 13.8 / 11.7, 16384 x 256 x 256 14.7 / 20, 131072 x 64 x 64
+// 14.5 / 22; rows of 602 bytes, 32768 x 301 x 47, 13.7 / 22.6; fp32 1024 x 1024 x 1024 135 / 41, 262144 x 128 x 32 84 / 45.
+template <class T> bool few_tiles(const ProductArgs &p, bool chunks)
+{
+    using F = std::conditional_t<std::is_same_v<T, uint8_t>, Widened8, T>;
+    if (p.splits > 1 || p.a.turned || p.b.turned) return false;
+    const double tiles = std::ceil(p.M / (double)kTileM) * std::ceil(p.N / (double)kTileN), steps = std::ceil(p.K * sizeof(T) / 64.0);
+    const double large = (9.0 + (std::is_same_v<T, float> ? 2.0 : 0.5) * steps) * std::max(1.0, tiles / 512.0);
+    const double blocks = std::ceil(p.M / 32.0) * std::ceil(p.N / 32.0), read = blocks * 64.0 * p.K / chunk_k<F>;
+    const double few = 3.0 + (chunks ? 1.65e-6 : 3.3e-6) * read + 1.3e-3 * blocks;
+    return few < large;
+}
+
 template <class T, class O, bool A_TURNED, bool B_TURNED> int launch_chunks(hipStream_t st, const ProductArgs &p)
 {
     return launch(st, k_chunks<T, O, kTileM, kTileN, A_TURNED, B_TURNED>, tile_grid<kTileM, kTileN>(p), 256, p);
@@ -686,8 +761,13 @@ template <class T, class O, bool A_TURNED, bool B_TURNED> int launch_chunks(hipS
 // the tiles of one product, or of the parts of one, whose results are of type p.e.type
 template <class T> int launch_tiles(hipStream_t st, const ProductArgs &p)
 {
+    const bool chunks = in_chunks<T>(p.a, p.M, p.K, kTileM) && in_chunks<T>(p.b, p.N, p.K, kTileN);
+    if (few_tiles<T>(p, chunks)) {
+        using F = std::conditional_t<std::is_same_v<T, uint8_t>, Widened8, T>;
+        return launch(st, k_few<F>, dim3((p.M + 31) / 32 * ((p.N + 31) / 32)), 256, p);
+    }
     if constexpr (!std::is_same_v<T, Widened8>) {
-        if (in_chunks<T>(p.a, p.M, p.K, kTileM) && in_chunks<T>(p.b, p.N, p.K, kTileN)) {
+        if (chunks) {
             if constexpr (!std::is_same_v<T, uint8_t>) {
                 if (p.a.turned) return p.e.type == ZG_F32 ? launch_chunks<T, float, true, true>(st, p) : launch_chunks<T, T, true, true>(st, p);
                 if (p.b.turned) return launch_chunks<T, T, false, true>(st, p);
@@ -782,7 +862,6 @@ int check_linear_grad(const zg_linear_grad_args *a)
 using namespace zg;
 
 extern "C" {
-
 int zg_linear(const zg_linear_args *a, void *stream)
 {
     return entry([&]() -> int {

@@ -8,6 +8,7 @@ uninitialised).  Work is enqueued on `stream` (default: torch's current one); no
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from dataclasses import dataclass
 from typing import NamedTuple, Optional
 
@@ -17,6 +18,7 @@ from . import zg
 
 _TYPES = {torch.float32: zg.F32, torch.float16: zg.F16, torch.bfloat16: zg.BF16, torch.float8_e4m3fn: zg.F8}
 _ACTS = {"none": zg.ACT_NONE, "relu": zg.ACT_RELU, "silu": zg.ACT_SILU, "gelu": zg.ACT_GELU}
+_F32, _I32 = torch.float32, torch.int32
 
 
 @dataclass
@@ -36,6 +38,30 @@ class NormResult(NamedTuple):
     scale: Optional[torch.Tensor]  # of an 8-bit y
 
 
+# The structs of include/zg.h as one pack() each (zg.LinearArgs and so on are the same by field): a call of a few rows takes the GPU less
+# than filling a ctypes structure field by field takes the host.
+_DROP = "dQIIq"
+_PACK = {"zg_linear": "@qq6i13q" + _DROP, "zg_linear_backward": "@qq6i13q" + _DROP, "zg_dropout": "@qq2i6q" + _DROP,
+         "zg_rms_norm": "@qq3if11q" + _DROP, "zg_rms_norm_backward": "@qq2i13q" + _DROP}
+_pack = {name: struct.Struct(f).pack for name, f in _PACK.items()}
+_entries: dict = {}
+
+
+def _entry(name):
+    """The library's function, taking the packed struct."""
+    f = _entries.get(name)
+    if f is None:
+        args = [C.c_char_p]
+        if name.endswith("_workspace"):
+            args.append(C.POINTER(C.c_size_t))
+        elif name.endswith("_backward"):
+            args += [C.c_void_p, C.c_size_t, C.c_void_p]
+        else:
+            args.append(C.c_void_p)
+        f = _entries[name] = C.CFUNCTYPE(C.c_int, *args)((name, zg.lib()))
+    return f
+
+
 def _type(t, what):
     try:
         return _TYPES[t]
@@ -43,76 +69,103 @@ def _type(t, what):
         raise TypeError(f"{what}: {t} is not one of {', '.join(str(k) for k in _TYPES)}") from None
 
 
-class _Call:
-    """One call: checks the tensors, fills the struct, and keeps what lives on another stream than the one it was made on."""
-
-    def __init__(self, like, rows_t, stream):
-        if not like.is_cuda:
-            raise ValueError("the operators take CUDA tensors")
-        self.device = like.device
-        self.stream = zg._stream_ptr(stream if stream is not None else torch.cuda.current_stream(self.device))
-        self.foreign = None
-        if stream is not None and self.stream != torch.cuda.current_stream(self.device).cuda_stream:
-            self.foreign = torch.cuda.ExternalStream(self.stream, device=self.device)
-        self.made = []
-        self.rows_ptr = self.vector(rows_t, "rows", 1, torch.int32)
-
-    def _device(self, t, what):
-        if t.device != self.device:
-            raise ValueError(f"{what} is on {t.device}, the others on {self.device}")
-
-    def matrix(self, t, what, rows, cols, dtype):
-        self._device(t, what)
-        if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype != dtype:
-            raise ValueError(f"{what} is {list(t.shape)} of {t.dtype}: [{rows}, {cols}] of {dtype} is wanted")
-        if t.stride(1) != 1 and cols > 1:
-            raise ValueError(f"the rows of {what} are not contiguous")
-        ld = t.stride(0) if rows > 1 else cols
-        if rows > 1 and ld < cols:
-            raise ValueError(f"the rows of {what} overlap")
-        return t.data_ptr(), ld
-
-    def vector(self, t, what, n, dtype=torch.float32):
-        if t is None:
-            return None
-        self._device(t, what)
-        if t.numel() != n or t.dtype != dtype or not t.is_contiguous():
-            raise ValueError(f"{what} is {list(t.shape)} of {t.dtype}: {n} contiguous elements of {dtype} are wanted")
-        return t.data_ptr()
-
-    def make(self, shape, dtype):
-        t = torch.empty(shape, dtype=dtype, device=self.device)
-        self.made.append(t)
-        return t
-
-    def drop(self, d, rows):
-        if d is None:
-            return zg.Drop()
-        return zg.Drop(d.p, d.key & 0xFFFFFFFFFFFFFFFF, d.layer & 0xFFFFFFFF, 0, self.vector(d.ids, "the dropout's ids", rows, torch.int32))
-
-    def run(self, name, args, workspace=False):
-        L = zg.lib()
-        with torch.cuda.device(self.device):
-            if workspace:
-                need = C.c_size_t()
-                zg._check(getattr(L, name + "_workspace")(C.byref(args), C.byref(need)))
-                ws = self.make((need.value,), torch.uint8)
-                if self.foreign is not None:  # blocks that torch hands out may still be in use by earlier work of the current stream
-                    self.foreign.wait_stream(torch.cuda.current_stream(self.device))
-                zg._check(getattr(L, name)(C.byref(args), ws.data_ptr(), need.value, self.stream))
-            else:
-                if self.foreign is not None and self.made:
-                    self.foreign.wait_stream(torch.cuda.current_stream(self.device))
-                zg._check(getattr(L, name)(C.byref(args), self.stream))
-        if self.foreign is not None:
-            for t in self.made:
-                t.record_stream(self.foreign)
-
-
 def _act(act):
-    if act not in _ACTS:
-        raise ValueError(f"act is {act!r}: one of {', '.join(_ACTS)} is wanted")
-    return _ACTS[act]
+    try:
+        return _ACTS[act]
+    except KeyError:
+        raise ValueError(f"act is {act!r}: one of {', '.join(_ACTS)} is wanted") from None
+
+
+def _matrix(t, what, rows, cols, dtype, device):
+    """(address, row stride)"""
+    if t.dtype is not dtype or t.shape != (rows, cols) or t.device != device:
+        raise ValueError(f"{what} is {list(t.shape)} of {t.dtype} on {t.device}: [{rows}, {cols}] of {dtype} on {device} is wanted")
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
+        raise ValueError(f"the rows of {what} are not contiguous")
+    if rows <= 1:
+        ld = cols
+    elif ld < cols:
+        raise ValueError(f"the rows of {what} overlap")
+    return t.data_ptr(), ld
+
+
+def _vector(t, what, n, dtype, device):
+    """address, or 0 for None"""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.numel() != n or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what} is {list(t.shape)} of {t.dtype} on {t.device}: {n} contiguous elements of {dtype} on {device} are wanted")
+    return t.data_ptr()
+
+
+def _out(t, what, m, n, dtype, device, made, like=None):
+    """(tensor, address, row stride) of an output: what the caller gave, or a new one"""
+    if t is not None:
+        return (t, *_matrix(t, what, m, n, dtype, device))
+    t = torch.empty_like(like) if like is not None and like.is_contiguous() else torch.empty((m, n), dtype=dtype, device=device)
+    made.append(t)
+    return t, t.data_ptr(), n
+
+
+def _out_vector(t, what, n, device, made):
+    """(tensor, address) of an output of float32"""
+    if t is not None:
+        return t, _vector(t, what, n, _F32, device)
+    t = torch.empty(n, dtype=_F32, device=device)
+    made.append(t)
+    return t, t.data_ptr()
+
+
+_NONE3 = None, 0, 0
+
+
+def _shape(t, what):
+    """([rows, cols], device) of the operand that a call goes by"""
+    if not t.is_cuda:
+        raise ValueError("the operators take CUDA tensors")
+    if t.dim() != 2:
+        raise ValueError(f"{what} is {list(t.shape)}: a matrix is wanted")
+    return t.shape, t.device
+
+
+def _mask(d, rows, device):
+    if d is None:
+        return 0.0, 0, 0, 0, 0
+    return d.p, d.key & 0xFFFFFFFFFFFFFFFF, d.layer & 0xFFFFFFFF, 0, _vector(d.ids, "the dropout's ids", rows, _I32, device)
+
+
+def _run(name, args, device, stream, made=(), workspace=False):
+    """Enqueues the call on `stream`.  `made`: tensors that were allocated for it - on torch's current stream, whose earlier work another
+    stream has to wait for, and whose memory must not be handed out again before that other stream is done with it."""
+    current = torch._C._cuda_getCurrentRawStream(device.index)
+    handle = current if stream is None else zg._stream_ptr(stream)
+    foreign = None
+    if handle != current:
+        foreign = torch.cuda.ExternalStream(handle, device=device)
+    args = _pack[name](*args)
+    if torch._C._cuda_getDevice() != device.index:
+        with torch.cuda.device(device):
+            return _enqueue(name, args, device, handle, foreign, made, workspace)
+    return _enqueue(name, args, device, handle, foreign, made, workspace)
+
+
+def _enqueue(name, args, device, handle, foreign, made, workspace):
+    if workspace:
+        need = C.c_size_t()
+        status = _entry(name + "_workspace")(args, C.byref(need))
+        if status:
+            raise zg.ZgError(status)
+        ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+        made = (*made, ws)
+    if foreign is not None and made:
+        foreign.wait_stream(torch.cuda.current_stream(device))
+    status = _entry(name)(args, ws.data_ptr(), need.value, handle) if workspace else _entry(name)(args, handle)
+    if foreign is not None:
+        for t in made:
+            t.record_stream(foreign)
+    if status:
+        raise zg.ZgError(status)
 
 
 def linear(a, w, *, bias=None, act="none", dropout: Optional[Dropout] = None, residual=None, scale_a=None, scale_w=None, out_dtype=None,
@@ -120,23 +173,17 @@ def linear(a, w, *, bias=None, act="none", dropout: Optional[Dropout] = None, re
     """drop(act(a w^T + bias)) + residual.  a: [rows, in], w: [out, in], bias: [out] float32, residual and result: [rows, out] of
     `out_dtype` (default: a's type; bfloat16 for 8-bit operands).  float8_e4m3fn operands may have scales by row (float32 [rows], [out]).
     `save` (or a tensor `preact`) returns (result, a w^T + bias) for `linear_backward`.  `out` may be the residual."""
-    c = _Call(a, rows, stream)
-    m, n = a.shape[0], w.shape[0]
-    kind = out_dtype or (torch.bfloat16 if a.dtype == torch.float8_e4m3fn else a.dtype)
-    out = c.make((m, n), kind) if out is None else out
-    preact = c.make((m, n), kind) if preact is None and save else preact
-    args = zg.LinearArgs(rows=m, d_rows=c.rows_ptr, in_=a.shape[1], out=n, dtype=_type(a.dtype, "a"), out_dtype=_type(kind, "out_dtype"), act=_act(act))
-    args.d_A, args.ld_A = c.matrix(a, "a", m, a.shape[1], a.dtype)
-    args.d_W, args.ld_W = c.matrix(w, "w", n, a.shape[1], a.dtype)
-    args.d_scale_A, args.d_scale_W = c.vector(scale_a, "scale_a", m), c.vector(scale_w, "scale_w", n)
-    args.d_bias = c.vector(bias, "bias", n)
-    if residual is not None:
-        args.d_R, args.ld_R = c.matrix(residual, "residual", m, n, kind)
-    args.d_Y, args.ld_Y = c.matrix(out, "out", m, n, kind)
-    if preact is not None:
-        args.d_Z, args.ld_Z = c.matrix(preact, "preact", m, n, kind)
-    args.drop = c.drop(dropout, m)
-    c.run("zg_linear", args)
+    (m, k), device = _shape(a, "a")
+    n, dtype = w.shape[0], a.dtype
+    kind = out_dtype or (torch.bfloat16 if dtype == torch.float8_e4m3fn else dtype)
+    made = []
+    out, y, ld_y = _out(out, "out", m, n, kind, device, made, a if k == n and kind is dtype else None)
+    preact, z, ld_z = _out(preact, "preact", m, n, kind, device, made) if save or preact is not None else _NONE3
+    _run("zg_linear", (m, _vector(rows, "rows", 1, _I32, device), k, n, _type(dtype, "a"), _type(kind, "out_dtype"), _act(act), 0,
+                       *_matrix(a, "a", m, k, dtype, device), _vector(scale_a, "scale_a", m, _F32, device),
+                       *_matrix(w, "w", n, k, dtype, device), _vector(scale_w, "scale_w", n, _F32, device), _vector(bias, "bias", n, _F32, device),
+                       *(_matrix(residual, "residual", m, n, kind, device) if residual is not None else (0, 0)),
+                       y, ld_y, z, ld_z, *_mask(dropout, m, device)), device, stream, made)
     return (out, preact) if preact is not None else out
 
 
@@ -144,39 +191,28 @@ def linear_backward(dy, a, w, *, preact=None, act="none", dropout: Optional[Drop
                     dw=None, dbias=None, stream=None):
     """Gradients (da, dw, dbias) of `linear` for the gradient dy of its result (that of the residual is dy itself); `need` says which
     are wanted, the others are None.  `preact` is what `linear(save=True)` returned; without an activation it is not needed."""
-    c = _Call(dy, rows, stream)
-    m, n, k = dy.shape[0], dy.shape[1], w.shape[1]
-    da = c.make((m, k), a.dtype) if da is None and need[0] else da
-    dw = c.make((n, k), a.dtype) if dw is None and need[1] else dw
-    dbias = c.make((n,), torch.float32) if dbias is None and need[2] else dbias
-    args = zg.LinearGradArgs(rows=m, d_rows=c.rows_ptr, in_=k, out=n, dtype=_type(a.dtype, "a"), out_dtype=_type(dy.dtype, "dy"), act=_act(act))
-    args.d_dY, args.ld_dY = c.matrix(dy, "dy", m, n, dy.dtype)
-    if preact is not None:
-        args.d_Z, args.ld_Z = c.matrix(preact, "preact", m, n, dy.dtype)
-    args.d_A, args.ld_A = c.matrix(a, "a", m, k, a.dtype)
-    args.d_W, args.ld_W = c.matrix(w, "w", n, k, a.dtype)
-    if da is not None:
-        args.d_dA, args.ld_dA = c.matrix(da, "da", m, k, a.dtype)
-    if dw is not None:
-        args.d_dW, args.ld_dW = c.matrix(dw, "dw", n, k, a.dtype)
-    args.d_dbias = c.vector(dbias, "dbias", n)
-    args.drop = c.drop(dropout, m)
-    c.run("zg_linear_backward", args, workspace=True)
+    (m, n), device = _shape(dy, "dy")
+    k, dtype, kind = w.shape[1], a.dtype, dy.dtype
+    made = []
+    da, da_at, ld_da = _out(da, "da", m, k, dtype, device, made) if need[0] or da is not None else _NONE3
+    dw, dw_at, ld_dw = _out(dw, "dw", n, k, dtype, device, made) if need[1] or dw is not None else _NONE3
+    dbias, db_at = _out_vector(dbias, "dbias", n, device, made) if need[2] or dbias is not None else (None, 0)
+    _run("zg_linear_backward", (m, _vector(rows, "rows", 1, _I32, device), k, n, _type(dtype, "a"), _type(kind, "dy"), _act(act), 0,
+                                *_matrix(dy, "dy", m, n, kind, device),
+                                *(_matrix(preact, "preact", m, n, kind, device) if preact is not None else (0, 0)),
+                                *_matrix(a, "a", m, k, dtype, device), *_matrix(w, "w", n, k, dtype, device),
+                                da_at, ld_da, dw_at, ld_dw, db_at, *_mask(dropout, m, device)), device, stream, made, workspace=True)
     return da, dw, dbias
 
 
 def dropout(x, mask: Optional[Dropout], *, residual=None, rows=None, out=None, stream=None):
     """drop(x) + residual; the gradient of x is the same call on the gradient of the result.  `out` may be x or the residual."""
-    c = _Call(x, rows, stream)
-    m, n = x.shape
-    out = c.make((m, n), x.dtype) if out is None else out
-    args = zg.DropoutArgs(rows=m, d_rows=c.rows_ptr, cols=n, dtype=_type(x.dtype, "x"))
-    args.d_x, args.ld_x = c.matrix(x, "x", m, n, x.dtype)
-    if residual is not None:
-        args.d_r, args.ld_r = c.matrix(residual, "residual", m, n, x.dtype)
-    args.d_y, args.ld_y = c.matrix(out, "out", m, n, x.dtype)
-    args.drop = c.drop(mask, m)
-    c.run("zg_dropout", args)
+    (m, n), device = _shape(x, "x")
+    dtype, made = x.dtype, []
+    out, y, ld_y = _out(out, "out", m, n, dtype, device, made, x)
+    _run("zg_dropout", (m, _vector(rows, "rows", 1, _I32, device), n, _type(dtype, "x"), *_matrix(x, "x", m, n, dtype, device),
+                        *(_matrix(residual, "residual", m, n, dtype, device) if residual is not None else (0, 0)),
+                        y, ld_y, *_mask(mask, m, device)), device, stream, made)
     return out
 
 
@@ -185,24 +221,20 @@ def rms_norm(x, *, gain=None, eps=1e-6, residual=None, dropout: Optional[Dropout
     """h = drop(x) + residual, rstd = 1 / sqrt(mean(h^2) + eps), y = h rstd gain (gain: float32 [cols]).  y is of `out_dtype` (default: x's
     type); with float8_e4m3fn y holds y / scale, scale float32 [rows] the row's largest |y| / 448.  h is written where a residual or
     dropout makes it differ from x (or where a tensor `h` is given; that may be the residual or x)."""
-    c = _Call(x, rows, stream)
-    m, n = x.shape
-    kind = out_dtype or x.dtype
-    y = c.make((m, n), kind) if y is None else y
-    h = c.make((m, n), x.dtype) if h is None and (residual is not None or (dropout is not None and dropout.p > 0)) else h
-    rstd = c.make((m,), torch.float32) if rstd is None else rstd
-    scale = c.make((m,), torch.float32) if scale is None and kind == torch.float8_e4m3fn else scale
-    args = zg.NormArgs(rows=m, d_rows=c.rows_ptr, cols=n, dtype=_type(x.dtype, "x"), out_dtype=_type(kind, "out_dtype"), eps=eps)
-    args.d_x, args.ld_x = c.matrix(x, "x", m, n, x.dtype)
-    if residual is not None:
-        args.d_r, args.ld_r = c.matrix(residual, "residual", m, n, x.dtype)
-    args.d_gain = c.vector(gain, "gain", n)
-    if h is not None:
-        args.d_h, args.ld_h = c.matrix(h, "h", m, n, x.dtype)
-    args.d_y, args.ld_y = c.matrix(y, "y", m, n, kind)
-    args.d_scale, args.d_rstd = c.vector(scale, "scale", m), c.vector(rstd, "rstd", m)
-    args.drop = c.drop(dropout, m)
-    c.run("zg_rms_norm", args)
+    (m, n), device = _shape(x, "x")
+    dtype = x.dtype
+    kind = out_dtype or dtype
+    made = []
+    y, y_at, ld_y = _out(y, "y", m, n, kind, device, made, x if kind is dtype else None)
+    summed = residual is not None or (dropout is not None and dropout.p > 0)
+    h, h_at, ld_h = _out(h, "h", m, n, dtype, device, made, x) if summed or h is not None else _NONE3
+    rstd, rstd_at = _out_vector(rstd, "rstd", m, device, made)
+    scale, scale_at = _out_vector(scale, "scale", m, device, made) if scale is not None or kind is torch.float8_e4m3fn else (None, 0)
+    _run("zg_rms_norm", (m, _vector(rows, "rows", 1, _I32, device), n, _type(dtype, "x"), _type(kind, "out_dtype"), eps,
+                         *_matrix(x, "x", m, n, dtype, device),
+                         *(_matrix(residual, "residual", m, n, dtype, device) if residual is not None else (0, 0)),
+                         _vector(gain, "gain", n, _F32, device), h_at, ld_h, y_at, ld_y, scale_at, rstd_at,
+                         *_mask(dropout, m, device)), device, stream, made)
     return NormResult(y, h, rstd, scale)
 
 
@@ -210,21 +242,16 @@ def rms_norm_backward(dy, h, rstd, *, gain=None, dh=None, dropout: Optional[Drop
                       dr=None, dgain=None, stream=None):
     """Gradients (dx, dr, dgain) of `rms_norm` for the gradient dy of its y and dh of its h (None: nothing reaches h from elsewhere).
     dr, the gradient of the residual, is a tensor of its own only with dropout (else dx is both, and None is returned for it)."""
-    c = _Call(dy, rows, stream)
-    m, n = dy.shape
-    dx = c.make((m, n), dy.dtype) if dx is None else dx
-    dr = c.make((m, n), dy.dtype) if dr is None and need_dr and dropout is not None and dropout.p > 0 else dr
-    dgain = c.make((n,), torch.float32) if dgain is None and need_dgain else dgain
-    args = zg.NormGradArgs(rows=m, d_rows=c.rows_ptr, cols=n, dtype=_type(dy.dtype, "dy"))
-    args.d_dy, args.ld_dy = c.matrix(dy, "dy", m, n, dy.dtype)
-    args.d_h, args.ld_h = c.matrix(h, "h", m, n, dy.dtype)
-    args.d_rstd, args.d_gain = c.vector(rstd, "rstd", m), c.vector(gain, "gain", n)
-    if dh is not None:
-        args.d_dh, args.ld_dh = c.matrix(dh, "dh", m, n, dy.dtype)
-    args.d_dx, args.ld_dx = c.matrix(dx, "dx", m, n, dy.dtype)
-    if dr is not None:
-        args.d_dr, args.ld_dr = c.matrix(dr, "dr", m, n, dy.dtype)
-    args.d_dgain = c.vector(dgain, "dgain", n)
-    args.drop = c.drop(dropout, m)
-    c.run("zg_rms_norm_backward", args, workspace=True)
+    (m, n), device = _shape(dy, "dy")
+    dtype = dy.dtype
+    made = []
+    dx, dx_at, ld_dx = _out(dx, "dx", m, n, dtype, device, made, dy)
+    two = dr is not None or (need_dr and dropout is not None and dropout.p > 0)
+    dr, dr_at, ld_dr = _out(dr, "dr", m, n, dtype, device, made, dy) if two else _NONE3
+    dgain, dg_at = _out_vector(dgain, "dgain", n, device, made) if need_dgain or dgain is not None else (None, 0)
+    _run("zg_rms_norm_backward", (m, _vector(rows, "rows", 1, _I32, device), n, _type(dtype, "dy"), *_matrix(dy, "dy", m, n, dtype, device),
+                                  *_matrix(h, "h", m, n, dtype, device), _vector(rstd, "rstd", m, _F32, device), _vector(gain, "gain", n, _F32, device),
+                                  *(_matrix(dh, "dh", m, n, dtype, device) if dh is not None else (0, 0)),
+                                  dx_at, ld_dx, dr_at, ld_dr, dg_at, *_mask(dropout, m, device)),
+         device, stream, made, workspace=True)
     return dx, dr, dgain

@@ -155,3 +155,16 @@ def test_no_rows_is_no_work():
     assert zg.lib().zg_linear(C.byref(a), None) == zg.OK
     assert zg.lib().zg_dropout(C.byref(zg.DropoutArgs(rows=0, cols=8, dtype=zg.F32)), None) == zg.OK
     assert zg.lib().zg_rms_norm(C.byref(zg.NormArgs(rows=0, cols=8, dtype=zg.F32, out_dtype=zg.F32)), None) == zg.OK
+
+
+def test_the_packed_structs_are_the_same_field_by_field():
+    import struct
+    for name, mirror in (("zg_linear", zg.LinearArgs), ("zg_linear_backward", zg.LinearGradArgs), ("zg_dropout", zg.DropoutArgs),
+                         ("zg_rms_norm", zg.NormArgs), ("zg_rms_norm_backward", zg.NormGradArgs)):
+        flat = [(f, t, getattr(mirror, f).offset) for f, t in mirror._fields_ if f != "drop"]
+        flat += [(f, t, mirror.drop.offset + getattr(zg.Drop, f).offset) for f, t in zg.Drop._fields_]
+        values = [i + (0.5 if t in (C.c_double, C.c_float) else 0) for i, (_, t, _) in enumerate(flat)]
+        packed = struct.pack(layers._PACK[name], *values)
+        assert len(packed) == C.sizeof(mirror)
+        for (field, t, at), v in zip(flat, values):
+            assert t.from_buffer_copy(packed, at).value == v, (name, field)
