@@ -306,7 +306,7 @@ template <class T, int tile, bool TURNED> struct Side {
 };
 
 // What a wavefront does with its 32 FM x 64 cells' sums.  Of 32 x 32 cells a lane has row lane % 32, columns 8 q + 4 half + 0..3 in registers
-// 4 q + 0..3: they go through LDS (`mine`: 16 KB of the wavefront's own, free from here on), 64 rows at a time, so that eight lanes have 64 columns of a row
+// 4 q + 0..3: they go through LDS (`mine`: 8 KB of the wavefront's own, free from here on), 32 rows at a time, so that eight lanes have 64 columns of a row
 // and memory sees whole lines.  Places are 16 bytes, 16 to a row, turned by the row so that neither way meets in a bank.
 template <class O, int FM> __device__ __forceinline__ void hand_over(const ProductArgs &p, f32x16 (&acc)[FM][2], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t split)
 {
@@ -315,52 +315,58 @@ template <class O, int FM> __device__ __forceinline__ void hand_over(const Produ
     Epilogue e = p.e;
     if (split) e.Y = static_cast<float *>(e.Y) + split * e.part;
 #pragma unroll
-    for (int h = 0; h < FM; h += 2) {
+    for (int i = 0; i < FM; ++i) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t at = (32 * i + row) * 16 + ((8 * j + 2 * q + half) ^ (row & 15));
-                    mine[at] = f32x4{acc[h + i][j][4 * q], acc[h + i][j][4 * q + 1], acc[h + i][j][4 * q + 2], acc[h + i][j][4 * q + 3]};
-                }
+            for (int q = 0; q < 4; ++q)
+                mine[row * 16 + ((8 * j + 2 * q + half) ^ (row & 15))] = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
         if (c.left <= 0) continue; // (a wavefront's LDS accesses are in order)
-#pragma unroll 1
-        for (uint32_t r0 = lane >> 3; r0 < 64; r0 += 32)
-            finish<O, 4>(e, c, m_wave + 32 * h + r0, 8, M, [&](int u, float (&v)[8]) {
-                const uint32_t r = r0 + 8 * u;
-                const f32x4 lo = mine[r * 16 + ((2 * g) ^ (r & 15))], hi = mine[r * 16 + ((2 * g + 1) ^ (r & 15))];
+        finish<O, 4>(e, c, m_wave + 32 * i + (lane >> 3), 8, M, [&](int u, float (&v)[8]) {
+            const uint32_t r = (lane >> 3) + 8 * u;
+            const f32x4 lo = mine[r * 16 + ((2 * g) ^ (r & 15))], hi = mine[r * 16 + ((2 * g + 1) ^ (r & 15))];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = lo[j], v[4 + j] = hi[j];
-            });
+            for (int j = 0; j < 4; ++j) v[j] = lo[j], v[4 + j] = hi[j];
+        });
     }
 }
 
-// Which tile, and which part of the sum, a workgroup has.  Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles, those of
-// one row of tiles (of one part of the sum) beside each other, so that what they share is in its L2.
+// The tiles of a product, and the parts of their sums.  Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles, those of one row of
+// tiles (of one part of the sum) beside each other, so that what they share is in its L2, and its workgroups take them in turn.
 struct Place {
-    uint32_t M, m0, n0, split, k_first, k_end;
+    uint32_t m0, n0, split, k_first, k_end;
 };
 
-template <int BM, int BN> __device__ __forceinline__ bool place_of(const ProductArgs &p, uint32_t depth, Place &w)
-{
-    const uint32_t live = p.rows.live();
-    w.M = p.rows_are_k ? p.M : min(p.M, live);
-    const uint32_t k_all = p.rows_are_k ? min(p.K, live) : p.K;
-    const uint32_t nt = (p.N + BN - 1) / BN, mt = (w.M + BM - 1) / BM;
-    const uint64_t in_part = (uint64_t)mt * nt, tiles = in_part * p.splits, share = (tiles + 7) / 8;
-    const uint64_t t = (blockIdx.x % 8) * share + blockIdx.x / 8;
-    if (blockIdx.x / 8 >= share || t >= tiles) return false;
-    w.split = p.splits > 1 ? (uint32_t)(t / in_part) : 0u;
-    const uint32_t in_split = (uint32_t)(t - w.split * in_part);
-    w.m0 = in_split / nt * BM;
-    w.n0 = in_split % nt * BN;
-    const uint32_t part_k = ((k_all + p.splits - 1) / p.splits + depth - 1) / depth * depth;
-    w.k_first = (uint32_t)min((uint64_t)k_all, (uint64_t)part_k * w.split);
-    w.k_end = (uint32_t)min((uint64_t)k_all, (uint64_t)w.k_first + part_k);
-    return true;
-}
+template <int BM, int BN> struct Tiles {
+    uint32_t M, k_all, nt, splits, part_k;
+    uint64_t in_part, next, end; // of this workgroup: the next tile, the end of its XCD's run
+
+    __device__ __forceinline__ Tiles(const ProductArgs &p, uint32_t depth)
+    {
+        const uint32_t live = p.rows.live();
+        M = p.rows_are_k ? p.M : min(p.M, live);
+        k_all = p.rows_are_k ? min(p.K, live) : p.K;
+        nt = (p.N + BN - 1) / BN;
+        splits = p.splits;
+        in_part = (uint64_t)((M + BM - 1) / BM) * nt;
+        part_k = ((k_all + splits - 1) / splits + depth - 1) / depth * depth;
+        const uint64_t tiles = in_part * splits, share = (tiles + 7) / 8;
+        next = blockIdx.x % 8 * share + blockIdx.x / 8;
+        end = min((blockIdx.x % 8 + 1) * share, tiles);
+    }
+    __device__ __forceinline__ bool take(Place &w)
+    {
+        if (next >= end) return false;
+        w.split = splits > 1 ? (uint32_t)(next / in_part) : 0u;
+        const uint32_t t = (uint32_t)(next - w.split * in_part);
+        w.m0 = t / nt * BM;
+        w.n0 = t % nt * BN;
+        w.k_first = (uint32_t)min((uint64_t)k_all, (uint64_t)part_k * w.split);
+        w.k_end = (uint32_t)min((uint64_t)k_all, (uint64_t)w.k_first + part_k);
+        next += gridDim.x / 8;
+        return true;
+    }
+};
 
 // A tile of BM x BN cells: four wavefronts, two by two, matrix instructions of 32 x 32 cells; eight chunks of k at a time through two buffers
 // in LDS, the next ones on their way in registers.  The first operand of an instruction is b, so that a lane's cells lie side by side in a
@@ -369,12 +375,13 @@ template <class T, int BM, int BN, bool A_TURNED, bool B_TURNED> __global__ __la
 {
     constexpr int K = chunk_k<T>, depth = 8 * K, FM = BM / 64, FN = BN / 64;
     __shared__ u32x4 lds[2][(BM + BN) * 8];
+    Tiles<BM, BN> tiles(p, depth);
     Place w;
-    if (!place_of<BM, BN>(p, depth, w)) return;
-    const uint32_t k_end = w.k_end;
+    if (!tiles.take(w)) return;
+    const uint32_t k_end = w.k_end, M = tiles.M;
     Side<T, BM, A_TURNED> a;
     Side<T, BN, B_TURNED> b;
-    a.p = static_cast<const T *>(p.a.p), a.ld = p.a.ld, a.first = w.m0, a.rows = w.M;
+    a.p = static_cast<const T *>(p.a.p), a.ld = p.a.ld, a.first = w.m0, a.rows = M;
     b.p = static_cast<const T *>(p.b.p), b.ld = p.b.ld, b.first = w.n0, b.rows = p.N;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const uint32_t wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2), am = wm + (lane & 31), bn = wn + (lane & 31);
@@ -411,7 +418,7 @@ template <class T, int BM, int BN, bool A_TURNED, bool B_TURNED> __global__ __la
         }
         __syncthreads();
     }
-    hand_over<AnyType>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 1024, w.m0 + wm, w.n0 + wn, w.M, w.split);
+    hand_over<AnyType>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 512, w.m0 + wm, w.n0 + wn, M, w.split);
 }
 
 // ---- operands in whole chunks ---------------------------------------------------------------------------------------------------
@@ -425,15 +432,17 @@ typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-template <int n> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory"); }
+// all but the last n loads of this wavefront are done, and so are its reads of LDS
+template <int n> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(n) : "memory"); }
 
 // One operand's buffer in LDS, 4 `tile` places of 16 bytes, and its way there: 64 places side by side are filled by one instruction of a
 // wavefront, each lane's from where it says.
-template <class T, int tile, bool TURNED> struct Feed;
+template <class T, int tile, int waves, bool TURNED> struct Feed;
 
-// Along k in memory: place (row i, chunk c) is 8 (i / 2) + 4 (i % 2) + (c ^ (i / 2) % 4), so that eight rows at one c lie in eight groups of banks.
-template <class T, int tile> struct Feed<T, tile, false> {
-    static constexpr int K = 16 / (int)sizeof(T), loads = tile * 4 / 256;
+// Along k in memory: place (row i, chunk c) is 4 i + (c ^ i / 4 % 4).  LDS serves 16 lanes of a 16-byte read at a time, 0-3, 12-15, 20-23 and 24-27
+// first: at one c those rows lie in 16 different groups of banks, as do the others'.
+template <class T, int tile, int waves> struct Feed<T, tile, waves, false> {
+    static constexpr int K = 16 / (int)sizeof(T), loads = tile * 4 / (64 * waves);
     const char *p;
     uint32_t from[loads], chunk;
 
@@ -444,7 +453,7 @@ template <class T, int tile> struct Feed<T, tile, false> {
 #pragma unroll
         for (int l = 0; l < loads; ++l) {
             const uint32_t s = (wave * loads + l) * 64 + lane, i = s / 4;
-            chunk = (s & 3) ^ ((s / 8) & 3); // (the same for every l: 64 places are 8 pairs of rows)
+            chunk = (s & 3) ^ ((s / 16) & 3); // (the same for every l: 64 places are 16 rows)
             from[l] = first + i < rows ? (uint32_t)(i * ld) + chunk * 16 : kReach;
         }
     }
@@ -460,13 +469,13 @@ template <class T, int tile> struct Feed<T, tile, false> {
     // chunk c of row i
     __device__ __forceinline__ static u32x4 chunk_of(const u32x4 *buffer, uint32_t i, uint32_t c)
     {
-        return buffer[(i >> 1) * 8 + (i & 1) * 4 + (c ^ ((i >> 1) & 3))];
+        return buffer[4 * i + (c ^ ((i >> 2) & 3))];
     }
 };
 
 // Along the rows in memory: the buffer holds a row of the tile's `tile` rows for each k, and a lane's chunk is put together as it is read.
-template <class T, int tile> struct Feed<T, tile, true> {
-    static constexpr int K = 16 / (int)sizeof(T), loads = tile * 4 / 256, row = tile / K; // places of one k
+template <class T, int tile, int waves> struct Feed<T, tile, waves, true> {
+    static constexpr int K = 16 / (int)sizeof(T), loads = tile * 4 / (64 * waves), row = tile / K; // places of one k
     const char *p;
     uint64_t ld;
     uint32_t from[loads], k_of[loads];
@@ -517,68 +526,93 @@ template <class T, int tile> struct Feed<T, tile, true> {
     }
 };
 
-template <class T, class O, int BM, int BN, bool A_TURNED, bool B_TURNED> __global__ __launch_bounds__(256, 2) void k_chunks(ProductArgs p)
+// WM x WN wavefronts, BLOCKS workgroups to a compute unit.  STAY: a workgroup takes one tile after the other, and the next tile's first steps are
+// on their way while this one's cells are handed over, which go through LDS of their own then.
+template <class T, class O, int BM, int BN, int WM, int WN, int BLOCKS, bool STAY, bool A_TURNED, bool B_TURNED>
+__global__ __launch_bounds__(WM *WN * 64, WM *WN *BLOCKS / 4) void k_chunks(ProductArgs p)
 {
-    using A = Feed<T, BM, A_TURNED>;
-    using B = Feed<T, BN, B_TURNED>;
-    constexpr int depth = 4 * A::K, FM = BM / 64, FN = BN / 64, stages = 3;
-    __shared__ u32x4 lds[stages][(BM + BN) * 4];
-    Place w;
-    if (!place_of<BM, BN>(p, depth, w)) return;
+    constexpr int waves = WM * WN;
+    using A = Feed<T, BM, waves, A_TURNED>;
+    using B = Feed<T, BN, waves, B_TURNED>;
+    constexpr int depth = 4 * A::K, FM = BM / WM / 32, FN = BN / WN / 32, stages = 3, stage = (BM + BN) * 4;
+    __shared__ u32x4 lds[stages * stage + (STAY ? waves * 512 : 0)];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const uint32_t wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2), am = wm + (lane & 31), bn = wn + (lane & 31);
+    const uint32_t wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN), am = wm + (lane & 31), bn = wn + (lane & 31);
+    Tiles<BM, BN> tiles(p, depth), ahead = tiles;
+    // the step that is asked for next: two before the one that is multiplied
+    Place w, h;
     A a;
     B b;
-    a.start(p.a, w.m0, w.M, wave, lane);
-    b.start(p.b, w.n0, p.N, wave, lane);
-    const auto fetch = [&](uint32_t k0, int stage) {
-        a.fetch(k0, w.k_end, lds[stage], wave);
-        b.fetch(k0, w.k_end, lds[stage] + BM * 4, wave);
+    uint32_t asked = 0, done = 0, into = 0;
+    bool more = ahead.take(h);
+    const auto start = [&] {
+        while (more && h.k_first >= h.k_end) more = ahead.take(h);
+        if (!more) return;
+        a.start(p.a, h.m0, tiles.M, wave, lane);
+        b.start(p.b, h.n0, p.N, wave, lane);
     };
-    f32x16 acc[FM][FN] = {};
-    const uint32_t steps = (w.k_end - w.k_first + depth - 1) / depth;
-    if (steps > 0) fetch(w.k_first, 0);
-    if (steps > 1) fetch(w.k_first + depth, 1);
-    int now = 0, next = 2;
-    for (uint32_t t = 0; t < steps; ++t) {
-        if (t + 1 < steps) wait_loads<A::loads + B::loads>();
-        else wait_loads<0>();
-        __builtin_amdgcn_s_barrier(); // every wavefront's chunks of this step are there, and the step before is multiplied
-        asm volatile("" ::: "memory");
-        if (t + 2 < steps) fetch(w.k_first + (t + 2) * depth, next);
-        const u32x4 *la = lds[now], *lb = lds[now] + BM * 4;
-        if constexpr (std::is_same_v<T, uint8_t>) {
-            u32x4 fa[FM][2], fb[FN][2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int i = 0; i < FM; ++i) fa[i][h] = A::chunk_of(la, am + 32 * i, 2 * half + h);
-#pragma unroll
-                for (int j = 0; j < FN; ++j) fb[j][h] = B::chunk_of(lb, bn + 32 * j, 2 * half + h);
-            }
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j) multiply2(fb[j][0], fb[j][1], fa[i][0], fa[i][1], acc[i][j]);
+    const auto fetch = [&] {
+        if (!more) return;
+        a.fetch(h.k_first, h.k_end, lds + into * stage, wave);
+        b.fetch(h.k_first, h.k_end, lds + into * stage + BM * 4, wave);
+        into = into == stages - 1 ? 0 : into + 1;
+        ++asked;
+        h.k_first += depth;
+        if (h.k_first < h.k_end) return;
+        if constexpr (STAY) {
+            more = ahead.take(h);
+            start();
         } else {
+            more = false;
+        }
+    };
+    start();
+    fetch();
+    fetch();
+    uint32_t now = 0;
+    while (tiles.take(w)) {
+        f32x16 acc[FM][FN] = {};
+        for (uint32_t k0 = w.k_first; k0 < w.k_end; k0 += depth) {
+            ++done;
+            if (asked > done) wait_loads<A::loads + B::loads>(); // (what was asked for last may still be on its way)
+            else wait_loads<0>();
+            __builtin_amdgcn_s_barrier(); // every wavefront's chunks of this step are there, and the step before is multiplied
+            asm volatile("" ::: "memory");
+            fetch();
+            const u32x4 *la = lds + now * stage, *lb = la + BM * 4;
+            if constexpr (std::is_same_v<T, uint8_t>) {
+                u32x4 fa[FM][2], fb[FN][2];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                u32x4 fa[FM], fb[FN];
+                for (int e = 0; e < 2; ++e) {
 #pragma unroll
-                for (int i = 0; i < FM; ++i) fa[i] = A::chunk_of(la, am + 32 * i, 2 * s + half);
+                    for (int i = 0; i < FM; ++i) fa[i][e] = A::chunk_of(la, am + 32 * i, 2 * half + e);
 #pragma unroll
-                for (int j = 0; j < FN; ++j) fb[j] = B::chunk_of(lb, bn + 32 * j, 2 * s + half);
+                    for (int j = 0; j < FN; ++j) fb[j][e] = B::chunk_of(lb, bn + 32 * j, 2 * half + e);
+                }
 #pragma unroll
                 for (int i = 0; i < FM; ++i)
 #pragma unroll
-                    for (int j = 0; j < FN; ++j) multiply(T(), fb[j], fa[i], acc[i][j]);
+                    for (int j = 0; j < FN; ++j) multiply2(fb[j][0], fb[j][1], fa[i][0], fa[i][1], acc[i][j]);
+            } else {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    u32x4 fa[FM], fb[FN];
+#pragma unroll
+                    for (int i = 0; i < FM; ++i) fa[i] = A::chunk_of(la, am + 32 * i, 2 * s + half);
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) fb[j] = B::chunk_of(lb, bn + 32 * j, 2 * s + half);
+#pragma unroll
+                    for (int i = 0; i < FM; ++i)
+#pragma unroll
+                        for (int j = 0; j < FN; ++j) multiply(T(), fb[j], fa[i], acc[i][j]);
+                }
             }
+            now = now == stages - 1 ? 0 : now + 1;
         }
-        now = now == stages - 1 ? 0 : now + 1;
-        next = next == stages - 1 ? 0 : next + 1;
+        if constexpr (!STAY) __syncthreads(); // the buffers are free
+        hand_over<O>(p, acc, reinterpret_cast<f32x4 *>(lds) + (STAY ? stages * stage : 0) + wave * 512, w.m0 + wm, w.n0 + wn, tiles.M, w.split);
+        if constexpr (!STAY) return;
     }
-    __syncthreads(); // the buffers are free
-    hand_over<O>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 1024, w.m0 + wm, w.n0 + wn, w.M, w.split);
 }
 
 // ---- few tiles ------------------------------------------------------------------------------------------------------------------
@@ -755,7 +789,13 @@ template <class T> bool few_tiles(const ProductArgs &p, bool chunks)
 
 template <class T, class O, bool A_TURNED, bool B_TURNED> int launch_chunks(hipStream_t st, const ProductArgs &p)
 {
-    return launch(st, k_chunks<T, O, kTileM, kTileN, A_TURNED, B_TURNED>, tile_grid<kTileM, kTileN>(p), 256, p);
+    if constexpr (std::is_same_v<T, float>) {
+        return launch(st, k_chunks<T, O, 128, 128, 2, 2, 3, false, A_TURNED, B_TURNED>, tile_grid<128, 128>(p), 256, p);
+    } else {
+        const dim3 grid = tile_grid<256, 256>(p);
+        if (grid.x >= 256) return launch(st, k_chunks<T, O, 256, 256, 2, 4, 1, true, A_TURNED, B_TURNED>, dim3(256), 512, p);
+        return launch(st, k_chunks<T, O, 256, 128, 2, 2, 2, false, A_TURNED, B_TURNED>, tile_grid<256, 128>(p), 256, p);
+    }
 }
 
 // the tiles of one product, or of the parts of one, whose results are of type p.e.type
