@@ -331,6 +331,31 @@ template <class O, int FM> __device__ __forceinline__ void hand_over(const Produ
     }
 }
 
+// The same through 4 KB, 32 x 32 cells at a time: four lanes have 32 columns of a row.
+template <class O, int FM> __device__ __forceinline__ void hand_over_narrow(const ProductArgs &p, f32x16 (&acc)[FM][2], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t split)
+{
+    const uint32_t lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31, g = lane & 3;
+    Epilogue e = p.e;
+    if (split) e.Y = static_cast<float *>(e.Y) + split * e.part;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const Columns c = columns_of(p.e, n_wave + 32 * j + 8 * g, p.N);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                mine[row * 8 + ((2 * q + half) ^ ((row >> 1) & 7))] = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+            if (c.left <= 0) continue;
+            finish<O, 2>(e, c, m_wave + 32 * i + (lane >> 2), 16, M, [&](int u, float (&v)[8]) {
+                const uint32_t r = (lane >> 2) + 16 * u;
+                const f32x4 lo = mine[r * 8 + ((2 * g) ^ ((r >> 1) & 7))], hi = mine[r * 8 + ((2 * g + 1) ^ ((r >> 1) & 7))];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = lo[k], v[4 + k] = hi[k];
+            });
+        }
+    }
+}
+
 // The tiles of a product, and the parts of their sums.  Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles, those of one row of
 // tiles (of one part of the sum) beside each other, so that what they share is in its L2, and its workgroups take them in turn.
 struct Place {
@@ -349,7 +374,7 @@ template <int BM, int BN> struct Tiles {
         nt = (p.N + BN - 1) / BN;
         splits = p.splits;
         in_part = (uint64_t)((M + BM - 1) / BM) * nt;
-        part_k = ((k_all + splits - 1) / splits + depth - 1) / depth * depth;
+        part_k = __builtin_amdgcn_readfirstlane(((k_all + splits - 1) / splits + depth - 1) / depth * depth);
         const uint64_t tiles = in_part * splits, share = (tiles + 7) / 8;
         next = blockIdx.x % 8 * share + blockIdx.x / 8;
         end = min((blockIdx.x % 8 + 1) * share, tiles);
@@ -357,12 +382,14 @@ template <int BM, int BN> struct Tiles {
     __device__ __forceinline__ bool take(Place &w)
     {
         if (next >= end) return false;
-        w.split = splits > 1 ? (uint32_t)(next / in_part) : 0u;
-        const uint32_t t = (uint32_t)(next - w.split * in_part);
-        w.m0 = t / nt * BM;
-        w.n0 = t % nt * BN;
-        w.k_first = (uint32_t)min((uint64_t)k_all, (uint64_t)part_k * w.split);
-        w.k_end = (uint32_t)min((uint64_t)k_all, (uint64_t)w.k_first + part_k);
+        // (all of it is the same in every lane: said so, or the divisions would leave it in vector registers)
+        const auto same = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane(v); };
+        w.split = splits > 1 ? same((uint32_t)(next / in_part)) : 0u;
+        const uint32_t t = same((uint32_t)(next - w.split * in_part)), row = same(t / nt);
+        w.m0 = row * BM;
+        w.n0 = (t - row * nt) * BN;
+        w.k_first = same((uint32_t)min((uint64_t)k_all, (uint64_t)part_k * w.split));
+        w.k_end = same((uint32_t)min((uint64_t)k_all, (uint64_t)w.k_first + part_k));
         next += gridDim.x / 8;
         return true;
     }
@@ -457,14 +484,15 @@ template <class T, int tile, int waves> struct Feed<T, tile, waves, false> {
             from[l] = first + i < rows ? (uint32_t)(i * ld) + chunk * 16 : kReach;
         }
     }
-    // k0 .. k0 + 4 K - 1, zeros from k_end on
-    __device__ __forceinline__ void fetch(uint32_t k0, uint32_t k_end, u32x4 *buffer, uint32_t wave) const
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t at(uint32_t k0) const
     {
-        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p) + (uint64_t)k0 * sizeof(T), 0, kReach, 0x00027000);
-        const uint32_t beyond = k0 + (chunk + 1) * K <= k_end ? 0u : kReach;
-#pragma unroll
-        for (int l = 0; l < loads; ++l)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u32x4 *)(buffer + (wave * loads + l) * 64), 16, (int)(from[l] | beyond), 0, 0, 0);
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p) + (uint64_t)k0 * sizeof(T), 0, kReach, 0x00027000);
+    }
+    // the lth of a step's loads, out of at(k0); zeros where there are no more than `left` k from k0 on
+    __device__ __forceinline__ void fetch(int l, __amdgpu_buffer_rsrc_t r, uint32_t left, u32x4 *buffer, uint32_t wave) const
+    {
+        const uint32_t beyond = (chunk + 1) * K <= left ? 0u : kReach;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u32x4 *)(buffer + (wave * loads + l) * 64), 16, (int)(from[l] | beyond), 0, 0, 0);
     }
     // chunk c of row i
     __device__ __forceinline__ static u32x4 chunk_of(const u32x4 *buffer, uint32_t i, uint32_t c)
@@ -494,12 +522,13 @@ template <class T, int tile, int waves> struct Feed<T, tile, waves, true> {
             from[l] = first + i < rows ? (uint32_t)(k_of[l] * ld) + i * (uint32_t)sizeof(T) : kReach;
         }
     }
-    __device__ __forceinline__ void fetch(uint32_t k0, uint32_t k_end, u32x4 *buffer, uint32_t wave) const
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t at(uint32_t k0) const
     {
-        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p) + k0 * ld, 0, kReach, 0x00027000);
-#pragma unroll
-        for (int l = 0; l < loads; ++l)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u32x4 *)(buffer + (wave * loads + l) * 64), 16, (int)(from[l] | (k0 + k_of[l] < k_end ? 0u : kReach)), 0, 0, 0);
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p) + k0 * ld, 0, kReach, 0x00027000);
+    }
+    __device__ __forceinline__ void fetch(int l, __amdgpu_buffer_rsrc_t r, uint32_t left, u32x4 *buffer, uint32_t wave) const
+    {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u32x4 *)(buffer + (wave * loads + l) * 64), 16, (int)(from[l] | (k_of[l] < left ? 0u : kReach)), 0, 0, 0);
     }
     // 16-bit: a group of 16 lanes reads four k of 16 rows, four rows to a lane, and each gets its row's four k (lane 4 k + r / 4 has
     // rows r .. r + 3 of the k-th); i = the lane's row.  fp32: four reads.
@@ -526,93 +555,193 @@ template <class T, int tile, int waves> struct Feed<T, tile, waves, true> {
     }
 };
 
-// WM x WN wavefronts, BLOCKS workgroups to a compute unit.  STAY: a workgroup takes one tile after the other, and the next tile's first steps are
-// on their way while this one's cells are handed over, which go through LDS of their own then.
-template <class T, class O, int BM, int BN, int WM, int WN, int BLOCKS, bool STAY, bool A_TURNED, bool B_TURNED>
-__global__ __launch_bounds__(WM *WN * 64, WM *WN *BLOCKS / 4) void k_chunks(ProductArgs p)
+// One of the two parts of a step: a wavefront's fragments of 32 rows, a chunk of each to a lane.  8 bits: both chunks of a lane in one
+// instruction, the parts are halves of a's fragments and b's are read with the first.
+template <class T, int FM, int FN> struct Part {
+    static constexpr bool both = std::is_same_v<T, uint8_t>;
+    static constexpr int fm = both ? FM / 2 : FM, chunks = both ? 2 : 1;
+    u32x4 a[fm][chunks], b[FN][chunks];
+
+    template <class A, class B> __device__ __forceinline__ void read(int part, const u32x4 *la, const u32x4 *lb, uint32_t am, uint32_t bn, uint32_t half)
+    {
+#pragma unroll
+        for (int c = 0; c < chunks; ++c) {
+            const uint32_t at = both ? 2 * half + c : 2 * part + half;
+            if (!both || part == 0) {
+#pragma unroll
+                for (int j = 0; j < FN; ++j) b[j][c] = B::chunk_of(lb, bn + 32 * j, at);
+            }
+#pragma unroll
+            for (int i = 0; i < fm; ++i) a[i][c] = A::chunk_of(la, am + 32 * (both ? part * fm + i : i), at);
+        }
+    }
+    // `between(n)` is called behind the nth product, n < fm FN
+    template <int part, class F> __device__ __forceinline__ void multiply_into(f32x16 (&acc)[FM][FN], const Part &with_b, F &&between) const
+    {
+#pragma unroll
+        for (int i = 0; i < fm; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                if constexpr (both) multiply2(with_b.b[j][0], with_b.b[j][1], a[i][0], a[i][1], acc[part * fm + i][j]);
+                else multiply(T(), with_b.b[j][0], a[i][0], acc[i][j]);
+                between(i * FN + j);
+            }
+    }
+};
+
+// The steps of a tile, one after the other, in two parts each: while the matrix instructions of one part run, the chunks of the next are on their way
+// from LDS.  Between the parts all wavefronts meet: from there on the step's buffer is free - it is asked to be filled with the step that comes
+// `stages` later - and the next step's is full.  The loads go out one by one between the products: together, right behind the meeting, those of
+// all wavefronts queue up and the products wait behind them.  (8 bits: the registers do not hold the next step's first part beside this one's second.)
+template <class T, class A, class B, int FM, int FN, int stages, class Fetch>
+__device__ __forceinline__ void multiply_steps(f32x16 (&acc)[FM][FN], const u32x4 *lds, int lb_at, uint32_t stage, uint32_t steps, uint32_t am, uint32_t bn,
+                                               uint32_t &now, Fetch &fetch)
 {
-    constexpr int waves = WM * WN;
-    using A = Feed<T, BM, waves, A_TURNED>;
-    using B = Feed<T, BN, waves, B_TURNED>;
-    constexpr int depth = 4 * A::K, FM = BM / WM / 32, FN = BN / WN / 32, stages = 3, stage = (BM + BN) * 4;
-    __shared__ u32x4 lds[stages * stage + (STAY ? waves * 512 : 0)];
-    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const uint32_t wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN), am = wm + (lane & 31), bn = wn + (lane & 31);
-    Tiles<BM, BN> tiles(p, depth), ahead = tiles;
-    // the step that is asked for next: two before the one that is multiplied
-    Place w, h;
+    constexpr int loads = A::loads + B::loads, products = Part<T, FM, FN>::fm * FN;
+    constexpr bool both = Part<T, FM, FN>::both;
+    const uint32_t half = (threadIdx.x & 63) >> 5;
+    Part<T, FM, FN> one, two;
+    const auto read = [&](Part<T, FM, FN> &part, int n) {
+        const u32x4 *const la = lds + now * stage;
+        part.template read<A, B>(n, la, la + lb_at, am, bn, half);
+    };
+    read(one, 0);
+    for (uint32_t t = 0; t < steps; ++t) {
+        read(two, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        one.template multiply_into<0>(acc, one, [](int) {});
+        __builtin_amdgcn_sched_barrier(0);
+        // this wavefront's share of the next step is there (what was asked for behind it may be on its way), and it has read this step's chunks
+        wait_loads<(stages - 2) * loads>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        now = now == stages - 1 ? 0 : now + 1;
+        if (!both) read(one, 0); // (behind the last step, too: nobody looks at it then)
+        __builtin_amdgcn_sched_barrier(0);
+        fetch.open();
+        two.template multiply_into<1>(acc, both ? one : two, [&](int n) {
+#pragma unroll
+            for (int l = 0; l < loads; ++l)
+                if (l * products / loads == n) fetch.load(l);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        fetch.next();
+        if (both) read(one, 0);
+    }
+}
+
+// What is asked for of both operands, step by step, into one buffer after the other; `on` moves it to the next tile, if there is one.  Where nothing is
+// left it asks for zeros all the same, into buffers that nobody reads: what a wavefront waits for is then the same at every step.
+template <class A, class B, int BM, int stage, int stages, class On> struct Fetch {
+    A &a;
+    B &b;
+    u32x4 *lds;
+    uint32_t wave, k, k_end;
+    On on;
+    uint32_t into = 0, left = 0;
+    __amdgpu_buffer_rsrc_t ra, rb;
+
+    __device__ __forceinline__ void open()
+    {
+        left = k < k_end ? k_end - k : 0u;
+        ra = a.at(k);
+        rb = b.at(k);
+    }
+    __device__ __forceinline__ void load(int l) const
+    {
+        u32x4 *const to = lds + into * stage;
+        if (l < A::loads) a.fetch(l, ra, left, to, wave);
+        else b.fetch(l - A::loads, rb, left, to + BM * 4, wave);
+    }
+    __device__ __forceinline__ void next()
+    {
+        into = into == stages - 1 ? 0 : into + 1;
+        if (left == 0) return;
+        k += 4 * A::K;
+        if (k >= k_end) on(*this);
+    }
+    // the first steps, of which the first is there then
+    __device__ __forceinline__ void begin()
+    {
+#pragma unroll
+        for (int i = 0; i < stages; ++i) {
+            open();
+#pragma unroll
+            for (int l = 0; l < A::loads + B::loads; ++l) load(l);
+            next();
+        }
+        wait_loads<(stages - 1) * (A::loads + B::loads)>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    }
+};
+
+// Four wavefronts, two by two, BLOCKS workgroups to a compute unit; three buffers.
+template <class T, class O, int BM, int BN, int BLOCKS, bool A_TURNED, bool B_TURNED> __global__ __launch_bounds__(256, BLOCKS) void k_chunks(ProductArgs p)
+{
+    using A = Feed<T, BM, 4, A_TURNED>;
+    using B = Feed<T, BN, 4, B_TURNED>;
+    constexpr int depth = 4 * A::K, FM = BM / 64, FN = BN / 64, stages = 3, stage = (BM + BN) * 4;
+    __shared__ u32x4 lds[stages * stage];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2), am = wm + (lane & 31), bn = wn + (lane & 31);
+    Tiles<BM, BN> tiles(p, depth);
+    Place w;
+    if (!tiles.take(w)) return;
     A a;
     B b;
-    uint32_t asked = 0, done = 0, into = 0;
-    bool more = ahead.take(h);
-    const auto start = [&] {
-        while (more && h.k_first >= h.k_end) more = ahead.take(h);
-        if (!more) return;
-        a.start(p.a, h.m0, tiles.M, wave, lane);
-        b.start(p.b, h.n0, p.N, wave, lane);
-    };
-    const auto fetch = [&] {
-        if (!more) return;
-        a.fetch(h.k_first, h.k_end, lds + into * stage, wave);
-        b.fetch(h.k_first, h.k_end, lds + into * stage + BM * 4, wave);
-        into = into == stages - 1 ? 0 : into + 1;
-        ++asked;
-        h.k_first += depth;
-        if (h.k_first < h.k_end) return;
-        if constexpr (STAY) {
-            more = ahead.take(h);
-            start();
-        } else {
-            more = false;
+    a.start(p.a, w.m0, tiles.M, wave, lane);
+    b.start(p.b, w.n0, p.N, wave, lane);
+    const uint32_t steps = (w.k_end - w.k_first + depth - 1) / depth;
+    const auto no_more = [](auto &) {};
+    Fetch<A, B, BM, stage, stages, decltype(no_more)> fetch{a, b, lds, wave, w.k_first, w.k_end, no_more};
+    f32x16 acc[FM][FN] = {};
+    uint32_t now = 0;
+    if (steps > 0) {
+        fetch.begin();
+        multiply_steps<T, A, B, FM, FN, stages>(acc, lds, BM * 4, stage, steps, am, bn, now, fetch);
+        wait_loads<0>();
+    }
+    __syncthreads(); // the buffers are free
+    hand_over<O>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 512, w.m0 + wm, w.n0 + wn, tiles.M, w.split);
+}
+
+// Eight wavefronts, 256 x 256 cells, one workgroup to a compute unit, which takes one tile after the other; four buffers.  The next tile's
+// first steps are on their way while this one's cells are handed over, through LDS of their own.
+template <class T, class O, bool A_TURNED, bool B_TURNED> __global__ __launch_bounds__(512, 2) void k_long(ProductArgs p)
+{
+    constexpr int BM = 256, BN = 256, FM = 4, FN = 2, stages = 4, stage = (BM + BN) * 4;
+    using A = Feed<T, BM, 8, A_TURNED>;
+    using B = Feed<T, BN, 8, B_TURNED>;
+    constexpr int depth = 4 * A::K;
+    __shared__ u32x4 lds[stages * stage + 8 * 256];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t wm = (wave >> 2) * 128, wn = (wave & 3) * 64, am = wm + (lane & 31), bn = wn + (lane & 31);
+    Tiles<BM, BN> tiles(p, depth), ahead = tiles;
+    A a{}; // (a workgroup without a tile asks for zeros)
+    B b{};
+    const auto on = [&](auto &fetch) { // to the next tile that has something to read
+        Place h;
+        while (ahead.take(h)) {
+            if (h.k_first >= h.k_end) continue;
+            a.start(p.a, h.m0, tiles.M, wave, lane);
+            b.start(p.b, h.n0, p.N, wave, lane);
+            fetch.k = h.k_first, fetch.k_end = h.k_end;
+            return;
         }
     };
-    start();
-    fetch();
-    fetch();
+    Fetch<A, B, BM, stage, stages, decltype(on)> fetch{a, b, lds, wave, 0, 0, on};
+    on(fetch);
+    fetch.begin();
+    Place w;
     uint32_t now = 0;
     while (tiles.take(w)) {
         f32x16 acc[FM][FN] = {};
-        for (uint32_t k0 = w.k_first; k0 < w.k_end; k0 += depth) {
-            ++done;
-            if (asked > done) wait_loads<A::loads + B::loads>(); // (what was asked for last may still be on its way)
-            else wait_loads<0>();
-            __builtin_amdgcn_s_barrier(); // every wavefront's chunks of this step are there, and the step before is multiplied
-            asm volatile("" ::: "memory");
-            fetch();
-            const u32x4 *la = lds + now * stage, *lb = la + BM * 4;
-            if constexpr (std::is_same_v<T, uint8_t>) {
-                u32x4 fa[FM][2], fb[FN][2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                    for (int i = 0; i < FM; ++i) fa[i][e] = A::chunk_of(la, am + 32 * i, 2 * half + e);
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) fb[j][e] = B::chunk_of(lb, bn + 32 * j, 2 * half + e);
-                }
-#pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) multiply2(fb[j][0], fb[j][1], fa[i][0], fa[i][1], acc[i][j]);
-            } else {
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    u32x4 fa[FM], fb[FN];
-#pragma unroll
-                    for (int i = 0; i < FM; ++i) fa[i] = A::chunk_of(la, am + 32 * i, 2 * s + half);
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) fb[j] = B::chunk_of(lb, bn + 32 * j, 2 * s + half);
-#pragma unroll
-                    for (int i = 0; i < FM; ++i)
-#pragma unroll
-                        for (int j = 0; j < FN; ++j) multiply(T(), fb[j], fa[i], acc[i][j]);
-                }
-            }
-            now = now == stages - 1 ? 0 : now + 1;
-        }
-        if constexpr (!STAY) __syncthreads(); // the buffers are free
-        hand_over<O>(p, acc, reinterpret_cast<f32x4 *>(lds) + (STAY ? stages * stage : 0) + wave * 512, w.m0 + wm, w.n0 + wn, tiles.M, w.split);
-        if constexpr (!STAY) return;
+        const uint32_t steps = (w.k_end - w.k_first + depth - 1) / depth;
+        if (steps > 0) multiply_steps<T, A, B, FM, FN, stages>(acc, lds, BM * 4, stage, steps, am, bn, now, fetch);
+        hand_over_narrow<O>(p, acc, reinterpret_cast<f32x4 *>(lds) + stages * stage + wave * 256, w.m0 + wm, w.n0 + wn, tiles.M, w.split);
     }
+    wait_loads<0>();
 }
 
 // ---- few tiles ------------------------------------------------------------------------------------------------------------------
@@ -790,11 +919,10 @@ template <class T> bool few_tiles(const ProductArgs &p, bool chunks)
 template <class T, class O, bool A_TURNED, bool B_TURNED> int launch_chunks(hipStream_t st, const ProductArgs &p)
 {
     if constexpr (std::is_same_v<T, float>) {
-        return launch(st, k_chunks<T, O, 128, 128, 2, 2, 3, false, A_TURNED, B_TURNED>, tile_grid<128, 128>(p), 256, p);
+        return launch(st, k_chunks<T, O, 128, 128, 3, A_TURNED, B_TURNED>, tile_grid<128, 128>(p), 256, p);
     } else {
-        const dim3 grid = tile_grid<256, 256>(p);
-        if (grid.x >= 256) return launch(st, k_chunks<T, O, 256, 256, 2, 4, 1, true, A_TURNED, B_TURNED>, dim3(256), 512, p);
-        return launch(st, k_chunks<T, O, 256, 128, 2, 2, 2, false, A_TURNED, B_TURNED>, tile_grid<256, 128>(p), 256, p);
+        if (tile_grid<256, 256>(p).x >= 256) return launch(st, k_long<T, O, A_TURNED, B_TURNED>, dim3(256), 512, p);
+        return launch(st, k_chunks<T, O, 256, 128, 2, A_TURNED, B_TURNED>, tile_grid<256, 128>(p), 256, p);
     }
 }
 
