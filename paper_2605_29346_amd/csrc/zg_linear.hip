@@ -462,26 +462,31 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 // all but the last n loads of this wavefront are done, and so are its reads of LDS
 template <int n> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(n) : "memory"); }
 
-// One operand's buffer in LDS, 4 `tile` places of 16 bytes, and its way there: 64 places side by side are filled by one instruction of a
+// One operand's buffer in LDS, CH `tile` places of 16 bytes (CH chunks of k a step), and its way there: 64 places side by side are filled by one instruction of a
 // wavefront, each lane's from where it says.
-template <class T, int tile, int waves, bool TURNED> struct Feed;
+template <class T, int tile, int waves, int CH, bool TURNED> struct Feed;
 
-// Along k in memory: place (row i, chunk c) is 4 i + (c ^ i / 4 % 4).  LDS serves 16 lanes of a 16-byte read at a time, 0-3, 12-15, 20-23 and 24-27
+// Along k in memory: place (row i, chunk c) is CH i + (c ^ turn(i)).  LDS serves 16 lanes of a 16-byte read at a time, 0-3, 12-15, 20-23 and 24-27
 // first: at one c those rows lie in 16 different groups of banks, as do the others'.
-template <class T, int tile, int waves> struct Feed<T, tile, waves, false> {
-    static constexpr int K = 16 / (int)sizeof(T), loads = tile * 4 / (64 * waves);
+template <class T, int tile, int waves, int CH> struct Feed<T, tile, waves, CH, false> {
+    static constexpr int K = 16 / (int)sizeof(T), loads = tile * CH / (64 * waves);
+    static_assert(CH == 4 || loads % 4 == 0, "");
     const char *p;
     uint32_t from[loads], chunk;
+
+    __device__ __forceinline__ static uint32_t turn(uint32_t i) { return CH == 4 ? (i >> 2) & 3 : (i ^ (i >> 2)) & 7; }
+    // which chunk a lane has in its lth load: the rows of one load are 64 / CH further on than those of the one before
+    __device__ __forceinline__ uint32_t chunk_at(int l) const { return CH == 4 ? chunk : chunk ^ (2 * l & 7); }
 
     __device__ __forceinline__ void start(const Operand &o, uint32_t first, uint32_t rows, uint32_t wave, uint32_t lane)
     {
         const uint64_t ld = (uint64_t)o.ld * sizeof(T);
         p = static_cast<const char *>(o.p) + first * ld;
+        chunk = (lane % CH) ^ turn(wave * loads * 64 / CH + lane / CH);
 #pragma unroll
         for (int l = 0; l < loads; ++l) {
-            const uint32_t s = (wave * loads + l) * 64 + lane, i = s / 4;
-            chunk = (s & 3) ^ ((s / 16) & 3); // (the same for every l: 64 places are 16 rows)
-            from[l] = first + i < rows ? (uint32_t)(i * ld) + chunk * 16 : kReach;
+            const uint32_t i = (wave * loads + l) * (64 / CH) + lane / CH;
+            from[l] = first + i < rows ? (uint32_t)(i * ld) + chunk_at(l) * 16 : kReach;
         }
     }
     __device__ __forceinline__ __amdgpu_buffer_rsrc_t at(uint32_t k0) const
@@ -491,19 +496,19 @@ template <class T, int tile, int waves> struct Feed<T, tile, waves, false> {
     // the lth of a step's loads, out of at(k0); zeros where there are no more than `left` k from k0 on
     __device__ __forceinline__ void fetch(int l, __amdgpu_buffer_rsrc_t r, uint32_t left, u32x4 *buffer, uint32_t wave) const
     {
-        const uint32_t beyond = (chunk + 1) * K <= left ? 0u : kReach;
+        const uint32_t beyond = (chunk_at(l) + 1) * K <= left ? 0u : kReach;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u32x4 *)(buffer + (wave * loads + l) * 64), 16, (int)(from[l] | beyond), 0, 0, 0);
     }
     // chunk c of row i
     __device__ __forceinline__ static u32x4 chunk_of(const u32x4 *buffer, uint32_t i, uint32_t c)
     {
-        return buffer[4 * i + (c ^ ((i >> 2) & 3))];
+        return buffer[CH * i + (c ^ turn(i))];
     }
 };
 
 // Along the rows in memory: the buffer holds a row of the tile's `tile` rows for each k, and a lane's chunk is put together as it is read.
-template <class T, int tile, int waves> struct Feed<T, tile, waves, true> {
-    static constexpr int K = 16 / (int)sizeof(T), loads = tile * 4 / (64 * waves), row = tile / K; // places of one k
+template <class T, int tile, int waves, int CH> struct Feed<T, tile, waves, CH, true> {
+    static constexpr int K = 16 / (int)sizeof(T), loads = tile * CH / (64 * waves), row = tile / K; // places of one k
     const char *p;
     uint64_t ld;
     uint32_t from[loads], k_of[loads];
@@ -555,84 +560,89 @@ template <class T, int tile, int waves> struct Feed<T, tile, waves, true> {
     }
 };
 
-// One of the two parts of a step: a wavefront's fragments of 32 rows, a chunk of each to a lane.  8 bits: both chunks of a lane in one
-// instruction, the parts are halves of a's fragments and b's are read with the first.
-template <class T, int FM, int FN> struct Part {
+// A part of a step, a pair of chunks of k: a wavefront's fragments of 32 rows, a chunk of each to a lane.  8 bits: four chunks of k, two of them a
+// lane's for one instruction; a part has half of a's fragments, and b's are read with the first half.
+template <class T, int FM, int FN, int CH> struct Part {
     static constexpr bool both = std::is_same_v<T, uint8_t>;
-    static constexpr int fm = both ? FM / 2 : FM, chunks = both ? 2 : 1;
+    static constexpr int fm = both ? FM / 2 : FM, chunks = both ? 2 : 1, parts = CH / 2;
     u32x4 a[fm][chunks], b[FN][chunks];
 
     template <class A, class B> __device__ __forceinline__ void read(int part, const u32x4 *la, const u32x4 *lb, uint32_t am, uint32_t bn, uint32_t half)
     {
 #pragma unroll
         for (int c = 0; c < chunks; ++c) {
-            const uint32_t at = both ? 2 * half + c : 2 * part + half;
-            if (!both || part == 0) {
+            const uint32_t at = both ? 4 * (part / 2) + 2 * half + c : 2 * part + half;
+            if (!both || part % 2 == 0) {
 #pragma unroll
                 for (int j = 0; j < FN; ++j) b[j][c] = B::chunk_of(lb, bn + 32 * j, at);
             }
 #pragma unroll
-            for (int i = 0; i < fm; ++i) a[i][c] = A::chunk_of(la, am + 32 * (both ? part * fm + i : i), at);
+            for (int i = 0; i < fm; ++i) a[i][c] = A::chunk_of(la, am + 32 * (both ? part % 2 * fm + i : i), at);
         }
     }
     // `between(n)` is called behind the nth product, n < fm FN
-    template <int part, class F> __device__ __forceinline__ void multiply_into(f32x16 (&acc)[FM][FN], const Part &with_b, F &&between) const
+    template <class F> __device__ __forceinline__ void multiply_into(int part, f32x16 (&acc)[FM][FN], const Part &with_b, F &&between) const
     {
 #pragma unroll
         for (int i = 0; i < fm; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                if constexpr (both) multiply2(with_b.b[j][0], with_b.b[j][1], a[i][0], a[i][1], acc[part * fm + i][j]);
+                if constexpr (both) multiply2(with_b.b[j][0], with_b.b[j][1], a[i][0], a[i][1], acc[part % 2 * fm + i][j]);
                 else multiply(T(), with_b.b[j][0], a[i][0], acc[i][j]);
                 between(i * FN + j);
             }
     }
 };
 
-// The steps of a tile, one after the other, in two parts each: while the matrix instructions of one part run, the chunks of the next are on their way
-// from LDS.  Between the parts all wavefronts meet: from there on the step's buffer is free - it is asked to be filled with the step that comes
-// `stages` later - and the next step's is full.  The loads go out one by one between the products: together, right behind the meeting, those of
-// all wavefronts queue up and the products wait behind them.  (8 bits: the registers do not hold the next step's first part beside this one's second.)
-template <class T, class A, class B, int FM, int FN, int stages, class Fetch>
+// The steps of a tile, one after the other, in parts: while the matrix instructions of one part run, the chunks of the next are on their way
+// from LDS.  In front of the last part all wavefronts meet: from there on the step's buffer is free - it is asked to be filled with the step that
+// comes `stages` later - and the next step's is full.  The loads go out one by one between the products: together, right behind the meeting, those
+// of all wavefronts queue up and the products wait behind them.  (8 bits: the registers do not hold a step's first part beside another one's b.)
+template <class T, class A, class B, int FM, int FN, int CH, int stages, class Fetch>
 __device__ __forceinline__ void multiply_steps(f32x16 (&acc)[FM][FN], const u32x4 *lds, int lb_at, uint32_t stage, uint32_t steps, uint32_t am, uint32_t bn,
                                                uint32_t &now, Fetch &fetch)
 {
-    constexpr int loads = A::loads + B::loads, products = Part<T, FM, FN>::fm * FN;
-    constexpr bool both = Part<T, FM, FN>::both;
+    using P = Part<T, FM, FN, CH>;
+    constexpr int loads = A::loads + B::loads, products = P::fm * FN, last = P::parts - 1;
     const uint32_t half = (threadIdx.x & 63) >> 5;
-    Part<T, FM, FN> one, two;
-    const auto read = [&](Part<T, FM, FN> &part, int n) {
+    P one, two;
+    const auto read = [&](P &part, int n) {
         const u32x4 *const la = lds + now * stage;
         part.template read<A, B>(n, la, la + lb_at, am, bn, half);
     };
     read(one, 0);
     for (uint32_t t = 0; t < steps; ++t) {
-        read(two, 1);
-        __builtin_amdgcn_sched_barrier(0);
-        one.template multiply_into<0>(acc, one, [](int) {});
-        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < last; ++n) {
+            P &cur = n % 2 ? two : one, &nxt = n % 2 ? one : two;
+            if (!P::both || n % 2 == 0) read(nxt, n + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            cur.multiply_into(n, acc, P::both ? one : cur, [](int) {});
+            __builtin_amdgcn_sched_barrier(0);
+            if (P::both && n % 2) read(nxt, n + 1);
+        }
         // this wavefront's share of the next step is there (what was asked for behind it may be on its way), and it has read this step's chunks
         wait_loads<(stages - 2) * loads>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         now = now == stages - 1 ? 0 : now + 1;
-        if (!both) read(one, 0); // (behind the last step, too: nobody looks at it then)
+        if (!P::both) read(one, 0); // (behind the last step, too: nobody looks at it then)
         __builtin_amdgcn_sched_barrier(0);
         fetch.open();
-        two.template multiply_into<1>(acc, both ? one : two, [&](int n) {
+        two.multiply_into(last, acc, P::both ? one : two, [&](int n) {
 #pragma unroll
             for (int l = 0; l < loads; ++l)
                 if (l * products / loads == n) fetch.load(l);
             __builtin_amdgcn_sched_barrier(0);
         });
         fetch.next();
-        if (both) read(one, 0);
+        if (P::both) read(one, 0);
     }
 }
 
 // What is asked for of both operands, step by step, into one buffer after the other; `on` moves it to the next tile, if there is one.  Where nothing is
 // left it asks for zeros all the same, into buffers that nobody reads: what a wavefront waits for is then the same at every step.
-template <class A, class B, int BM, int stage, int stages, class On> struct Fetch {
+template <class A, class B, int b_at, int step_k, int stage, int stages, class On> struct Fetch {
     A &a;
     B &b;
     u32x4 *lds;
@@ -651,13 +661,13 @@ template <class A, class B, int BM, int stage, int stages, class On> struct Fetc
     {
         u32x4 *const to = lds + into * stage;
         if (l < A::loads) a.fetch(l, ra, left, to, wave);
-        else b.fetch(l - A::loads, rb, left, to + BM * 4, wave);
+        else b.fetch(l - A::loads, rb, left, to + b_at, wave);
     }
     __device__ __forceinline__ void next()
     {
         into = into == stages - 1 ? 0 : into + 1;
         if (left == 0) return;
-        k += 4 * A::K;
+        k += step_k;
         if (k >= k_end) on(*this);
     }
     // the first steps, of which the first is there then
@@ -679,8 +689,8 @@ template <class A, class B, int BM, int stage, int stages, class On> struct Fetc
 // Four wavefronts, two by two, BLOCKS workgroups to a compute unit; three buffers.
 template <class T, class O, int BM, int BN, int BLOCKS, bool A_TURNED, bool B_TURNED> __global__ __launch_bounds__(256, BLOCKS) void k_chunks(ProductArgs p)
 {
-    using A = Feed<T, BM, 4, A_TURNED>;
-    using B = Feed<T, BN, 4, B_TURNED>;
+    using A = Feed<T, BM, 4, 4, A_TURNED>;
+    using B = Feed<T, BN, 4, 4, B_TURNED>;
     constexpr int depth = 4 * A::K, FM = BM / 64, FN = BN / 64, stages = 3, stage = (BM + BN) * 4;
     __shared__ u32x4 lds[stages * stage];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -694,26 +704,26 @@ template <class T, class O, int BM, int BN, int BLOCKS, bool A_TURNED, bool B_TU
     b.start(p.b, w.n0, p.N, wave, lane);
     const uint32_t steps = (w.k_end - w.k_first + depth - 1) / depth;
     const auto no_more = [](auto &) {};
-    Fetch<A, B, BM, stage, stages, decltype(no_more)> fetch{a, b, lds, wave, w.k_first, w.k_end, no_more};
+    Fetch<A, B, BM * 4, depth, stage, stages, decltype(no_more)> fetch{a, b, lds, wave, w.k_first, w.k_end, no_more};
     f32x16 acc[FM][FN] = {};
     uint32_t now = 0;
     if (steps > 0) {
         fetch.begin();
-        multiply_steps<T, A, B, FM, FN, stages>(acc, lds, BM * 4, stage, steps, am, bn, now, fetch);
+        multiply_steps<T, A, B, FM, FN, 4, stages>(acc, lds, BM * 4, stage, steps, am, bn, now, fetch);
         wait_loads<0>();
     }
     __syncthreads(); // the buffers are free
     hand_over<O>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 512, w.m0 + wm, w.n0 + wn, tiles.M, w.split);
 }
 
-// Eight wavefronts, 256 x 256 cells, one workgroup to a compute unit, which takes one tile after the other; four buffers.  The next tile's
+// Eight wavefronts, 256 x 256 cells, one workgroup to a compute unit, which takes one tile after the other; two buffers of eight chunks (128 bytes) of k, or four of four.  The next tile's
 // first steps are on their way while this one's cells are handed over, through LDS of their own.
 template <class T, class O, bool A_TURNED, bool B_TURNED> __global__ __launch_bounds__(512, 2) void k_long(ProductArgs p)
 {
-    constexpr int BM = 256, BN = 256, FM = 4, FN = 2, stages = 4, stage = (BM + BN) * 4;
-    using A = Feed<T, BM, 8, A_TURNED>;
-    using B = Feed<T, BN, 8, B_TURNED>;
-    constexpr int depth = 4 * A::K;
+    constexpr int BM = 256, BN = 256, FM = 4, FN = 2, CH = std::is_same_v<T, uint8_t> ? 4 : 8, stages = CH == 4 ? 4 : 2, stage = (BM + BN) * CH;
+    using A = Feed<T, BM, 8, CH, A_TURNED>;
+    using B = Feed<T, BN, 8, CH, B_TURNED>;
+    constexpr int depth = CH * A::K;
     __shared__ u32x4 lds[stages * stage + 8 * 256];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wm = (wave >> 2) * 128, wn = (wave & 3) * 64, am = wm + (lane & 31), bn = wn + (lane & 31);
@@ -730,7 +740,7 @@ template <class T, class O, bool A_TURNED, bool B_TURNED> __global__ __launch_bo
             return;
         }
     };
-    Fetch<A, B, BM, stage, stages, decltype(on)> fetch{a, b, lds, wave, 0, 0, on};
+    Fetch<A, B, BM * CH, depth, stage, stages, decltype(on)> fetch{a, b, lds, wave, 0, 0, on};
     on(fetch);
     fetch.begin();
     Place w;
@@ -738,7 +748,7 @@ template <class T, class O, bool A_TURNED, bool B_TURNED> __global__ __launch_bo
     while (tiles.take(w)) {
         f32x16 acc[FM][FN] = {};
         const uint32_t steps = (w.k_end - w.k_first + depth - 1) / depth;
-        if (steps > 0) multiply_steps<T, A, B, FM, FN, stages>(acc, lds, BM * 4, stage, steps, am, bn, now, fetch);
+        if (steps > 0) multiply_steps<T, A, B, FM, FN, CH, stages>(acc, lds, BM * CH, stage, steps, am, bn, now, fetch);
         hand_over_narrow<O>(p, acc, reinterpret_cast<f32x4 *>(lds) + stages * stage + wave * 256, w.m0 + wm, w.n0 + wn, tiles.M, w.split);
     }
     wait_loads<0>();
@@ -896,7 +906,7 @@ template <int BM, int BN> dim3 tile_grid(const ProductArgs &p)
 template <class T> bool in_chunks(const Operand &o, uint32_t rows, uint32_t K, int tile)
 {
     const uint64_t ld = (uint64_t)o.ld * sizeof(T), along = (uint64_t)(o.turned ? rows : K) * sizeof(T);
-    const uint64_t span = o.turned ? ld * (64 / sizeof(T)) + tile * sizeof(T) : ld * tile + 64;
+    const uint64_t span = o.turned ? ld * (128 / sizeof(T)) + tile * sizeof(T) : ld * tile + 128;
     return reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && ld % 16 == 0 && along % 16 == 0 && span < kReach;
 }
 
