@@ -597,18 +597,25 @@ template <class T, int FM, int FN, int CH> struct Part {
 // The steps of a tile, one after the other, in parts: while the matrix instructions of one part run, the chunks of the next are on their way
 // from LDS.  In front of the last part all wavefronts meet: from there on the step's buffer is free - it is asked to be filled with the step that
 // comes `stages` later - and the next step's is full.  The loads go out one by one between the products: together, right behind the meeting, those
-// of all wavefronts queue up and the products wait behind them.  (8 bits: the registers do not hold a step's first part beside another one's b.)
+// of all wavefronts queue up and the products wait behind them; half of them behind the next step's first part.  (8 bits: the registers do not hold a step's first part beside another one's b.)
 template <class T, class A, class B, int FM, int FN, int CH, int stages, class Fetch>
 __device__ __forceinline__ void multiply_steps(f32x16 (&acc)[FM][FN], const u32x4 *lds, int lb_at, uint32_t stage, uint32_t steps, uint32_t am, uint32_t bn,
                                                uint32_t &now, Fetch &fetch)
 {
     using P = Part<T, FM, FN, CH>;
-    constexpr int loads = A::loads + B::loads, products = P::fm * FN, last = P::parts - 1;
+    constexpr int loads = A::loads + B::loads, half_of = loads / 2, products = P::fm * FN, last = P::parts - 1;
     const uint32_t half = (threadIdx.x & 63) >> 5;
     P one, two;
     const auto read = [&](P &part, int n) {
         const u32x4 *const la = lds + now * stage;
         part.template read<A, B>(n, la, la + lb_at, am, bn, half);
+    };
+    // loads first .. end - 1, evenly behind the products of a part
+    const auto spread = [&](int m, int first, int end) {
+#pragma unroll
+        for (int l = 0; l < loads; ++l)
+            if (l >= first && l < end && (l - first) * products / (end - first) == m) fetch.load(l);
+        __builtin_amdgcn_sched_barrier(0);
     };
     read(one, 0);
     for (uint32_t t = 0; t < steps; ++t) {
@@ -617,8 +624,11 @@ __device__ __forceinline__ void multiply_steps(f32x16 (&acc)[FM][FN], const u32x
             P &cur = n % 2 ? two : one, &nxt = n % 2 ? one : two;
             if (!P::both || n % 2 == 0) read(nxt, n + 1);
             __builtin_amdgcn_sched_barrier(0);
-            cur.multiply_into(n, acc, P::both ? one : cur, [](int) {});
+            cur.multiply_into(n, acc, P::both ? one : cur, [&](int m) {
+                if (n == 0) spread(m, half_of, loads);
+            });
             __builtin_amdgcn_sched_barrier(0);
+            if (n == 0) fetch.next();
             if (P::both && n % 2) read(nxt, n + 1);
         }
         // this wavefront's share of the next step is there (what was asked for behind it may be on its way), and it has read this step's chunks
@@ -629,13 +639,7 @@ __device__ __forceinline__ void multiply_steps(f32x16 (&acc)[FM][FN], const u32x
         if (!P::both) read(one, 0); // (behind the last step, too: nobody looks at it then)
         __builtin_amdgcn_sched_barrier(0);
         fetch.open();
-        two.multiply_into(last, acc, P::both ? one : two, [&](int n) {
-#pragma unroll
-            for (int l = 0; l < loads; ++l)
-                if (l * products / loads == n) fetch.load(l);
-            __builtin_amdgcn_sched_barrier(0);
-        });
-        fetch.next();
+        two.multiply_into(last, acc, P::both ? one : two, [&](int m) { spread(m, 0, half_of); });
         if (P::both) read(one, 0);
     }
 }
@@ -670,17 +674,18 @@ template <class A, class B, int b_at, int step_k, int stage, int stages, class O
         k += step_k;
         if (k >= k_end) on(*this);
     }
-    // the first steps, of which the first is there then
+    // the first steps, but for half of the last one's loads; the first is there then
     __device__ __forceinline__ void begin()
     {
+        constexpr int loads = A::loads + B::loads;
 #pragma unroll
         for (int i = 0; i < stages; ++i) {
             open();
 #pragma unroll
-            for (int l = 0; l < A::loads + B::loads; ++l) load(l);
-            next();
+            for (int l = 0; l < (i + 1 < stages ? loads : loads / 2); ++l) load(l);
+            if (i + 1 < stages) next();
         }
-        wait_loads<(stages - 1) * (A::loads + B::loads)>();
+        wait_loads<(stages - 2) * loads + loads / 2>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     }
