@@ -177,13 +177,27 @@ template <class T> __device__ __forceinline__ void load8(const T *p, int n, floa
     }
 }
 
-template <class T> __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])
+// 16 bytes past the caches, at any alignment
+typedef uint32_t u32x4_anywhere __attribute__((ext_vector_type(4), aligned(1)));
+
+// Results above this size go past the caches (the eight L2s hold 32 MB): norm of 120001 x 1024 bf16 209 -> 161 us, dropout of 285127 x 512
+// 129 -> 102 us.
+constexpr int64_t kStreamBytes = 32 << 20;
+
+template <class T> __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8], bool stream = false)
 {
     T t[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) t[i] = (T)v[i];
     if (n >= 8) {
-        __builtin_memcpy(p, t, sizeof t);
+        if (stream) {
+            u32x4_anywhere w[sizeof t / 16];
+            __builtin_memcpy(w, t, sizeof t);
+#pragma unroll
+            for (unsigned i = 0; i < sizeof t / 16; ++i) __builtin_nontemporal_store(w[i], reinterpret_cast<u32x4_anywhere *>(p) + i);
+        } else {
+            __builtin_memcpy(p, t, sizeof t);
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -199,11 +213,11 @@ __device__ __forceinline__ void load8(const void *p, int32_t type, int64_t at, i
     else load8(static_cast<const __bf16 *>(p) + at, n, v);
 }
 
-__device__ __forceinline__ void store8(void *p, int32_t type, int64_t at, int n, const float (&v)[8])
+__device__ __forceinline__ void store8(void *p, int32_t type, int64_t at, int n, const float (&v)[8], bool stream = false)
 {
-    if (type == ZG_F32) store8(static_cast<float *>(p) + at, n, v);
-    else if (type == ZG_F16) store8(static_cast<_Float16 *>(p) + at, n, v);
-    else store8(static_cast<__bf16 *>(p) + at, n, v);
+    if (type == ZG_F32) store8(static_cast<float *>(p) + at, n, v, stream);
+    else if (type == ZG_F16) store8(static_cast<_Float16 *>(p) + at, n, v, stream);
+    else store8(static_cast<__bf16 *>(p) + at, n, v, stream);
 }
 
 // ---- activations, fp32 ----------------------------------------------------------------------------------------------------------

@@ -20,39 +20,53 @@ struct Epilogue {
     int64_t ld_R;
     void *Y, *Z;
     int64_t ld_Y, ld_Z;
+    bool stream;  // Y and Z go past the caches
     int64_t part; // elements between the parts of a sum that is made in parts (all else is left out then)
 };
 
 struct AnyType {}; // the type of R, Y and Z is looked up in the epilogue
 
+// eight elements as they lie in memory (16 bits: two to a register)
 template <class O> struct Eight {
-    O t[8];
-};
-template <> struct Eight<AnyType> {
-    float t[8];
+    using E = std::conditional_t<std::is_same_v<O, AnyType>, float, O>;
+    uint32_t w[2 * sizeof(E)];
+
+    __device__ __forceinline__ float at(int j) const
+    {
+        if constexpr (sizeof(E) == 4) return __builtin_bit_cast(float, w[j]);
+        else return (float)__builtin_bit_cast(E, (uint16_t)(j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu));
+    }
 };
 
 template <class O> __device__ __forceinline__ Eight<O> get8(const void *p, int32_t type, int64_t at, int n)
 {
     Eight<O> r;
     if constexpr (std::is_same_v<O, AnyType>) {
-        load8(p, type, at, n, r.t);
+        float v[8];
+        load8(p, type, at, n, v);
+        __builtin_memcpy(r.w, v, sizeof v);
     } else {
         const O *from = static_cast<const O *>(p) + at;
         if (n >= 8) {
-            __builtin_memcpy(r.t, from, sizeof r.t);
+            __builtin_memcpy(r.w, from, sizeof r.w);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) r.t[j] = j < n ? from[j] : (O)0.0f;
+            for (auto &w : r.w) w = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (j >= n) continue;
+                if constexpr (sizeof(O) == 4) r.w[j] = __builtin_bit_cast(uint32_t, from[j]);
+                else r.w[j / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, from[j]) << (j & 1 ? 16 : 0);
+            }
         }
     }
     return r;
 }
 
-template <class O> __device__ __forceinline__ void put8(void *p, int32_t type, int64_t at, int n, const float (&v)[8])
+template <class O> __device__ __forceinline__ void put8(void *p, int32_t type, int64_t at, int n, const float (&v)[8], bool stream)
 {
-    if constexpr (std::is_same_v<O, AnyType>) store8(p, type, at, n, v);
-    else store8(static_cast<O *>(p) + at, n, v);
+    if constexpr (std::is_same_v<O, AnyType>) store8(p, type, at, n, v, stream);
+    else store8(static_cast<O *>(p) + at, n, v, stream);
 }
 
 // what the epilogue has of eight columns, whatever the row
@@ -78,41 +92,58 @@ __device__ __forceinline__ Columns columns_of(const Epilogue &e, uint32_t n, uin
     return c;
 }
 
-// Eight columns of ROWS rows, `step` apart: what the rows need from memory is asked for first, for all of them.
-template <class O, int ROWS, class F> __device__ __forceinline__ void finish(const Epilogue &e, const Columns &c, uint32_t m0, uint32_t step, uint32_t M, F &&sums)
-{
+// Eight columns of ROWS rows, `step` apart: what they need from memory, asked for well before it is used.
+template <class O, int ROWS, bool PLAIN = false> struct Needs {
     Eight<O> r[ROWS];
     uint32_t id[ROWS];
     float scale[ROWS];
+
+    __device__ __forceinline__ void ask(const Epilogue &e, uint32_t n, int left, uint32_t m0, uint32_t step, uint32_t M)
+    {
 #pragma unroll
-    for (int u = 0; u < ROWS; ++u) {
-        const uint32_t m = m0 + u * step;
-        id[u] = m;
-        scale[u] = 1.0f;
-        if (m >= M) continue;
-        if (e.R) r[u] = get8<O>(e.R, e.type, m * e.ld_R + c.n, c.left);
-        if (e.drop.ids) id[u] = (uint32_t)e.drop.ids[m];
-        if (e.scale_m) scale[u] = e.scale_m[m];
+        for (int u = 0; u < ROWS; ++u) {
+            const uint32_t m = m0 + u * step;
+            if (PLAIN) continue;
+            id[u] = m;
+            scale[u] = 1.0f;
+            if (m >= M || left <= 0) continue;
+            if (e.R) r[u] = get8<O>(e.R, e.type, m * e.ld_R + n, left);
+            if (e.drop.ids) id[u] = (uint32_t)e.drop.ids[m];
+            if (e.scale_m) scale[u] = e.scale_m[m];
+        }
     }
+};
+
+// PLAIN: factor and rounding are all there is, as for gradients and parts of sums.
+template <class O, int ROWS, bool PLAIN, class F>
+__device__ __forceinline__ void finish(const Epilogue &e, const Columns &c, const Needs<O, ROWS, PLAIN> &needs, uint32_t m0, uint32_t step, uint32_t M, F &&sums)
+{
+    if (c.left <= 0) return;
 #pragma unroll
     for (int u = 0; u < ROWS; ++u) {
         const uint32_t m = m0 + u * step;
         if (m >= M) continue;
         float v[8];
         sums(u, v);
+        if constexpr (PLAIN) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = fmaf(v[j], scale[u] * c.scale[j], c.bias[j]);
-        if (e.Z) put8<O>(e.Z, e.type, m * e.ld_Z + c.n, c.left, v);
+            for (int j = 0; j < 8; ++j) v[j] *= e.factor;
+            put8<O>(e.Y, e.type, m * e.ld_Y + c.n, c.left, v, e.stream);
+            continue;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = fmaf(v[j], needs.scale[u] * c.scale[j], c.bias[j]);
+        if (e.Z) put8<O>(e.Z, e.type, m * e.ld_Z + c.n, c.left, v, e.stream);
         if (e.act != ZG_ACT_NONE) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = act_of(e.act, v[j]);
         }
-        if (e.drop.cut) mask8(e.drop, id[u], c.n >> 3, e.drop.scale, v);
+        if (e.drop.cut) mask8(e.drop, needs.id[u], c.n >> 3, e.drop.scale, v);
         if (e.R) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += (float)r[u].t[j];
+            for (int j = 0; j < 8; ++j) v[j] += needs.r[u].at(j);
         }
-        put8<O>(e.Y, e.type, m * e.ld_Y + c.n, c.left, v);
+        put8<O>(e.Y, e.type, m * e.ld_Y + c.n, c.left, v, e.stream);
     }
 }
 
@@ -308,51 +339,66 @@ template <class T, int tile, bool TURNED> struct Side {
 // What a wavefront does with its 32 FM x 64 cells' sums.  Of 32 x 32 cells a lane has row lane % 32, columns 8 q + 4 half + 0..3 in registers
 // 4 q + 0..3: they go through LDS (`mine`: 8 KB of the wavefront's own, free from here on), 32 rows at a time, so that eight lanes have 64 columns of a row
 // and memory sees whole lines.  Places are 16 bytes, 16 to a row, turned by the row so that neither way meets in a bank.
-template <class O, int FM> __device__ __forceinline__ void hand_over(const ProductArgs &p, f32x16 (&acc)[FM][2], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t split)
+template <class O, bool PLAIN, int FM> __device__ __forceinline__ void hand_over(const ProductArgs &p, f32x16 (&acc)[FM][2], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t split)
 {
     const uint32_t lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31, g = lane & 7;
     const Columns c = columns_of(p.e, n_wave + 8 * g, p.N);
     Epilogue e = p.e;
     if (split) e.Y = static_cast<float *>(e.Y) + split * e.part;
+    constexpr int ahead = sizeof(Eight<O>) > 16 ? 0 : 1; // (what fits beside the sums)
+    Needs<O, 4, PLAIN> needs[ahead + 1];
+    const auto first = [&](int i) { return m_wave + 32 * i + (lane >> 3); };
+    if (ahead) needs[0].ask(e, c.n, c.left, first(0), 8, M);
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
+        if (i + ahead < FM) needs[(i + ahead) % (ahead + 1)].ask(e, c.n, c.left, first(i + ahead), 8, M);
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 mine[row * 16 + ((8 * j + 2 * q + half) ^ (row & 15))] = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        if (c.left <= 0) continue; // (a wavefront's LDS accesses are in order)
-        finish<O, 4>(e, c, m_wave + 32 * i + (lane >> 3), 8, M, [&](int u, float (&v)[8]) {
+        // (a wavefront's LDS accesses are in order)
+        finish(e, c, needs[i % (ahead + 1)], first(i), 8, M, [&](int u, float (&v)[8]) {
             const uint32_t r = (lane >> 3) + 8 * u;
             const f32x4 lo = mine[r * 16 + ((2 * g) ^ (r & 15))], hi = mine[r * 16 + ((2 * g + 1) ^ (r & 15))];
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = lo[j], v[4 + j] = hi[j];
         });
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
-// The same through 4 KB, 32 x 32 cells at a time: four lanes have 32 columns of a row.
-template <class O, int FM> __device__ __forceinline__ void hand_over_narrow(const ProductArgs &p, f32x16 (&acc)[FM][2], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t split)
+// The same through 4 KB, 32 x 32 cells at a time: four lanes have 32 columns of a row.  What a part needs from memory is asked for
+// ahead.
+template <class O, bool PLAIN, int FM> __device__ __forceinline__ void hand_over_narrow(const ProductArgs &p, f32x16 (&acc)[FM][2], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t split)
 {
+    constexpr int parts = 2 * FM, ahead = sizeof(Eight<O>) > 16 ? 0 : 2; // (what fits beside the sums)
     const uint32_t lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31, g = lane & 3;
     Epilogue e = p.e;
     if (split) e.Y = static_cast<float *>(e.Y) + split * e.part;
+    Columns c;
+    const auto ask = [&](Needs<O, 2, PLAIN> &needs, int n) {
+        const uint32_t col = n_wave + 32 * (n / FM) + 8 * g;
+        needs.ask(e, col, (int)(p.N - col), m_wave + 32 * (n % FM) + (lane >> 2), 16, M);
+    };
+    Needs<O, 2, PLAIN> needs[ahead + 1];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const Columns c = columns_of(p.e, n_wave + 32 * j + 8 * g, p.N);
+    for (int n = 0; n < ahead; ++n) ask(needs[n], n);
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
+    for (int n = 0; n < parts; ++n) {
+        const int i = n % FM, j = n / FM;
+        if (i == 0) c = columns_of(p.e, n_wave + 32 * j + 8 * g, p.N);
+        if (n + ahead < parts) ask(needs[(n + ahead) % (ahead + 1)], n + ahead);
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                mine[row * 8 + ((2 * q + half) ^ ((row >> 1) & 7))] = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-            if (c.left <= 0) continue;
-            finish<O, 2>(e, c, m_wave + 32 * i + (lane >> 2), 16, M, [&](int u, float (&v)[8]) {
-                const uint32_t r = (lane >> 2) + 16 * u;
-                const f32x4 lo = mine[r * 8 + ((2 * g) ^ ((r >> 1) & 7))], hi = mine[r * 8 + ((2 * g + 1) ^ ((r >> 1) & 7))];
+        for (int q = 0; q < 4; ++q)
+            mine[row * 8 + ((2 * q + half) ^ ((row >> 1) & 7))] = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        finish(e, c, needs[n % (ahead + 1)], m_wave + 32 * i + (lane >> 2), 16, M, [&](int u, float (&v)[8]) {
+            const uint32_t r = (lane >> 2) + 16 * u;
+            const f32x4 lo = mine[r * 8 + ((2 * g) ^ ((r >> 1) & 7))], hi = mine[r * 8 + ((2 * g + 1) ^ ((r >> 1) & 7))];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = lo[k], v[4 + k] = hi[k];
-            });
-        }
+            for (int k = 0; k < 4; ++k) v[k] = lo[k], v[4 + k] = hi[k];
+        });
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
@@ -445,7 +491,7 @@ template <class T, int BM, int BN, bool A_TURNED, bool B_TURNED> __global__ __la
         }
         __syncthreads();
     }
-    hand_over<AnyType>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 512, w.m0 + wm, w.n0 + wn, M, w.split);
+    hand_over<AnyType, false>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 512, w.m0 + wm, w.n0 + wn, M, w.split);
 }
 
 // ---- operands in whole chunks ---------------------------------------------------------------------------------------------------
@@ -718,7 +764,7 @@ template <class T, class O, int BM, int BN, int BLOCKS, bool A_TURNED, bool B_TU
         wait_loads<0>();
     }
     __syncthreads(); // the buffers are free
-    hand_over<O>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 512, w.m0 + wm, w.n0 + wn, tiles.M, w.split);
+    hand_over<O, B_TURNED>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 512, w.m0 + wm, w.n0 + wn, tiles.M, w.split);
 }
 
 // Eight wavefronts, 256 x 256 cells, one workgroup to a compute unit, which takes one tile after the other; two buffers of eight chunks (128 bytes) of k, or four of four.  The next tile's
@@ -754,7 +800,7 @@ template <class T, class O, bool A_TURNED, bool B_TURNED> __global__ __launch_bo
         f32x16 acc[FM][FN] = {};
         const uint32_t steps = (w.k_end - w.k_first + depth - 1) / depth;
         if (steps > 0) multiply_steps<T, A, B, FM, FN, CH, stages>(acc, lds, BM * CH, stage, steps, am, bn, now, fetch);
-        hand_over_narrow<O>(p, acc, reinterpret_cast<f32x4 *>(lds) + stages * stage + wave * 256, w.m0 + wm, w.n0 + wn, tiles.M, w.split);
+        hand_over_narrow<O, B_TURNED>(p, acc, reinterpret_cast<f32x4 *>(lds) + stages * stage + wave * 256, w.m0 + wm, w.n0 + wn, tiles.M, w.split);
     }
     wait_loads<0>();
 }
@@ -791,6 +837,8 @@ template <class T> __global__ __launch_bounds__(256) void k_few(ProductArgs p)
     a.k_end = b.k_end = p.K;
     const uint32_t row = threadIdx.x >> 2, group = threadIdx.x & 3; // of the lanes that hand the sums over
     const Columns c = columns_of(p.e, n0 + 8 * group, p.N);
+    Needs<AnyType, 1> needs;
+    if (row < 32) needs.ask(p.e, c.n, c.left, m0 + row, 1, live);
     f32x16 acc = {};
     for (uint32_t k0 = wave * 2 * K; k0 < p.K; k0 += ahead * 8 * K) {
         u32x4 x[ahead], y[ahead];
@@ -808,7 +856,7 @@ template <class T> __global__ __launch_bounds__(256) void k_few(ProductArgs p)
         *reinterpret_cast<f32x4 *>(&lds[wave][(lane & 31) * stride + 8 * q + 4 * half]) = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
     __syncthreads();
     if (row >= 32 || c.left <= 0) return;
-    finish<AnyType, 1>(p.e, c, m0 + row, 1, live, [&](int, float(&v)[8]) {
+    finish(p.e, c, needs, m0 + row, 1, live, [&](int, float(&v)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = 0.0f;
 #pragma unroll
@@ -844,7 +892,10 @@ __global__ __launch_bounds__(256) void k_join(JoinArgs p)
     for (int j = 0; j < 8; ++j) lds[lane][g][j] = v[j];
     __syncthreads();
     if (lane || !there) return;
-    finish<AnyType, 1>(p.e, columns_of(p.e, n, p.N), m, 1, p.M, [&](int, float(&sum)[8]) {
+    const Columns c = columns_of(p.e, n, p.N);
+    Needs<AnyType, 1> needs;
+    needs.ask(p.e, c.n, c.left, m, 1, p.M);
+    finish(p.e, c, needs, m, 1, p.M, [&](int, float(&sum)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
         for (uint32_t s = 0; s < min(p.splits, 32u); ++s)
@@ -936,7 +987,12 @@ template <class T, class O, bool A_TURNED, bool B_TURNED> int launch_chunks(hipS
     if constexpr (std::is_same_v<T, float>) {
         return launch(st, k_chunks<T, O, 128, 128, 3, A_TURNED, B_TURNED>, tile_grid<128, 128>(p), 256, p);
     } else {
-        if (tile_grid<256, 256>(p).x >= 256) return launch(st, k_long<T, O, A_TURNED, B_TURNED>, dim3(256), 512, p);
+        // Two workgroups to a compute unit hide each other's epilogue; one with larger tiles reads less and loses its own.  us with tiles of 256 x 128 /
+        // 256 x 256: bf16 65536 x 1024 x 1024 with nothing but a rounding 177 / 162, with GELU, dropout, residual and Z 281 / 292; 262144 x 256 x 256
+        // 86 / 97; 4096 x 16384 x 4096 615 / 433; 8 bits 65536 x 1024 x 2048 with SiLU 272 / 294; gradients of 65536 x 1024 x 1024 472 / 424.
+        const bool light = p.e.act == ZG_ACT_NONE && !p.e.drop.cut && !p.e.R && !p.e.Z;
+        if (tile_grid<256, 256>(p).x >= 256 && (B_TURNED || p.K * sizeof(T) >= (light ? 2048u : 4096u)))
+            return launch(st, k_long<T, O, A_TURNED, B_TURNED>, dim3(256), 512, p);
         return launch(st, k_chunks<T, O, 256, 128, 2, A_TURNED, B_TURNED>, tile_grid<256, 128>(p), 256, p);
     }
 }
@@ -1078,6 +1134,7 @@ int zg_linear(const zg_linear_args *a, void *stream)
         p.e.factor = 1.0f;
         p.e.scale_m = a->d_scale_A, p.e.scale_n = a->d_scale_W, p.e.bias = a->d_bias;
         p.e.act = a->act, p.e.type = a->out_dtype, p.e.drop = make_drop(a->drop);
+        p.e.stream = a->rows * a->out * (int64_t)type_size(a->out_dtype) > kStreamBytes;
         p.e.R = a->d_R, p.e.ld_R = a->ld_R, p.e.Y = a->d_Y, p.e.ld_Y = a->ld_Y, p.e.Z = a->d_Z, p.e.ld_Z = a->ld_Z;
         return launch_product(static_cast<hipStream_t>(stream), a->dtype, p);
     });
@@ -1148,6 +1205,7 @@ int zg_linear_backward(const zg_linear_grad_args *a, void *d_workspace, size_t w
             p.M = (uint32_t)a->rows, p.N = (uint32_t)a->in, p.K = (uint32_t)a->out;
             p.splits = 1;
             p.e.Y = a->d_dA, p.e.ld_Y = a->ld_dA;
+            p.e.stream = a->rows * a->in * (int64_t)type_size(a->dtype) > kStreamBytes;
             ZG_TRY(launch_product(st, a->dtype, p));
         }
         if (a->d_dW) {
@@ -1157,6 +1215,7 @@ int zg_linear_backward(const zg_linear_grad_args *a, void *d_workspace, size_t w
             p.rows_are_k = 1;
             p.splits = g.splits;
             p.e.Y = a->d_dW, p.e.ld_Y = a->ld_dW;
+            p.e.stream = false;
             ZG_TRY(launch_product(st, a->dtype, p, reinterpret_cast<float *>(ws + g.off_dw)));
         }
         return ZG_OK;

@@ -87,6 +87,70 @@ def test_linear_8bit(size, out_kind):
         R.check(y, want[0], want[1], "y")
 
 
+# enough rows and columns for the large tiles: of operands in whole 16-byte chunks (the two sizes of tiles; widths that end inside a step, inside a
+# tile and inside a lane's eight columns) and of operands that lie anyhow
+LARGE = [(20000, 264, 264, 0, 0), (33000, 72, 520, 8, 0), (17000, 1096, 1032, 0, 0), (9000, 2056, 2049, 8, 0), (33333, 301, 47, 2, 0), (20001, 130, 257, 1, 1)]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", LARGE, ids=str)
+def test_linear_in_large_tiles(size, kind):
+    rows, k, n, pad, shift = size
+    g = _gen(size, str(kind), "large")
+    a, w = _matrix(g, rows, k, kind, pad, shift), _matrix(g, n, k, kind, pad, shift, k**-0.5)
+    bias, r = torch.randn(n, device="cuda", generator=g), _matrix(g, rows, n, kind, pad, shift)
+    mask = (0.3, 12345678901, 7)
+    live = rows - 300
+    dev = torch.tensor([live], dtype=torch.int32, device="cuda")
+    whole_y, y = _buffer(rows, n, kind, pad)
+    whole_z, z = _buffer(rows, n, kind, pad)
+    some = torch.cat((torch.arange(0, 700), torch.arange(live - 700, live)))  # rows of the first and the last tiles, every column
+    want = R.linear(a[some.cuda()], w, bias, r[some.cuda()], "silu", None, kind)
+    layers.linear(a, w, bias=bias, act="silu", residual=r, rows=dev, out=y, preact=z)
+    R.check(z[some.cuda()], want[2], want[3], "z")
+    R.check(y[some.cuda()], want[0], want[1], "y")
+    _untouched(whole_y, live, n, "y")
+    _untouched(whole_z, live, n, "z")
+    # with dropout, and plain: the same cells as small calls on the same rows give
+    ids = torch.arange(rows, dtype=torch.int32, device="cuda")
+    at = slice(live - 256, live)
+    for drop, act in ((mask, "gelu"), (None, "none")):
+        big = layers.linear(a, w, act=act, dropout=layers.Dropout(*drop) if drop else None)
+        small = layers.linear(a[at], w, act=act, dropout=layers.Dropout(*drop, ids[at]) if drop else None)
+        want = R.linear(a[at], w, None, None, act, drop, kind, ids=range(live - 256, live))
+        R.check(big[at], want[0], want[1], f"large {act}")
+        R.check(small, want[0], want[1], f"small {act}")
+
+
+@pytest.mark.parametrize("out_kind", KINDS)
+@pytest.mark.parametrize("size", [(40000, 528, 272), (9000, 4112, 2064), (33000, 80, 520)], ids=str)
+def test_linear_8bit_in_large_tiles(size, out_kind):
+    rows, k, n = size
+    g = _gen(size, str(out_kind), "f8 large")
+    a, w = _matrix(g, rows, k, F8, 0, 0, 60.0), _matrix(g, n, k, F8, 0, 0, 60.0)
+    sa, sw = torch.rand(rows, device="cuda", generator=g) * 0.01 + 1e-4, torch.rand(n, device="cuda", generator=g) * 0.01 + 1e-4
+    y = layers.linear(a, w, act="relu", scale_a=sa, scale_w=sw, out_dtype=out_kind)
+    some = torch.cat((torch.arange(0, 300), torch.arange(rows - 300, rows)))
+    want = R.linear(a[some.cuda()], w, None, None, "relu", None, out_kind, sa[some.cuda()], sw)
+    R.check(y[some.cuda()], want[0], want[1])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", [(20000, 264, 264), (9000, 1032, 2056), (30011, 130, 257)], ids=str)
+def test_linear_gradients_in_large_tiles(size, kind):
+    rows, k, n = size
+    g = _gen(size, str(kind), "large back")
+    a, w, dy, z = _matrix(g, rows, k, kind), _matrix(g, n, k, kind, 0, 0, k**-0.5), _matrix(g, rows, n, kind), _matrix(g, rows, n, kind)
+    for act, mask, live in (("none", None, rows), ("relu", (0.25, 9, 9), rows - 777)):
+        dev = torch.tensor([live], dtype=torch.int32, device="cuda")
+        whole, da = _buffer(rows, k, kind)
+        _, dw, db = layers.linear_backward(dy, a, w, preact=z, act=act, dropout=layers.Dropout(*mask) if mask else None, rows=dev, da=da)
+        grads = R.linear_grads(dy, a, w, z, act, mask, kind, rows=live)
+        for got, (want, bound), what in zip((da[:live], dw, db), grads, ("da", "dw", "dbias")):
+            R.check(got, want, bound, f"{what} {act}")
+        _untouched(whole, live, k, "da")
+
+
 @pytest.mark.parametrize("out_kind", KINDS)
 @pytest.mark.parametrize("kind", KINDS)
 def test_linear_result_in_another_type(kind, out_kind):
