@@ -370,9 +370,9 @@ template <class O, bool PLAIN, int FM> __device__ __forceinline__ void hand_over
 
 // The same through 4 KB, 32 x 32 cells at a time: four lanes have 32 columns of a row.  What a part needs from memory is asked for
 // ahead.
-template <class O, bool PLAIN, int FM> __device__ __forceinline__ void hand_over_narrow(const ProductArgs &p, f32x16 (&acc)[FM][2], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t split)
+template <class O, bool PLAIN, int FM, int FN> __device__ __forceinline__ void hand_over_narrow(const ProductArgs &p, f32x16 (&acc)[FM][FN], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t split)
 {
-    constexpr int parts = 2 * FM, ahead = sizeof(Eight<O>) > 16 ? 0 : 2; // (what fits beside the sums)
+    constexpr int parts = FN * FM, ahead = sizeof(Eight<O>) > 16 ? 0 : 2; // (what fits beside the sums)
     const uint32_t lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31, g = lane & 3;
     Epilogue e = p.e;
     if (split) e.Y = static_cast<float *>(e.Y) + split * e.part;
@@ -383,7 +383,7 @@ template <class O, bool PLAIN, int FM> __device__ __forceinline__ void hand_over
     };
     Needs<O, 2, PLAIN> needs[ahead + 1];
 #pragma unroll
-    for (int n = 0; n < ahead; ++n) ask(needs[n], n);
+    for (int n = 0; n < ahead && n < parts; ++n) ask(needs[n], n);
 #pragma unroll
     for (int n = 0; n < parts; ++n) {
         const int i = n % FM, j = n / FM;
@@ -491,7 +491,8 @@ template <class T, int BM, int BN, bool A_TURNED, bool B_TURNED> __global__ __la
         }
         __syncthreads();
     }
-    hand_over<AnyType, false>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 512, w.m0 + wm, w.n0 + wn, M, w.split);
+    if constexpr (FN == 2) hand_over<AnyType, false>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 512, w.m0 + wm, w.n0 + wn, M, w.split);
+    else hand_over_narrow<AnyType, false>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 256, w.m0 + wm, w.n0 + wn, M, w.split);
 }
 
 // ---- operands in whole chunks ---------------------------------------------------------------------------------------------------
@@ -997,6 +998,18 @@ template <class T, class O, bool A_TURNED, bool B_TURNED> int launch_chunks(hipS
     }
 }
 
+// Operands that lie anyhow, in tiles of tile x tile: the smaller ones where the larger ones would not be two to a compute unit (33333 x 301 x 47 fp16
+// 17.6 -> 11.5 us).
+template <class T, int tile> int launch_anyhow(hipStream_t st, const ProductArgs &p)
+{
+    const dim3 grid = tile_grid<tile, tile>(p);
+    if constexpr (!std::is_same_v<T, Widened8>) {
+        if (p.a.turned) return launch(st, k_product<T, tile, tile, true, true>, grid, 256, p);
+        if (p.b.turned) return launch(st, k_product<T, tile, tile, false, true>, grid, 256, p);
+    }
+    return launch(st, k_product<T, tile, tile, false, false>, grid, 256, p);
+}
+
 // the tiles of one product, or of the parts of one, whose results are of type p.e.type
 template <class T> int launch_tiles(hipStream_t st, const ProductArgs &p)
 {
@@ -1016,16 +1029,8 @@ template <class T> int launch_tiles(hipStream_t st, const ProductArgs &p)
             return launch_chunks<T, __bf16, false, false>(st, p);
         }
     }
-    if constexpr (std::is_same_v<T, uint8_t>) {
-        return launch_tiles<Widened8>(st, p);
-    } else {
-        const dim3 grid = tile_grid<kTile, kTile>(p);
-        if constexpr (!std::is_same_v<T, Widened8>) {
-            if (p.a.turned) return launch(st, k_product<T, kTile, kTile, true, true>, grid, 256, p);
-            if (p.b.turned) return launch(st, k_product<T, kTile, kTile, false, true>, grid, 256, p);
-        }
-        return launch(st, k_product<T, kTile, kTile, false, false>, grid, 256, p);
-    }
+    if constexpr (std::is_same_v<T, uint8_t>) return launch_tiles<Widened8>(st, p);
+    else return tile_grid<kTile, kTile>(p).x < 512 ? launch_anyhow<T, kTile / 2>(st, p) : launch_anyhow<T, kTile>(st, p);
 }
 
 // `part`: room for splits x M x N sums where there are parts
