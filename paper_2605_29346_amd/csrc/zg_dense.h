@@ -41,6 +41,14 @@ template <class... P, class... A> int launch(hipStream_t st, void (*kernel)(P...
     return ZG_OK;
 }
 
+// A launch's lanes in one dimension number less than 2^32: beyond 2^21 workgroups the grid has a second one (with workgroups to spare, which
+// find no rows).
+inline dim3 grid_of(uint64_t blocks)
+{
+    constexpr uint64_t most = 1 << 21;
+    return blocks <= most ? dim3((unsigned)blocks) : dim3((unsigned)most, (unsigned)((blocks + most - 1) / most));
+}
+
 inline int check_rows(int64_t rows)
 {
     return rows < 0 || rows > kMaxRows ? fail(ZG_EINVAL, "rows outside 0..2^31-1") : ZG_OK;
@@ -112,6 +120,9 @@ struct Rows {
 };
 
 #ifdef __HIPCC__
+
+// this workgroup's number in a grid_of()
+__device__ __forceinline__ uint32_t block_number() { return blockIdx.y * gridDim.x + blockIdx.x; }
 
 __device__ __forceinline__ uint64_t mask_product(uint32_t a, uint32_t b)
 {

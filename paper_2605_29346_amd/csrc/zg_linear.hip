@@ -422,7 +422,7 @@ template <int BM, int BN> struct Tiles {
         in_part = (uint64_t)((M + BM - 1) / BM) * nt;
         part_k = __builtin_amdgcn_readfirstlane(((k_all + splits - 1) / splits + depth - 1) / depth * depth);
         const uint64_t tiles = in_part * splits, share = (tiles + 7) / 8;
-        next = blockIdx.x % 8 * share + blockIdx.x / 8;
+        next = blockIdx.x % 8 * share + block_number() / 8; // (a grid's first dimension is a multiple of 8)
         end = min((blockIdx.x % 8 + 1) * share, tiles);
     }
     __device__ __forceinline__ bool take(Place &w)
@@ -829,7 +829,7 @@ template <class T> __global__ __launch_bounds__(256) void k_few(ProductArgs p)
     constexpr int K = chunk_k<T>, ahead = 4, stride = 36; // floats to a row of LDS: rows start in different groups of banks
     __shared__ float lds[4][32 * stride];
     const uint32_t live = min(p.M, p.rows.live()), nt = (p.N + 31) / 32;
-    const uint32_t m0 = blockIdx.x / nt * 32, n0 = blockIdx.x % nt * 32;
+    const uint32_t number = block_number(), m0 = number / nt * 32, n0 = number % nt * 32;
     if (m0 >= live) return;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     Along<T> a, b;
@@ -878,7 +878,7 @@ __global__ __launch_bounds__(256) void k_join(JoinArgs p)
 {
     __shared__ float lds[32][8][8 + 1];
     const uint32_t groups = (p.N + 7) / 8, g = threadIdx.x & 7, lane = threadIdx.x >> 3;
-    const uint64_t i = blockIdx.x * 8ull + g, cells = (uint64_t)p.M * p.N;
+    const uint64_t i = block_number() * 8ull + g, cells = (uint64_t)p.M * p.N;
     const bool there = i < (uint64_t)p.M * groups;
     const uint32_t m = there ? (uint32_t)(i / groups) : 0u, n = there ? (uint32_t)(i % groups) * 8 : 0u;
     float v[8] = {};
@@ -953,15 +953,18 @@ template <class TO, class T> __global__ __launch_bounds__(256) void k_slope(Slop
 
 constexpr int kTile = 128, kTileM = 256, kTileN = 128; // of operands that lie anyhow, and of those in chunks
 
-template <int BM, int BN> dim3 tile_grid(const ProductArgs &p)
+template <int BM, int BN> uint64_t tile_blocks(const ProductArgs &p)
 {
     const uint64_t tiles = (uint64_t)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN) * p.splits;
-    return dim3((unsigned)((tiles + 7) / 8 * 8));
+    return (tiles + 7) / 8 * 8;
 }
 
-// Whether an operand's rows (a tile has `tile` of them) start on 16-byte boundaries, are whole chunks long, and near enough to each other.
-template <class T> bool in_chunks(const Operand &o, uint32_t rows, uint32_t K, int tile)
+template <int BM, int BN> dim3 tile_grid(const ProductArgs &p) { return grid_of(tile_blocks<BM, BN>(p)); }
+
+// Whether an operand's rows start on 16-byte boundaries, are whole chunks long, and near enough to each other.
+template <class T> bool in_chunks(const Operand &o, uint32_t rows, uint32_t K)
 {
+    constexpr int tile = 256; // the largest there is
     const uint64_t ld = (uint64_t)o.ld * sizeof(T), along = (uint64_t)(o.turned ? rows : K) * sizeof(T);
     const uint64_t span = o.turned ? ld * (128 / sizeof(T)) + tile * sizeof(T) : ld * tile + 128;
     return reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && ld % 16 == 0 && along % 16 == 0 && span < kReach;
@@ -992,7 +995,7 @@ template <class T, class O, bool A_TURNED, bool B_TURNED> int launch_chunks(hipS
         // 256 x 256: bf16 65536 x 1024 x 1024 with nothing but a rounding 177 / 162, with GELU, dropout, residual and Z 281 / 292; 262144 x 256 x 256
         // 86 / 97; 4096 x 16384 x 4096 615 / 433; 8 bits 65536 x 1024 x 2048 with SiLU 272 / 294; gradients of 65536 x 1024 x 1024 472 / 424.
         const bool light = p.e.act == ZG_ACT_NONE && !p.e.drop.cut && !p.e.R && !p.e.Z;
-        if (tile_grid<256, 256>(p).x >= 256 && (B_TURNED || p.K * sizeof(T) >= (light ? 2048u : 4096u)))
+        if (tile_blocks<256, 256>(p) >= 256 && (B_TURNED || p.K * sizeof(T) >= (light ? 2048u : 4096u)))
             return launch(st, k_long<T, O, A_TURNED, B_TURNED>, dim3(256), 512, p);
         return launch(st, k_chunks<T, O, 256, 128, 2, A_TURNED, B_TURNED>, tile_grid<256, 128>(p), 256, p);
     }
@@ -1013,10 +1016,10 @@ template <class T, int tile> int launch_anyhow(hipStream_t st, const ProductArgs
 // the tiles of one product, or of the parts of one, whose results are of type p.e.type
 template <class T> int launch_tiles(hipStream_t st, const ProductArgs &p)
 {
-    const bool chunks = in_chunks<T>(p.a, p.M, p.K, kTileM) && in_chunks<T>(p.b, p.N, p.K, kTileN);
+    const bool chunks = in_chunks<T>(p.a, p.M, p.K) && in_chunks<T>(p.b, p.N, p.K);
     if (few_tiles<T>(p, chunks)) {
         using F = std::conditional_t<std::is_same_v<T, uint8_t>, Widened8, T>;
-        return launch(st, k_few<F>, dim3((p.M + 31) / 32 * ((p.N + 31) / 32)), 256, p);
+        return launch(st, k_few<F>, grid_of((uint64_t)((p.M + 31) / 32) * ((p.N + 31) / 32)), 256, p);
     }
     if constexpr (!std::is_same_v<T, Widened8>) {
         if (chunks) {
@@ -1030,7 +1033,7 @@ template <class T> int launch_tiles(hipStream_t st, const ProductArgs &p)
         }
     }
     if constexpr (std::is_same_v<T, uint8_t>) return launch_tiles<Widened8>(st, p);
-    else return tile_grid<kTile, kTile>(p).x < 512 ? launch_anyhow<T, kTile / 2>(st, p) : launch_anyhow<T, kTile>(st, p);
+    else return tile_blocks<kTile, kTile>(p) < 512 ? launch_anyhow<T, kTile / 2>(st, p) : launch_anyhow<T, kTile>(st, p);
 }
 
 // `part`: room for splits x M x N sums where there are parts
@@ -1044,7 +1047,7 @@ template <class T> int launch_product(hipStream_t st, const ProductArgs &p, floa
     q.e.Y = part, q.e.ld_Y = p.N, q.e.part = (int64_t)p.M * p.N;
     ZG_TRY(launch_tiles<T>(st, q));
     const uint64_t groups = (uint64_t)p.M * ((p.N + 7) / 8);
-    return launch(st, k_join, dim3((unsigned)((groups + 7) / 8)), 256, JoinArgs{part, p.M, p.N, p.splits, p.e});
+    return launch(st, k_join, grid_of((groups + 7) / 8), 256, JoinArgs{part, p.M, p.N, p.splits, p.e});
 }
 
 int launch_product(hipStream_t st, int32_t type, const ProductArgs &p, float *part = nullptr)

@@ -27,7 +27,7 @@ struct DropoutArgs {
 template <class T> __global__ __launch_bounds__(kRowsBlock) void k_dropout(DropoutArgs a)
 {
     const uint32_t live = a.rows.live();
-    const uint64_t first = (uint64_t)blockIdx.x * a.per_block;
+    const uint64_t first = (uint64_t)block_number() * a.per_block;
     if (first >= live) return;
     const uint32_t n = (uint32_t)min((uint64_t)a.per_block, live - first) * a.groups;
     for (uint32_t e = threadIdx.x; e < n; e += kRowsBlock) {
@@ -128,7 +128,7 @@ template <class T, int PER, int CH> __global__ __launch_bounds__(PER > kRowsBloc
 {
     __shared__ float lds[16];
     constexpr int block = PER > kRowsBlock ? PER : kRowsBlock;
-    const uint64_t row64 = (uint64_t)blockIdx.x * (block / PER) + threadIdx.x / PER;
+    const uint64_t row64 = (uint64_t)block_number() * (block / PER) + threadIdx.x / PER;
     if (row64 >= a.rows.live()) return; // (whole workgroups where lanes of several wavefronts share a row)
     const uint32_t row = (uint32_t)row64, lane = threadIdx.x % PER;
     float v[CH][8];
@@ -373,7 +373,7 @@ int zg_dropout(const zg_dropout_args *a, void *stream)
         k.x = a->d_x, k.ld_x = a->ld_x, k.r = a->d_r, k.ld_r = a->ld_r, k.y = a->d_y, k.ld_y = a->ld_y;
         k.drop = make_drop(a->drop);
         const uint32_t grid = (uint32_t)((a->rows + k.per_block - 1) / k.per_block);
-        return with_type(a->dtype, [&](auto t) { return launch(static_cast<hipStream_t>(stream), k_dropout<decltype(t)>, dim3(grid), kRowsBlock, k); });
+        return with_type(a->dtype, [&](auto t) { return launch(static_cast<hipStream_t>(stream), k_dropout<decltype(t)>, grid_of(grid), kRowsBlock, k); });
     });
 }
 
@@ -411,7 +411,7 @@ int zg_rms_norm(const zg_norm_args *a, void *stream)
             return with_shape(a->cols, [&](auto per, auto ch) {
                 constexpr int P = decltype(per)::value, block = P > kRowsBlock ? P : kRowsBlock;
                 const uint32_t grid = (uint32_t)((a->rows + block / P - 1) / (block / P));
-                return launch(static_cast<hipStream_t>(stream), k_norm<decltype(t), P, decltype(ch)::value>, dim3(grid), block, k);
+                return launch(static_cast<hipStream_t>(stream), k_norm<decltype(t), P, decltype(ch)::value>, grid_of(grid), block, k);
             });
         });
     });

@@ -507,6 +507,37 @@ def test_many_rows():
     assert torch.equal(layers.dropout(a, layers.Dropout(0.3, 5))[at], layers.dropout(a[at], layers.Dropout(0.3, 5, 0, ids[at])))
 
 
+def test_more_workgroups_than_a_grids_first_dimension_takes():
+    rows, cols = 70_000_003, 8
+    g = _gen("rows")
+    x = torch.empty(rows, cols, device="cuda", dtype=BF16).normal_(generator=g)
+    w = _matrix(g, 8, cols, BF16)
+    at = slice(rows - 5000, rows)
+    for part in (at, slice(0, 5000), slice(67_108_864 - 2500, 67_108_864 + 2500)):
+        assert torch.equal(layers.linear(x, w, act="relu")[part], layers.linear(x[part], w, act="relu"))
+        assert torch.equal(layers.rms_norm(x).y[part], layers.rms_norm(x[part]).y)
+    ids = torch.arange(rows, dtype=torch.int32, device="cuda")
+    assert torch.equal(layers.dropout(x, layers.Dropout(0.3, 5))[at], layers.dropout(x[at], layers.Dropout(0.3, 5, 0, ids[at])))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", [(5, 40, 24), (700, 301, 47), (20000, 264, 264), (9000, 2056, 520)], ids=str)
+def test_a_result_in_the_residuals_place(size, kind):
+    rows, k, n = size
+    g = _gen(size, str(kind), "in place")
+    a, w, r = _matrix(g, rows, k, kind), _matrix(g, n, k, kind, 0, 0, k**-0.5), _matrix(g, rows, n, kind, 8)
+    want = layers.linear(a, w, act="silu", residual=r)
+    whole = torch.full((rows, n + 8), SENTINEL, device="cuda").to(kind)
+    y = whole[:, :n]
+    y.copy_(r)
+    layers.linear(a, w, act="silu", residual=y, out=y)
+    assert torch.equal(y, want) and bool((whole[:, n:] == torch.tensor(SENTINEL, device="cuda").to(kind)).all())
+    x = _matrix(g, rows, n, kind)
+    want = layers.dropout(x, layers.Dropout(0.5, 1), residual=r)
+    y.copy_(r)
+    assert torch.equal(layers.dropout(x, layers.Dropout(0.5, 1), residual=y, out=y), want)
+
+
 def test_same_bits_every_time():
     g = _gen("bits")
     a, w, dy, z = _matrix(g, 5000, 130, F32), _matrix(g, 70, 130, F32), _matrix(g, 5000, 70, F32), _matrix(g, 5000, 70, F32)
