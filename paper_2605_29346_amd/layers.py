@@ -1,10 +1,10 @@
 """Dense operators on the rows of a mini-batch (the last section of include/zg.h): argument marshalling for torch tensors.
 
-`linear`, `dropout` and `rms_norm` with their gradients, and the same as differentiable functions (`Linear`, `DropoutFn`, `RmsNorm`) for
-torch's autograd.  Matrices are 2-D CUDA tensors whose rows are contiguous (`stride(1) == 1`, any `stride(0) >= shape[1]`) of float32,
+`linear`, `dropout` and `rms_norm` with their gradients (`paper_2605_29346_amd.train` puts them together).  Matrices are 2-D CUDA tensors whose rows are contiguous (`stride(1) == 1`, any `stride(0) >= shape[1]`) of float32,
 float16 or bfloat16; `rows` is an int32 CUDA tensor with the number of live rows (e.g. `plan.view_counts()[0][h:h + 1]`): the others are
 neither read nor written, and take no part in any sum.  Outputs that are not given are allocated (rows beyond `rows` stay
-uninitialised).  Work is enqueued on `stream` (default: torch's current one); nothing synchronises."""
+uninitialised).  Work is enqueued on `stream` (default: torch's current one; what another stream is to read has to be there when it gets to
+it); nothing synchronises."""
 from __future__ import annotations
 
 import ctypes as C
