@@ -328,6 +328,15 @@ template <class T, int tile, bool TURNED> struct Side {
     }
 };
 
+// What lanes of a wavefront put into LDS before this, its other lanes read behind it, and what they read before it may be written over behind it.  LDS
+// serves a wavefront in order, so no instruction is needed; it holds the compiler to that order.
+__device__ __forceinline__ void lds_exchange()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // What a wavefront does with its 32 FM x 64 cells' sums.  Of 32 x 32 cells a lane has row lane % 32, columns 8 q + 4 half + 0..3 in registers
 // 4 q + 0..3: they go through LDS (`mine`: 8 KB of the wavefront's own, free from here on), 32 rows at a time, so that eight lanes have 64 columns of a row
 // and memory sees whole lines.  Places are 16 bytes, 16 to a row, turned by the row so that neither way meets in a bank.
@@ -349,13 +358,14 @@ template <class O, bool PLAIN, int FM> __device__ __forceinline__ void hand_over
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 mine[row * 16 + ((8 * j + 2 * q + half) ^ (row & 15))] = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        // (a wavefront's LDS accesses are in order)
+        lds_exchange();
         finish(e, c, needs[i % (ahead + 1)], first(i), 8, M, [&](int u, float (&v)[8]) {
             const uint32_t r = (lane >> 3) + 8 * u;
             const f32x4 lo = mine[r * 16 + ((2 * g) ^ (r & 15))], hi = mine[r * 16 + ((2 * g + 1) ^ (r & 15))];
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = lo[j], v[4 + j] = hi[j];
         });
+        lds_exchange();
         __builtin_amdgcn_sched_barrier(0);
     }
 }
@@ -384,12 +394,14 @@ template <class O, bool PLAIN, int FM, int FN> __device__ __forceinline__ void h
 #pragma unroll
         for (int q = 0; q < 4; ++q)
             mine[row * 8 + ((2 * q + half) ^ ((row >> 1) & 7))] = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        lds_exchange();
         finish(e, c, needs[n % (ahead + 1)], m_wave + 32 * i + (lane >> 2), 16, M, [&](int u, float (&v)[8]) {
             const uint32_t r = (lane >> 2) + 16 * u;
             const f32x4 lo = mine[r * 8 + ((2 * g) ^ ((r >> 1) & 7))], hi = mine[r * 8 + ((2 * g + 1) ^ ((r >> 1) & 7))];
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] = lo[k], v[4 + k] = hi[k];
         });
+        lds_exchange();
         __builtin_amdgcn_sched_barrier(0);
     }
 }
