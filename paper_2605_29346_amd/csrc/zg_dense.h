@@ -232,17 +232,54 @@ __device__ __forceinline__ void store8(void *p, int32_t type, int64_t at, int n,
 }
 
 // ---- activations, fp32 ----------------------------------------------------------------------------------------------------------
-// exp(x) is 2^(x log2 e) in one instruction, 1 / x another.  What the product's rounding does to the power matters where exp(x) is
-// small beside 1, or large: there the functions below do not depend on it.
+// PRECISE, where the result is fp32: right to a few units in the last place of each value, and to z^2 / 2 of them in the normal distribution's
+// tails.  Otherwise, where the result is rounded to 16 bits: exp(x) as 2^(x log2 e) in one instruction, off by |x| 2^-24 of itself, 1 / x in another,
+// and an erf of 1.5e-7.
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
 
-// The normal distribution function and the factor exp(-z^2 / 2) in it: erf by Abramowitz and Stegun 7.1.26 (a polynomial in 1 / (1 + p x) times
-// exp(-x^2), off by at most 1.5e-7), a third of the instructions of the library's erf, which took 136 us of the vector units' time over 67 M cells.
-__device__ __forceinline__ float normal_cdf(float z, float &bell)
+// exp(x + rest), |x| <= 150 and rest of x's rounding: what the power's own rounding leaves out goes into a factor
+__device__ __forceinline__ float exp_precise(float x, float rest = 0.0f)
+{
+    constexpr float high = 1.4426950216293335f, low = 1.925963033500011e-8f; // log2 e
+    const float power = x * high, left = fmaf(rest, high, fmaf(x, low, fmaf(x, high, -power)));
+    return __builtin_amdgcn_exp2f(power) * fmaf(left, 0.69314718f, 1.0f);
+}
+
+template <bool PRECISE> __device__ __forceinline__ float sigmoid(float z)
+{
+    if (!PRECISE) return __builtin_amdgcn_rcpf(1.0f + exp_of(-z));
+    return __builtin_amdgcn_rcpf(1.0f + exp_precise(fminf(fmaxf(-z, -150.0f), 150.0f)));
+}
+
+// The normal distribution function and the factor exp(-z^2 / 2) in it.  With x = |z|, its tail is that factor times erfcx(x / sqrt 2) / 2, a polynomial in
+// u = c x / (1 + c x), c = 0.34, fitted up to x = 14.5 to 2e-8 of itself (u is 0 where x is, so that its rounding does not count there; beyond 14.5
+// the tail is 0 in fp32).
+__device__ __forceinline__ float normal_cdf_precise(float z, float &bell)
+{
+    const float x = fminf(fabsf(z), 14.5f), u = 0.34f * x * __builtin_amdgcn_rcpf(fmaf(0.34f, x, 1.0f)), square = x * x;
+    bell = exp_precise(-0.5f * square, -0.5f * fmaf(x, x, -square));
+    float s = 0.0281659849f;
+    s = fmaf(s, u, -0.103897132f);
+    s = fmaf(s, u, 0.11172124f);
+    s = fmaf(s, u, -0.0112492209f);
+    s = fmaf(s, u, 0.0540692918f);
+    s = fmaf(s, u, -0.163854495f);
+    s = fmaf(s, u, -0.230821952f);
+    s = fmaf(s, u, 0.989227057f);
+    s = fmaf(s, u, -1.17335868f);
+    s = fmaf(s, u, 0.5f);
+    const float tail = s * bell;
+    return z < 0.0f ? tail : 1.0f - tail;
+}
+
+// For 16-bit results: erf by Abramowitz and Stegun 7.1.26 (a polynomial in 1 / (1 + p x) times exp(-x^2)), half the instructions of the one above.
+// z times it is off by 4e-6 of itself for z > -2, 5e-4 from z = -4 on and 4e-3 from -6 on, where it is 6e-9, against 2^-9 and 2^-12 for the
+// rounding to 16 bits (and 3e-8, where fp16 ends).
+__device__ __forceinline__ float normal_cdf(float z)
 {
     const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
-    bell = exp_of(-x * x);
+    const float bell = exp_of(-x * x);
     float s = fmaf(1.061405429f, t, -1.453152027f);
     s = fmaf(s, t, 1.421413741f);
     s = fmaf(s, t, -0.284496736f);
@@ -251,27 +288,28 @@ __device__ __forceinline__ float normal_cdf(float z, float &bell)
     return z < 0.0f ? tail : 1.0f - tail;
 }
 
-__device__ __forceinline__ float act_of(int act, float z)
+template <bool PRECISE> __device__ __forceinline__ float act_of(int act, float z)
 {
     if (act == ZG_ACT_RELU) return z > 0.0f ? z : z != z ? z : 0.0f; // (not a number stays that)
-    if (act == ZG_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + exp_of(-z));
+    if (act == ZG_ACT_SILU) return z * sigmoid<PRECISE>(z);
     if (act == ZG_ACT_GELU) {
         float bell;
-        return z * normal_cdf(z, bell);
+        return z * (PRECISE ? normal_cdf_precise(z, bell) : normal_cdf(z));
     }
     return z;
 }
 
+// precise: a bias' gradient, the sum of slopes, is fp32 whatever the operands are
 __device__ __forceinline__ float act_slope(int act, float z)
 {
     if (act == ZG_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
     if (act == ZG_ACT_SILU) {
-        const float g = __builtin_amdgcn_rcpf(1.0f + exp_of(-z));
+        const float g = sigmoid<true>(z);
         return g * fmaf(z, 1.0f - g, 1.0f);
     }
     if (act == ZG_ACT_GELU) {
         float bell;
-        const float c = normal_cdf(z, bell);
+        const float c = normal_cdf_precise(z, bell);
         return fmaf(z * bell, 0.39894228040143268f, c);
     }
     return 1.0f;
