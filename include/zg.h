@@ -405,7 +405,7 @@ typedef struct {
 } zg_linear_args;
 int zg_linear(const zg_linear_args *a, void *stream);
 
-/* Gradients of zg_linear: with dZ = drop(dY) act'(Z),  dA = dZ W,  dW = dZ^T A,  dbias = sum of dZ over the rows (dR is dY itself).
+/* Gradients of zg_linear: with dZ = drop(dY act'(Z)) (a dropped cell's is 0 whatever dY and Z are there),  dA = dZ W,  dW = dZ^T A,  dbias = sum of dZ over the rows (dR is dY itself).
  * dtype is the type of A, W, dA and dW, out_dtype that of dY and Z; Z may be NULL where act is ZG_ACT_NONE.  d_dA, d_dW and d_dbias
  * may be NULL: that gradient is not wanted (d_W is not needed without d_dA, d_A not without d_dW).  dZ is held in `dtype` (the
  * products' operand; exact where the slope is 0 or 1, as of ZG_ACT_NONE and ZG_ACT_RELU: dropout's factor is applied behind the

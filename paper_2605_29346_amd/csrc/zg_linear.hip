@@ -951,13 +951,13 @@ template <class TO, class T> __global__ __launch_bounds__(256) void k_slope(Slop
     for (uint64_t r = (uint64_t)blockIdx.y * in_block + mine; r < live && left > 0; r += (uint64_t)gridDim.y * in_block) {
         float v[8];
         load8(static_cast<const TO *>(a.dy) + r * a.ld_dy + 8 * g, left, v);
-        if (a.drop.cut) mask8(a.drop, mask_id(a.drop, (uint32_t)r), g, 1.0f, v);
         if (a.act != ZG_ACT_NONE) {
             float z[8];
             load8(static_cast<const TO *>(a.z) + r * a.ld_z + 8 * g, left, z);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] *= act_slope(a.act, z[j]);
         }
+        if (a.drop.cut) mask8(a.drop, mask_id(a.drop, (uint32_t)r), g, 1.0f, v); // (behind the slope: a dropped cell's may be anything)
 #pragma unroll
         for (int j = 0; j < 8; ++j) sums[j] += v[j];
         if (a.dz) store8(static_cast<T *>(a.dz) + r * a.ld_dz + 8 * g, left, v);
