@@ -49,6 +49,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
     sid = source_id()
     flags = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+             "-mllvm", "-pragma-unroll-threshold=65536",  # (loops over sums that live in registers: one that is given up puts them into memory)
              "-ffp-contract=off", "-Wall", "-Wno-unused-function", f'-DZG_BUILD_ID="{sid}"',
              "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
     with tempfile.TemporaryDirectory() as tmp:

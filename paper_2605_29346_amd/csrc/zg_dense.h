@@ -249,7 +249,7 @@ __device__ __forceinline__ float exp_precise(float x, float rest = 0.0f)
 template <bool PRECISE> __device__ __forceinline__ float sigmoid(float z)
 {
     if (!PRECISE) return __builtin_amdgcn_rcpf(1.0f + exp_of(-z));
-    return __builtin_amdgcn_rcpf(1.0f + exp_precise(fminf(fmaxf(-z, -150.0f), 150.0f)));
+    return __builtin_amdgcn_rcpf(1.0f + exp_precise(__builtin_amdgcn_fmed3f(-z, -150.0f, 150.0f)));
 }
 
 // The normal distribution function and the factor exp(-z^2 / 2) in it.  With x = |z|, its tail is that factor times erfcx(x / sqrt 2) / 2, a polynomial in

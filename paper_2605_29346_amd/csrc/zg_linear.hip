@@ -3,7 +3,6 @@
 
 #include <algorithm>
 #include <tuple>
-#include <utility>
 
 namespace zg {
 
@@ -329,10 +328,6 @@ template <class T, int tile, bool TURNED> struct Side {
     }
 };
 
-// f(0), f(1) .. f(N - 1), the numbers constants: unrolled whatever its size (a loop that is given up leaves sums that it indexes in memory)
-template <class F, int... I> __device__ __forceinline__ void unrolled(F &&f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>()), ...); }
-template <int N, class F> __device__ __forceinline__ void unrolled(F &&f) { unrolled(f, std::make_integer_sequence<int, N>()); }
-
 // What lanes of a wavefront put into LDS before this, its other lanes read behind it, and what they read before it may be written over behind it.  LDS
 // serves a wavefront in order, so no instruction is needed; it holds the compiler to that order.
 __device__ __forceinline__ void lds_exchange()
@@ -355,8 +350,8 @@ template <class O, bool PLAIN, int FM> __device__ __forceinline__ void hand_over
     Needs<O, 4, PLAIN> needs[ahead + 1];
     const auto first = [&](int i) { return m_wave + 32 * i + (lane >> 3); };
     if (ahead) needs[0].ask(e, c.n, c.left, first(0), 8, M);
-    unrolled<FM>([&](auto number) __attribute__((always_inline)) {
-        constexpr int i = decltype(number)::value;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
         if (i + ahead < FM) needs[(i + ahead) % (ahead + 1)].ask(e, c.n, c.left, first(i + ahead), 8, M);
 #pragma unroll
         for (int j = 0; j < 2; ++j)
@@ -372,7 +367,7 @@ template <class O, bool PLAIN, int FM> __device__ __forceinline__ void hand_over
         });
         lds_exchange();
         __builtin_amdgcn_sched_barrier(0);
-    });
+    }
 }
 
 // The same through 4 KB, 32 x 32 cells at a time: four lanes have 32 columns of a row.  What a part needs from memory is asked for
@@ -391,8 +386,9 @@ template <class O, bool PLAIN, int FM, int FN> __device__ __forceinline__ void h
     Needs<O, 2, PLAIN> needs[ahead + 1];
 #pragma unroll
     for (int n = 0; n < ahead && n < parts; ++n) ask(needs[n], n);
-    unrolled<parts>([&](auto number) __attribute__((always_inline)) {
-        constexpr int n = decltype(number)::value, i = n % FM, j = n / FM;
+#pragma unroll
+    for (int n = 0; n < parts; ++n) {
+        const int i = n % FM, j = n / FM;
         if (i == 0) c = columns_of(p.e, n_wave + 32 * j + 8 * g, p.N);
         if (n + ahead < parts) ask(needs[(n + ahead) % (ahead + 1)], n + ahead);
 #pragma unroll
@@ -407,7 +403,7 @@ template <class O, bool PLAIN, int FM, int FN> __device__ __forceinline__ void h
         });
         lds_exchange();
         __builtin_amdgcn_sched_barrier(0);
-    });
+    }
 }
 
 // The tiles of a product, and the parts of their sums.  Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles, those of one row of
