@@ -408,8 +408,9 @@ int zg_linear(const zg_linear_args *a, void *stream);
 /* Gradients of zg_linear: with dZ = drop(dY act'(Z)) (a dropped cell's is 0 whatever dY and Z are there),  dA = dZ W,  dW = dZ^T A,  dbias = sum of dZ over the rows (dR is dY itself).
  * dtype is the type of A, W, dA and dW, out_dtype that of dY and Z; Z may be NULL where act is ZG_ACT_NONE.  d_dA, d_dW and d_dbias
  * may be NULL: that gradient is not wanted (d_W is not needed without d_dA, d_A not without d_dW).  dZ is held in `dtype` (the
- * products' operand; exact where the slope is 0 or 1, as of ZG_ACT_NONE and ZG_ACT_RELU: dropout's factor is applied behind the
- * products), dbias is summed from its fp32 values. */
+ * products' operand), dropout's factor being applied behind the products: that is dY itself where the slope is 0 or 1 (ZG_ACT_NONE and ZG_ACT_RELU) and
+ * out_dtype is dtype, else dZ rounded once.  A ZG_F16 dZ of a wider dY is held beside a power of two that brings the largest finite |dZ| to the top of the
+ * type, so that neither end of its range is met (one more pass over dY and Z).  dbias is summed from dZ's fp32 values. */
 typedef struct {
     int64_t rows;
     const uint32_t *d_rows;

@@ -13,6 +13,7 @@ namespace {
 // What happens to a product's sums: v = factor scale_m scale_n sum, z = v + bias, y = R + drop(act(z)).
 struct Epilogue {
     float factor;
+    const float *power; // null, or a power of two (the device's own) that the sum is multiplied by before all else
     const float *scale_m, *scale_n, *bias;
     int32_t act, type; // type of R, Y and Z
     Drop drop;
@@ -119,12 +120,18 @@ template <class O, int ROWS, bool PLAIN, class F>
 __device__ __forceinline__ void finish(const Epilogue &e, const Columns &c, const Needs<O, ROWS, PLAIN> &needs, uint32_t m0, uint32_t step, uint32_t M, F &&sums)
 {
     if (c.left <= 0) return;
+    constexpr bool gradients = PLAIN || std::is_same_v<O, AnyType>; // (or either)
+    const float power = gradients && e.power ? *e.power : 1.0f;
 #pragma unroll
     for (int u = 0; u < ROWS; ++u) {
         const uint32_t m = m0 + u * step;
         if (m >= M) continue;
         float v[8];
         sums(u, v);
+        if (gradients && e.power) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= power;
+        }
         if constexpr (PLAIN) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] *= e.factor;
@@ -934,28 +941,85 @@ struct SlopeArgs {
     void *dz; // or null: only the sums are wanted
     int64_t ld_dz;
     float *part; // [gridDim.y, cols] or null
+    float *tops; // of holds_power: the largest |dZ| of each workgroup, then the power of two that dZ was divided by
     Drop drop;
 };
+
+// Whether a dZ of type T, made of a dY of type TO, is held as what is left beside a power of two: fp16's range ends at 65504 above and at 2^-24 below, the
+// other types' do not, and the caller of a wider dY may mean either (a mean's gradient over 65536 rows is 2^-16 and less).
+template <class TO, class T> constexpr bool holds_power = std::is_same_v<T, _Float16> && !std::is_same_v<TO, _Float16>;
+
+// eight cells of dZ without dropout's factor
+template <class TO> __device__ __forceinline__ void slopes8(const SlopeArgs &a, uint64_t r, uint32_t g, int left, float (&v)[8])
+{
+    load8(static_cast<const TO *>(a.dy) + r * a.ld_dy + 8 * g, left, v);
+    if (a.act != ZG_ACT_NONE) {
+        float z[8];
+        load8(static_cast<const TO *>(a.z) + r * a.ld_z + 8 * g, left, z);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= act_slope(a.act, z[j]);
+    }
+    if (a.drop.cut) mask8(a.drop, mask_id(a.drop, (uint32_t)r), g, 1.0f, v); // (behind the slope: a dropped cell's may be anything)
+}
+
+__device__ __forceinline__ float block_max(float v, float *lds) // of 256 lanes
+{
+    __syncthreads();
+    lds[threadIdx.x] = v;
+    __syncthreads();
+#pragma unroll
+    for (int n = 128; n > 0; n >>= 1) {
+        if (threadIdx.x < n) lds[threadIdx.x] = fmaxf(lds[threadIdx.x], lds[threadIdx.x + n]);
+        __syncthreads();
+    }
+    return lds[0];
+}
+
+// The largest finite |dZ| of each workgroup, in the grid that k_slope has: 65536 x 1024 of fp32 dY and Z with SiLU 105 us of all gradients' 540.
+template <class TO> __global__ __launch_bounds__(256) void k_slope_top(SlopeArgs a)
+{
+    __shared__ float lds[256];
+    const uint32_t live = a.rows.live(), in_block = 256 / a.lanes, g = blockIdx.x * a.lanes + threadIdx.x % a.lanes;
+    const int left = (int)a.cols - (int)(8 * g);
+    float top = 0.0f;
+    for (uint64_t r = (uint64_t)blockIdx.y * in_block + threadIdx.x / a.lanes; r < live && left > 0; r += (uint64_t)gridDim.y * in_block) {
+        float v[8];
+        slopes8<TO>(a, r, g, left, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fabsf(v[j]) <= 3.402823466e38f ? fmaxf(top, fabsf(v[j])) : top;
+    }
+    top = block_max(top, lds);
+    if (threadIdx.x == 0) a.tops[blockIdx.y * gridDim.x + blockIdx.x] = top;
+}
 
 template <class TO, class T> __global__ __launch_bounds__(256) void k_slope(SlopeArgs a)
 {
     __shared__ float lds[256 * 8];
+    float power = 1.0f;
+    if (holds_power<TO, T> && a.dz) {
+        const uint32_t n = gridDim.x * gridDim.y;
+        float top = 0.0f;
+        for (uint32_t i = threadIdx.x; i < n; i += 256) top = fmaxf(top, a.tops[i]);
+        top = block_max(top, lds);
+        // top 2^e in [2^14, 2^15): the sums of products with other fp16 stay far inside fp32
+        const int e = top > 0.0f ? min(15 - __builtin_amdgcn_frexp_expf(top), 126) : 0;
+        power = ldexpf(1.0f, e);
+        if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) a.tops[n] = ldexpf(1.0f, -e);
+        __syncthreads();
+    }
     const uint32_t live = a.rows.live(), lane = threadIdx.x % a.lanes, in_block = 256 / a.lanes, mine = threadIdx.x / a.lanes;
     const uint32_t g = blockIdx.x * a.lanes + lane;
     const int left = (int)a.cols - (int)(8 * g);
     float sums[8] = {};
     for (uint64_t r = (uint64_t)blockIdx.y * in_block + mine; r < live && left > 0; r += (uint64_t)gridDim.y * in_block) {
         float v[8];
-        load8(static_cast<const TO *>(a.dy) + r * a.ld_dy + 8 * g, left, v);
-        if (a.act != ZG_ACT_NONE) {
-            float z[8];
-            load8(static_cast<const TO *>(a.z) + r * a.ld_z + 8 * g, left, z);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= act_slope(a.act, z[j]);
-        }
-        if (a.drop.cut) mask8(a.drop, mask_id(a.drop, (uint32_t)r), g, 1.0f, v); // (behind the slope: a dropped cell's may be anything)
+        slopes8<TO>(a, r, g, left, v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) sums[j] += v[j];
+        if (holds_power<TO, T>) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= power;
+        }
         if (a.dz) store8(static_cast<T *>(a.dz) + r * a.ld_dz + 8 * g, left, v);
     }
     if (!a.part) return;
@@ -1085,7 +1149,8 @@ struct GradPlan {
     int64_t ld_dz;
     uint32_t lanes, slope_x, slope_y; // of k_slope
     uint32_t splits;   // parts of dW's sum over the rows
-    size_t off_dz, off_part, off_dw, total;
+    bool power;        // dZ is held beside a power of two
+    size_t off_dz, off_tops, off_part, off_dw, total;
 };
 
 GradPlan grad_plan(const zg_linear_grad_args &a)
@@ -1106,6 +1171,8 @@ GradPlan grad_plan(const zg_linear_grad_args &a)
     const int64_t tiles = (int64_t)((a.out + kTileM - 1) / kTileM) * ((a.in + kTileN - 1) / kTileN);
     g.splits = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, (a.rows + 255) / 256));
     if (g.slopes && (a.d_dA || a.d_dW)) g.off_dz = take((size_t)a.rows * g.ld_dz * type_size(a.dtype));
+    g.power = g.slopes && (a.d_dA || a.d_dW) && a.dtype == ZG_F16 && a.out_dtype != ZG_F16;
+    if (g.power) g.off_tops = take(((size_t)g.slope_x * g.slope_y + 1) * sizeof(float));
     if (a.d_dbias) g.off_part = take((size_t)g.slope_y * a.out * sizeof(float));
     if (a.d_dW && g.splits > 1) g.off_dw = take((size_t)g.splits * a.out * a.in * sizeof(float));
     return g;
@@ -1209,8 +1276,10 @@ int zg_linear_backward(const zg_linear_grad_args *a, void *d_workspace, size_t w
             s.dy = a->d_dY, s.ld_dy = a->ld_dY, s.z = a->d_Z, s.ld_z = a->ld_Z;
             s.dz = dz != a->d_dY ? const_cast<void *>(dz) : nullptr, s.ld_dz = ld_dz;
             s.part = a->d_dbias ? reinterpret_cast<float *>(ws + g.off_part) : nullptr;
+            s.tops = g.power ? reinterpret_cast<float *>(ws + g.off_tops) : nullptr;
             s.drop = drop;
             const dim3 grid(g.slope_x, g.slope_y);
+            if (g.power) ZG_TRY(a->out_dtype == ZG_F32 ? launch(st, k_slope_top<float>, grid, 256, s) : launch(st, k_slope_top<__bf16>, grid, 256, s));
             auto from = [&](auto to) {
                 using TO = decltype(to);
                 if (a->dtype == ZG_F32) return launch(st, k_slope<TO, float>, grid, 256, s);
@@ -1225,6 +1294,7 @@ int zg_linear_backward(const zg_linear_grad_args *a, void *d_workspace, size_t w
         ProductArgs p{};
         p.rows = rows;
         p.e.factor = factor;
+        if (g.power && a->rows > 0) p.e.power = reinterpret_cast<const float *>(ws + g.off_tops) + (size_t)g.slope_x * g.slope_y;
         p.e.type = a->dtype;
         if (a->d_dA && a->rows > 0) {
             p.a = {dz, ld_dz, false};
