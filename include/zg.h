@@ -349,9 +349,10 @@ int zg_overflow_clear(zg_plan_t *p, void *stream);
  *    to nearest even.  One rounding more where a gradient of ZG_F16 or ZG_BF16 passes through an activation: see zg_linear_backward.
  *  - The calls enqueue kernels on `stream` (default-priority, under capture or not) and nothing else: no allocation, no memset
  *    node, no synchronisation.  They use the current device.  Results do not depend on the launch: no atomics add them up.
- *  - Outputs must not overlap inputs or each other, except where a call says that one may be the other (same address, same stride).
+ *  - Outputs must not overlap inputs or each other, except where a call says that one may be the other (same address, same stride, same
+ *    type).  Matrices may lie between each other's rows.  What a call does not read does not count.
  *  - Structs start from zero: a field that is not needed is 0 / NULL.
- * Errors: ZG_EINVAL (null pointers, widths, strides, types), ZG_ENOMEM (workspace too small), ZG_EHIP (a launch failed). */
+ * Errors: ZG_EINVAL (null pointers, widths, strides, types, overlaps), ZG_ENOMEM (workspace too small), ZG_EHIP (a launch failed). */
 #define ZG_MAX_WIDTH 32768
 #define ZG_MAX_NORM_WIDTH 16384 /* of zg_rms_norm and its gradients, which hold a row in one workgroup's registers */
 
@@ -455,7 +456,7 @@ int zg_dropout(const zg_dropout_args *a, void *stream);
 
 /* h = drop(x) + r,  rstd = 1 / sqrt(mean over the row of h^2 + eps),  y = h rstd gain.
  * x, r, h: [rows, cols] of type dtype (r NULL: no residual; h NULL: not wanted; h may be r or x); gain: [cols] or NULL (ones);
- * rstd: [rows] or NULL.  y is of type out_dtype; the statistics and y are made from the fp32 sums, not from h as it is rounded.
+ * rstd: [rows] or NULL.  y is of type out_dtype (and may be r or x where h is not); the statistics and y are made from the fp32 sums, not from h as it is rounded.
  * out_dtype = ZG_F8: scale[i] = max over the row of |y| / 448 (1 where that is 0 or not a number) and y holds y / scale to nearest
  * even - the operand of a zg_linear of type ZG_F8, with d_scale_A = scale. */
 typedef struct {
@@ -482,7 +483,7 @@ int zg_rms_norm(const zg_norm_args *a, void *stream);
 /* Gradients of zg_rms_norm (out_dtype = dtype) from dy, h and rstd, and dh, the gradient that reaches h from elsewhere (NULL: none):
  *   dr = dh + rstd (gain dy - h rstd^2 mean over the row of (gain dy h)),  dx = drop(dr),  dgain = sum over the rows of dy h rstd.
  * dr (the gradient of the residual and of h) may be NULL; dx may be NULL where dr is not; without dropout they are the same values.
- * dx or dr may be dh or dy.  dgain may be NULL: then no workspace is needed. */
+ * dx or dr may be dh, dy or h.  dgain may be NULL: then no workspace is needed. */
 typedef struct {
     int64_t rows;
     const uint32_t *d_rows;

@@ -5,6 +5,7 @@
 
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <tuple>
 
 namespace zg {
@@ -85,6 +86,59 @@ inline int check_workspace(const void *p, size_t have, size_t need)
     if (!p || reinterpret_cast<uintptr_t>(p) % 256) return fail(ZG_EINVAL, "the workspace is null or not 256-byte aligned");
     return have < need ? fail(ZG_ENOMEM, "the workspace is smaller than the call needs") : ZG_OK;
 }
+
+// ---- what lies where ------------------------------------------------------------------------------------------------------------
+// Workgroups read and write in no order, so what a call writes must not lie on what it reads; a cell that one lane reads and then writes may be
+// the same one.
+
+struct Span {
+    const char *what;
+    const void *p; // null: nothing is there
+    int64_t rows, pitch, width; // bytes from row to row, bytes of a row
+    int32_t size;               // of an element
+};
+
+inline Span matrix_span(const char *what, const void *p, int64_t rows, int64_t ld, int64_t cols, int32_t type)
+{
+    const int32_t size = (int32_t)type_size(type);
+    return {what, p, rows, rows > 1 ? ld * size : cols * size, cols * size, size};
+}
+
+inline Span vector_span(const char *what, const void *p, int64_t n) { return {what, p, 1, n * 4, n * 4, 4}; }
+
+// Whether a byte of `a` is one of `b`.  Where the rows are not equally far apart and only their ranges meet, the caller's word is taken unless the
+// first rows meet.
+inline bool meet(const Span &a, const Span &b)
+{
+    if (!a.p || !b.p || a.rows == 0 || b.rows == 0) return false;
+    const __int128 d = (__int128) reinterpret_cast<uintptr_t>(b.p) - (__int128) reinterpret_cast<uintptr_t>(a.p); // from a's first byte to b's
+    const auto reach = [](const Span &s) { return (__int128)(s.rows - 1) * s.pitch + s.width; };
+    if (d >= reach(a) || -d >= reach(b)) return false;
+    if (a.rows > 1 && b.rows > 1 && a.pitch != b.pitch) return d < a.width && -d < b.width;
+    const __int128 pitch = a.rows > 1 ? a.pitch : b.pitch;
+    if (a.rows == 1 && b.rows == 1) return true;
+    // row i of a and row i + m of b: m such that b's begins less than a row's width in front of a's, or behind it
+    __int128 q = d / pitch;
+    if (d % pitch < 0) --q;
+    const __int128 behind = d - q * pitch; // of b's first row, from the beginning of row q of a
+    const auto rows_meet = [&](__int128 m) { return m <= b.rows - 1 && -m <= a.rows - 1; };
+    return (behind < a.width && rows_meet(-q)) || (pitch - behind < b.width && rows_meet(-q - 1));
+}
+
+inline bool same_cells(const Span &a, const Span &b) { return a.p == b.p && a.pitch == b.pitch && a.width == b.width && a.size == b.size; }
+
+// `out` lies on none of the first list and, unless cell on cell, on none of the second
+inline int check_apart(const Span &out, std::initializer_list<Span> apart, std::initializer_list<Span> apart_or_same = {})
+{
+    for (const Span &s : apart)
+        if (meet(out, s)) return fail(ZG_EINVAL, std::string(out.what) + " lies on " + s.what);
+    for (const Span &s : apart_or_same)
+        if (meet(out, s) && !same_cells(out, s)) return fail(ZG_EINVAL, std::string(out.what) + " lies on " + s.what + " and is not the same matrix");
+    return ZG_OK;
+}
+
+inline Span ids_span(const zg_drop &d, int64_t rows) { return vector_span("the dropout's d_ids", d.p > 0.0 ? d.d_ids : nullptr, rows); }
+inline Span rows_span(const uint32_t *d_rows) { return vector_span("d_rows", d_rows, 1); }
 
 #define ZG_TRY(call)                                                                                         \
     do {                                                                                                     \

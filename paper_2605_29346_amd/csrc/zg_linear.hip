@@ -1217,8 +1217,15 @@ int zg_linear(const zg_linear_args *a, void *stream)
         ZG_TRY(check_matrix("d_Y", a->d_Y, a->ld_Y, a->out, a->out_dtype));
         if (a->d_R) ZG_TRY(check_matrix("d_R", a->d_R, a->ld_R, a->out, a->out_dtype));
         if (a->d_Z) ZG_TRY(check_matrix("d_Z", a->d_Z, a->ld_Z, a->out, a->out_dtype));
-        if (a->d_Y == a->d_A || a->d_Z == a->d_A || a->d_Z == a->d_Y || (a->d_Z && a->d_Z == a->d_R))
-            return fail(ZG_EINVAL, "an output lies on an input or on the other output");
+        {
+            const Span A = matrix_span("d_A", a->d_A, a->rows, a->ld_A, a->in, a->dtype), W = matrix_span("d_W", a->d_W, a->out, a->ld_W, a->in, a->dtype);
+            const Span R = matrix_span("d_R", a->d_R, a->rows, a->ld_R, a->out, a->out_dtype), Y = matrix_span("d_Y", a->d_Y, a->rows, a->ld_Y, a->out, a->out_dtype);
+            const Span Z = matrix_span("d_Z", a->d_Z, a->rows, a->ld_Z, a->out, a->out_dtype), bias = vector_span("d_bias", a->d_bias, a->out);
+            const Span scale_A = vector_span("d_scale_A", a->d_scale_A, a->rows), scale_W = vector_span("d_scale_W", a->d_scale_W, a->out);
+            const Span ids = ids_span(a->drop, a->rows), count = rows_span(a->d_rows);
+            ZG_TRY(check_apart(Y, {A, W, Z, bias, scale_A, scale_W, ids, count}, {R}));
+            ZG_TRY(check_apart(Z, {A, W, R, bias, scale_A, scale_W, ids, count}));
+        }
         ProductArgs p{};
         p.a = {a->d_A, a->ld_A, false};
         p.b = {a->d_W, a->ld_W, false};
@@ -1262,6 +1269,17 @@ int zg_linear_backward(const zg_linear_grad_args *a, void *d_workspace, size_t w
             if (a->d_dW) ZG_TRY(check_matrix("d_A", a->d_A, a->ld_A, a->in, a->dtype));
         }
         if (a->d_dW) ZG_TRY(check_matrix("d_dW", a->d_dW, a->ld_dW, a->in, a->dtype));
+        {
+            const Span dY = matrix_span("d_dY", a->d_dY, a->rows, a->ld_dY, a->out, a->out_dtype);
+            const Span Z = matrix_span("d_Z", a->act != ZG_ACT_NONE ? a->d_Z : nullptr, a->rows, a->ld_Z, a->out, a->out_dtype);
+            const Span A = matrix_span("d_A", a->d_dW ? a->d_A : nullptr, a->rows, a->ld_A, a->in, a->dtype);
+            const Span W = matrix_span("d_W", a->d_dA ? a->d_W : nullptr, a->out, a->ld_W, a->in, a->dtype);
+            const Span dA = matrix_span("d_dA", a->d_dA, a->rows, a->ld_dA, a->in, a->dtype), dW = matrix_span("d_dW", a->d_dW, a->out, a->ld_dW, a->in, a->dtype);
+            const Span dbias = vector_span("d_dbias", a->d_dbias, a->out), ids = ids_span(a->drop, a->rows), count = rows_span(a->d_rows);
+            ZG_TRY(check_apart(dA, {dY, Z, A, W, ids, count}));
+            ZG_TRY(check_apart(dW, {dY, Z, A, W, ids, count, dA}));
+            ZG_TRY(check_apart(dbias, {dY, Z, A, W, ids, count, dA, dW}));
+        }
         const hipStream_t st = static_cast<hipStream_t>(stream);
         char *const ws = static_cast<char *>(d_workspace);
         const Rows rows{a->d_rows, (uint32_t)a->rows};

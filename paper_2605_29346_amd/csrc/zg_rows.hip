@@ -366,6 +366,8 @@ int zg_dropout(const zg_dropout_args *a, void *stream)
         ZG_TRY(check_matrix("d_x", a->d_x, a->ld_x, a->cols, a->dtype));
         if (a->d_r) ZG_TRY(check_matrix("d_r", a->d_r, a->ld_r, a->cols, a->dtype));
         ZG_TRY(check_matrix("d_y", a->d_y, a->ld_y, a->cols, a->dtype));
+        ZG_TRY(check_apart(matrix_span("d_y", a->d_y, a->rows, a->ld_y, a->cols, a->dtype), {ids_span(a->drop, a->rows), rows_span(a->d_rows)},
+                           {matrix_span("d_x", a->d_x, a->rows, a->ld_x, a->cols, a->dtype), matrix_span("d_r", a->d_r, a->rows, a->ld_r, a->cols, a->dtype)}));
         DropoutArgs k{};
         k.rows = {a->d_rows, (uint32_t)a->rows};
         k.cols = (uint32_t)a->cols;
@@ -400,6 +402,16 @@ int zg_rms_norm(const zg_norm_args *a, void *stream)
         if (a->d_h) ZG_TRY(check_matrix("d_h", a->d_h, a->ld_h, a->cols, a->dtype));
         ZG_TRY(check_matrix("d_y", a->d_y, a->ld_y, a->cols, a->out_dtype));
         if (a->out_dtype == ZG_F8 && !a->d_scale) return fail(ZG_EINVAL, "an 8-bit result needs d_scale");
+        {
+            const Span x = matrix_span("d_x", a->d_x, a->rows, a->ld_x, a->cols, a->dtype), r = matrix_span("d_r", a->d_r, a->rows, a->ld_r, a->cols, a->dtype);
+            const Span h = matrix_span("d_h", a->d_h, a->rows, a->ld_h, a->cols, a->dtype), y = matrix_span("d_y", a->d_y, a->rows, a->ld_y, a->cols, a->out_dtype);
+            const Span gain = vector_span("d_gain", a->d_gain, a->cols), rstd = vector_span("d_rstd", a->d_rstd, a->rows);
+            const Span scale = vector_span("d_scale", a->out_dtype == ZG_F8 ? a->d_scale : nullptr, a->rows), ids = ids_span(a->drop, a->rows), count = rows_span(a->d_rows);
+            ZG_TRY(check_apart(h, {gain, ids, count}, {x, r}));
+            ZG_TRY(check_apart(y, {gain, ids, count, h}, {x, r}));
+            ZG_TRY(check_apart(rstd, {gain, ids, count, h, y, x, r}));
+            ZG_TRY(check_apart(scale, {gain, ids, count, h, y, x, r, rstd}));
+        }
         NormArgs k{};
         k.rows = {a->d_rows, (uint32_t)a->rows};
         k.cols = (uint32_t)a->cols;
@@ -455,6 +467,14 @@ int zg_rms_norm_backward(const zg_norm_grad_args *a, void *d_workspace, size_t w
             if (a->d_dx) ZG_TRY(check_matrix("d_dx", a->d_dx, a->ld_dx, a->cols, a->dtype));
             if (a->d_dr) ZG_TRY(check_matrix("d_dr", a->d_dr, a->ld_dr, a->cols, a->dtype));
             if (!a->d_dx && !a->d_dr) return fail(ZG_EINVAL, "d_dx and d_dr are both null");
+            const Span dy = matrix_span("d_dy", a->d_dy, a->rows, a->ld_dy, a->cols, a->dtype), h = matrix_span("d_h", a->d_h, a->rows, a->ld_h, a->cols, a->dtype);
+            const Span dh = matrix_span("d_dh", a->d_dh, a->rows, a->ld_dh, a->cols, a->dtype), dx = matrix_span("d_dx", a->d_dx, a->rows, a->ld_dx, a->cols, a->dtype);
+            const Span dr = matrix_span("d_dr", a->d_dr, a->rows, a->ld_dr, a->cols, a->dtype), gain = vector_span("d_gain", a->d_gain, a->cols);
+            const Span rstd = vector_span("d_rstd", a->d_rstd, a->rows), ids = ids_span(a->drop, a->rows), count = rows_span(a->d_rows);
+            ZG_TRY(check_apart(dx, {gain, rstd, ids, count}, {dy, h, dh}));
+            ZG_TRY(check_apart(dr, {gain, rstd, ids, count}, {dy, h, dh}));
+            ZG_TRY(a->drop.p > 0.0 ? check_apart(dr, {dx}) : check_apart(dr, {}, {dx})); // (without dropout they are the same values)
+            ZG_TRY(check_apart(vector_span("d_dgain", a->d_dgain, a->cols), {gain, rstd, ids, count, dy, h, dh, dx, dr}));
         }
         const hipStream_t st = static_cast<hipStream_t>(stream);
         NormGradArgs k{};

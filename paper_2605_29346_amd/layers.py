@@ -3,7 +3,7 @@
 `linear`, `dropout` and `rms_norm` with their gradients (`paper_2605_29346_amd.train` puts them together).  Matrices are 2-D CUDA tensors whose rows are contiguous (`stride(1) == 1`, any `stride(0) >= shape[1]`) of float32,
 float16 or bfloat16; `rows` is an int32 CUDA tensor with the number of live rows (e.g. `plan.view_counts()[0][h:h + 1]`): the others are
 neither read nor written, and take no part in any sum.  Outputs that are not given are allocated (rows beyond `rows` stay
-uninitialised).  Work is enqueued on `stream` (default: torch's current one; what another stream is to read has to be there when it gets to
+uninitialised); one that lies on what the call reads is refused, unless it is named below as one that may.  Work is enqueued on `stream` (default: torch's current one; what another stream is to read has to be there when it gets to
 it); nothing synchronises."""
 from __future__ import annotations
 
