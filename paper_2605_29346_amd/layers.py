@@ -4,7 +4,7 @@
 float16 or bfloat16; `rows` is an int32 CUDA tensor with the number of live rows (e.g. `plan.view_counts()[0][h:h + 1]`): the others are
 neither read nor written, and take no part in any sum.  Outputs that are not given are allocated (rows beyond `rows` stay
 uninitialised); one that lies on what the call reads is refused, unless it is named below as one that may.  Work is enqueued on `stream` (default: torch's current one; what another stream is to read has to be there when it gets to
-it); nothing synchronises."""
+it); nothing synchronises.  Autograd does not see the calls: operands that require a gradient are refused where one would be recorded."""
 from __future__ import annotations
 
 import ctypes as C
@@ -120,6 +120,15 @@ def _out_vector(t, what, n, device, made):
 _NONE3 = None, 0, 0
 
 
+def _no_history(*operands):
+    """Refuses operands that autograd would want a gradient of: the results have no history, and it would be lost."""
+    if torch.is_grad_enabled():
+        for t in operands:
+            if t is not None and t.requires_grad:
+                raise ValueError("an operand requires a gradient, which the operators do not record: call them under torch.no_grad() or on detached tensors, "
+                                 "and linear_backward, dropout or rms_norm_backward for the gradients")
+
+
 def _shape(t, what):
     """([rows, cols], device) of the operand that a call goes by"""
     if not t.is_cuda:
@@ -173,6 +182,7 @@ def linear(a, w, *, bias=None, act="none", dropout: Optional[Dropout] = None, re
     """drop(act(a w^T + bias)) + residual.  a: [rows, in], w: [out, in], bias: [out] float32, residual and result: [rows, out] of
     `out_dtype` (default: a's type; bfloat16 for 8-bit operands).  float8_e4m3fn operands may have scales by row (float32 [rows], [out]).
     `save` (or a tensor `preact`) returns (result, a w^T + bias) for `linear_backward`.  `out` may be the residual."""
+    _no_history(a, w, bias, residual, scale_a, scale_w)
     (m, k), device = _shape(a, "a")
     n, dtype = w.shape[0], a.dtype
     kind = out_dtype or (torch.bfloat16 if dtype == torch.float8_e4m3fn else dtype)
@@ -191,6 +201,7 @@ def linear_backward(dy, a, w, *, preact=None, act="none", dropout: Optional[Drop
                     dw=None, dbias=None, stream=None):
     """Gradients (da, dw, dbias) of `linear` for the gradient dy of its result (that of the residual is dy itself); `need` says which
     are wanted, the others are None.  `preact` is what `linear(save=True)` returned; without an activation it is not needed."""
+    _no_history(dy, a, w, preact)
     (m, n), device = _shape(dy, "dy")
     k, dtype, kind = w.shape[1], a.dtype, dy.dtype
     made = []
@@ -207,6 +218,7 @@ def linear_backward(dy, a, w, *, preact=None, act="none", dropout: Optional[Drop
 
 def dropout(x, mask: Optional[Dropout], *, residual=None, rows=None, out=None, stream=None):
     """drop(x) + residual; the gradient of x is the same call on the gradient of the result.  `out` may be x or the residual."""
+    _no_history(x, residual)
     (m, n), device = _shape(x, "x")
     dtype, made = x.dtype, []
     out, y, ld_y = _out(out, "out", m, n, dtype, device, made, x)
@@ -221,6 +233,7 @@ def rms_norm(x, *, gain=None, eps=1e-6, residual=None, dropout: Optional[Dropout
     """h = drop(x) + residual, rstd = 1 / sqrt(mean(h^2) + eps), y = h rstd gain (gain: float32 [cols]).  y is of `out_dtype` (default: x's
     type); with float8_e4m3fn y holds y / scale, scale float32 [rows] the row's largest |y| / 448.  h is written where a residual or
     dropout makes it differ from x (or where a tensor `h` is given; that may be the residual or x)."""
+    _no_history(x, gain, residual)
     (m, n), device = _shape(x, "x")
     dtype = x.dtype
     kind = out_dtype or dtype
@@ -242,6 +255,7 @@ def rms_norm_backward(dy, h, rstd, *, gain=None, dh=None, dropout: Optional[Drop
                       dr=None, dgain=None, stream=None):
     """Gradients (dx, dr, dgain) of `rms_norm` for the gradient dy of its y and dh of its h (None: nothing reaches h from elsewhere).
     dr, the gradient of the residual, is a tensor of its own only with dropout (else dx is both, and None is returned for it)."""
+    _no_history(dy, h, rstd, gain, dh)
     (m, n), device = _shape(dy, "dy")
     dtype = dy.dtype
     made = []
