@@ -1053,7 +1053,7 @@ template <class T> bool in_chunks(const Operand &o, uint32_t rows, uint32_t K)
 }
 
 // Whether cells of 32 x 32 (k_few) take less time than large tiles, both as measured on an MI355X.  A large tile alone takes 9 us and 0.5 us
-// for 64 bytes of k (fp32: 2 us, its instructions' own time), 512 of them at a time; k_few 3 us, 1.65 us for a million chunks out of the
+// for 64 bytes of k (fp32: 2 us, its instructions' own time; 8 bits, widened: 0.8), 512 of them at a time; k_few 3 us, 1.65 us for a million chunks out of the
 // caches (twice that where rows start anywhere) and 1.3 us for a thousand workgroups.  bf16, large tiles / k_few: 1 x 256 x 512 8.1 / 3.0 us,
 // 256 x 2048 x 512 40 / 9.7, 4096 x 256 x 256 13.6 / 6.6, 8192 x 256 x 256 13.8 / 11.7, 16384 x 256 x 256 14.7 / 20, 131072 x 64 x 64
 // 14.5 / 22; rows of 602 bytes, 32768 x 301 x 47, 13.7 / 22.6; fp32 1024 x 1024 x 1024 135 / 41, 262144 x 128 x 32 84 / 45.
@@ -1062,7 +1062,7 @@ template <class T> bool few_tiles(const ProductArgs &p, bool chunks)
     using F = std::conditional_t<std::is_same_v<T, uint8_t>, Widened8, T>;
     if (p.splits > 1 || p.a.turned || p.b.turned) return false;
     const double tiles = std::ceil(p.M / (double)kTileM) * std::ceil(p.N / (double)kTileN), steps = std::ceil(p.K * sizeof(T) / 64.0);
-    const double large = (9.0 + (std::is_same_v<T, float> ? 2.0 : 0.5) * steps) * std::max(1.0, tiles / 512.0);
+    const double large = (9.0 + (std::is_same_v<T, float> ? 2.0 : sizeof(T) == 1 ? 0.8 : 0.5) * steps) * std::max(1.0, tiles / 512.0);
     const double blocks = std::ceil(p.M / 32.0) * std::ceil(p.N / 32.0), read = blocks * 64.0 * p.K / chunk_k<F>;
     const double few = 3.0 + (chunks ? 1.65e-6 : 3.3e-6) * read + 1.3e-3 * blocks;
     return few < large;
