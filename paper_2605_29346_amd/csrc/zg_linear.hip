@@ -792,7 +792,7 @@ template <class T, class O, int BM, int BN, int BLOCKS, bool A_TURNED, bool B_TU
 
 // Eight wavefronts, 256 x 256 cells, one workgroup to a compute unit, which takes one tile after the other; two buffers of eight chunks (128 bytes) of k.  For 16-bit types.  The next tile's
 // first steps are on their way while this one's cells are handed over, through LDS of their own.  Bound by what is between the matrix
-// instructions (they run for half of the time over 1024 terms): bf16 65536 x 1024 x 1024 162 us, 850 TFLOP/s, 4096 x 16384 x 4096 433 us, 1270.
+// instructions (counters: they run for 0.38 to 0.43 of the time over 1024 terms): bf16 65536 x 1024 x 1024 162 us, 850 TFLOP/s, 4096 x 16384 x 4096 433 us, 1270.
 template <class T, class O, bool A_TURNED, bool B_TURNED> __global__ __launch_bounds__(512, 2) void k_long(ProductArgs p)
 {
     constexpr int BM = 256, BN = 256, FM = 4, FN = 2, CH = 8, stages = 2, stage = (BM + BN) * CH;
@@ -832,7 +832,7 @@ template <class T, class O, bool A_TURNED, bool B_TURNED> __global__ __launch_bo
 // ---- few tiles ------------------------------------------------------------------------------------------------------------------
 // Where tiles of the sizes above would leave most of the chip idle, or be mostly empty: a workgroup has 32 x 32 cells, its four wavefronts
 // every fourth pair of chunks of k each, straight from memory into registers; their sums meet in LDS.  Nothing is shared but what the caches
-// hold, and a call lasts little more than one way to memory and back: 1 x 256 x 512 bf16 3 us, 1 x 2048 x 2048 7.1, 512 x 512 x 512 4.5.  Operands
+// hold, and a call lasts little more than one way to memory and back: 1 x 256 x 512 bf16 4 us, 1 x 2048 x 2048 7.1, 512 x 512 x 512 4.5.  Operands
 // lie along k, anyhow.
 template <class T> struct Along {
     static constexpr int K = chunk_k<T>;
@@ -930,7 +930,7 @@ __global__ __launch_bounds__(256) void k_join(JoinArgs p)
 }
 
 // dZ without dropout's factor (dropped cells 0), and the sums of dZ over a workgroup's rows.  A lane has eight columns.  Bound by memory: 65536 x 1024
-// bf16 SiLU with dropout 90 us, 4.5 TB/s; 100000 x 256 fp32 ReLU 54 us, 5.7 TB/s (twice the workgroups: 13 us more for both cases' gradients).
+// bf16 SiLU with dropout 92 us, 4.4 TB/s; 100000 x 256 fp32 ReLU 51 us, 6.0 TB/s (twice the workgroups: 13 us more for both cases' gradients).
 struct SlopeArgs {
     Rows rows;
     uint32_t cols;

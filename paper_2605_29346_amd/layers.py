@@ -1,4 +1,4 @@
-"""Dense operators on the rows of a mini-batch (the last section of include/zg.h): argument marshalling for torch tensors.
+"""Dense operators on the rows of a mini-batch (a section of include/zg.h): argument marshalling for torch tensors.
 
 `linear`, `dropout` and `rms_norm` with their gradients (`paper_2605_29346_amd.train` puts them together).  Matrices are 2-D CUDA tensors whose rows are contiguous (`stride(1) == 1`, any `stride(0) >= shape[1]`) of float32,
 float16 or bfloat16; `rows` is an int32 CUDA tensor with the number of live rows (e.g. `plan.view_counts()[0][h:h + 1]`): the others are
@@ -232,7 +232,7 @@ def rms_norm(x, *, gain=None, eps=1e-6, residual=None, dropout: Optional[Dropout
              rstd=None, scale=None, stream=None) -> NormResult:
     """h = drop(x) + residual, rstd = 1 / sqrt(mean(h^2) + eps), y = h rstd gain (gain: float32 [cols]).  y is of `out_dtype` (default: x's
     type); with float8_e4m3fn y holds y / scale, scale float32 [rows] the row's largest |y| / 448.  h is written where a residual or
-    dropout makes it differ from x (or where a tensor `h` is given; that may be the residual or x)."""
+    dropout makes it differ from x (or where a tensor `h` is given; that may be the residual or x, and so may y be where h is not)."""
     _no_history(x, gain, residual)
     (m, n), device = _shape(x, "x")
     dtype = x.dtype
@@ -254,7 +254,8 @@ def rms_norm(x, *, gain=None, eps=1e-6, residual=None, dropout: Optional[Dropout
 def rms_norm_backward(dy, h, rstd, *, gain=None, dh=None, dropout: Optional[Dropout] = None, rows=None, need_dr=True, need_dgain=True, dx=None,
                       dr=None, dgain=None, stream=None):
     """Gradients (dx, dr, dgain) of `rms_norm` for the gradient dy of its y and dh of its h (None: nothing reaches h from elsewhere).
-    dr, the gradient of the residual, is a tensor of its own only with dropout (else dx is both, and None is returned for it)."""
+    dr, the gradient of the residual, is a tensor of its own only with dropout (else dx is both, and None is returned for it).  dx and dr may
+    be dy, h or dh."""
     _no_history(dy, h, rstd, gain, dh)
     (m, n), device = _shape(dy, "dy")
     dtype = dy.dtype
