@@ -346,7 +346,8 @@ int zg_overflow_clear(zg_plan_t *p, void *stream);
  *    holds it: min(*d_rows, rows) rows are read and written, the others are left alone and take no part in any sum.
  *  - Types: ZG_F32, ZG_F16, ZG_BF16 (and ZG_F8 where it says so).  Vectors (bias, gain, scales, their gradients) and the
  *    norm's statistics are fp32.  Sums, activations and everything in between are fp32; a result is rounded to its type once,
- *    to nearest even.  One rounding more where a gradient of ZG_F16 or ZG_BF16 passes through an activation: see zg_linear_backward.
+ *    to nearest even.  One rounding more where a gradient of ZG_F16 or ZG_BF16 passes through an activation or
+ *    comes from another type: see zg_linear_backward.
  *  - The calls enqueue kernels on `stream` (default-priority, under capture or not) and nothing else: no allocation, no memset
  *    node, no synchronisation.  They use the current device.  Results do not depend on the launch: no atomics add them up.
  *  - Outputs must not overlap inputs or each other, except where a call says that one may be the other (same address, same stride, same
