@@ -508,6 +508,66 @@ typedef struct {
 int zg_rms_norm_backward_workspace(const zg_norm_grad_args *a, size_t *bytes);
 int zg_rms_norm_backward(const zg_norm_grad_args *a, void *d_workspace, size_t workspace_bytes, void *stream);
 
+/* ---- what closes a training step ------------------------------------------------------------------
+ * The loss of a linear layer over many classes with its gradients, and the update of a layer's weights.  The conventions of the dense operators above hold here, too. */
+#define ZG_MAX_CLASSES (1 << 24)
+
+/* Softmax cross entropy of the logits Z = A W^T + bias, which are not kept:
+ *   lse[i] = log sum over c of exp(Z[i,c]),   row_loss[i] = lse[i] - Z[i, label[i]],   total = sum of weight[i],   loss = (sum of weight[i] row_loss[i]) / total,
+ * the sums over the rows that count: those with a label in 0..out-1 (any other value: the row has none, its row_loss is 0) and a weight that is not 0.  loss = 0 where no row counts.
+ * A: [rows, in], W: [out, in] of type dtype; bias: [out] or NULL (-infinity takes a class out); labels: [rows] of type label_dtype (ZG_I32 or ZG_I64); weight: [rows] or
+ * NULL (ones).  out <= ZG_MAX_CLASSES.  Logits and all that is made of them are fp32 whatever dtype is, the sums over the rows 64 bits.  A row whose logits hold a NaN or +infinity, or
+ * nothing but -infinity, has the NaN or infinity that the formula gives, and so has the loss if the row counts.  lse (what the gradients need of this pass) is written for every live row. */
+typedef struct {
+    int64_t rows;
+    const uint32_t *d_rows;
+    int32_t in, out;
+    int32_t dtype, label_dtype;
+    const void *d_A;
+    int64_t ld_A;
+    const void *d_W;
+    int64_t ld_W;
+    const float *d_bias;
+    const void *d_labels;
+    const float *d_weight;
+    float *d_loss;     /* [1] */
+    float *d_total;    /* [1] or NULL */
+    float *d_lse;      /* [rows] */
+    float *d_row_loss; /* [rows] or NULL */
+} zg_linear_cross_entropy_args;
+/* Workspace bytes of the call with this very struct (8 bytes for 32 or 64 logits, and copies of operands whose rows are not whole multiples of 16 bytes where the product is large).  Host only. */
+int zg_linear_cross_entropy_workspace(const zg_linear_cross_entropy_args *a, size_t *bytes);
+int zg_linear_cross_entropy(const zg_linear_cross_entropy_args *a, void *d_workspace, size_t workspace_bytes, void *stream);
+
+/* Gradients of zg_linear_cross_entropy's loss: with dZ[i,c] = g weight[i] / total (exp(Z[i,c] - lse[i]) - [c = label[i]]) for the rows that count, 0 for the others,
+ *   dA = dZ W,  dW = dZ^T A,  dbias = sum of dZ over the rows.
+ * g = *d_dloss (NULL: 1), total = *d_total (NULL: 1, the gradients of the sum; 0: all gradients are 0).  d_dA, d_dW and d_dbias may be NULL.  The logits are made again,
+ * a piece of the classes at a time; dZ is held in dtype (rounded once, the products' operand), without g / total, which is applied behind the sums, and for ZG_F16 beside a power of two that
+ * brings the largest |weight| to the top of the type.  dbias is summed from dZ's fp32 values.  A row that does not count is still an operand of dW (as a zero times what A holds there). */
+typedef struct {
+    int64_t rows;
+    const uint32_t *d_rows;
+    int32_t in, out;
+    int32_t dtype, label_dtype;
+    const void *d_A;
+    int64_t ld_A;
+    const void *d_W;
+    int64_t ld_W;
+    const float *d_bias;
+    const void *d_labels;
+    const float *d_weight;
+    const float *d_lse;
+    const float *d_total;
+    const float *d_dloss;
+    void *d_dA;
+    int64_t ld_dA;
+    void *d_dW;
+    int64_t ld_dW;
+    float *d_dbias;
+} zg_linear_cross_entropy_grad_args;
+int zg_linear_cross_entropy_backward_workspace(const zg_linear_cross_entropy_grad_args *a, size_t *bytes);
+int zg_linear_cross_entropy_backward(const zg_linear_cross_entropy_grad_args *a, void *d_workspace, size_t workspace_bytes, void *stream);
+
 /* ---- measurement helpers ----------------------------------------------------------------------
  * Identifier of the sources the library was built from (a hash the build step passes in); lets a caller
  * detect a stale binary.  Library-owned string. */

@@ -28,6 +28,7 @@ struct JoinArgs {
     const float *part;
     uint32_t M, N, splits;
     Epilogue e;
+    Rows rows; // the device's count bounds M
 };
 
 __global__ __launch_bounds__(256) void k_join(JoinArgs p)
@@ -35,7 +36,7 @@ __global__ __launch_bounds__(256) void k_join(JoinArgs p)
     __shared__ float lds[32][8][8 + 1];
     const uint32_t groups = (p.N + 7) / 8, g = threadIdx.x & 7, lane = threadIdx.x >> 3;
     const uint64_t i = block_number() * 8ull + g, cells = (uint64_t)p.M * p.N;
-    const bool there = i < (uint64_t)p.M * groups;
+    const bool there = i < (uint64_t)min(p.M, p.rows.live()) * groups;
     const uint32_t m = there ? (uint32_t)(i / groups) : 0u, n = there ? (uint32_t)(i % groups) * 8 : 0u;
     float v[8] = {};
     if (there)
@@ -228,8 +229,7 @@ template <class T> int launch_product(hipStream_t st, const ProductArgs &p, floa
     q.e.type = ZG_F32;
     q.e.Y = part, q.e.ld_Y = p.N, q.e.part = (int64_t)p.M * p.N;
     ZG_TRY(launch_tiles<T>(st, q));
-    const uint64_t groups = (uint64_t)p.M * ((p.N + 7) / 8);
-    return launch(st, k_join, grid_of((groups + 7) / 8), 256, JoinArgs{part, p.M, p.N, p.splits, p.e});
+    return dense_join(st, part, p.M, p.N, p.splits, p.e, {nullptr, p.M});
 }
 
 int launch_product(hipStream_t st, int32_t type, const ProductArgs &p, float *part = nullptr)
@@ -289,6 +289,12 @@ int check_linear_grad(const zg_linear_grad_args *a)
 } // namespace
 
 int dense_product(hipStream_t st, int32_t type, const ProductArgs &p, float *part) { return launch_product(st, type, p, part); }
+
+int dense_join(hipStream_t st, const float *part, uint32_t M, uint32_t N, uint32_t splits, const Epilogue &e, Rows rows)
+{
+    const uint64_t groups = (uint64_t)M * ((N + 7) / 8);
+    return launch(st, k_join, grid_of((groups + 7) / 8), 256, JoinArgs{part, M, N, splits, e, rows});
+}
 
 } // namespace zg
 

@@ -1,0 +1,873 @@
+// Softmax cross entropy of a linear layer: the loss over many classes without keeping the logits, and its gradients.
+//
+// z = A W^T + bias.  The product's tiles keep, of every row of their cells, the largest z and the sum of exp(z - largest) - 8 bytes for 32 or 64 logits -, which a
+// second launch joins to lse = log sum exp z.  The gradients make the logits again, a piece of the classes at a time: dZ = f (exp(z - lse) - [class is the label]) leaves the
+// product's tiles in the operands' type, f being the row's weight, and goes into the products dW = dZ^T A and dA += dZ W; what all rows have in common (1 / the sum of weights, and what the
+// loss' own gradient is) is applied behind the sums.
+#include "zg_product.h"
+
+namespace zg {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// what a row counts: its label's class, or kNone
+constexpr uint32_t kNone = 0xFFFFFFFFu;
+
+struct Labels {
+    const void *p;
+    int32_t wide; // int64
+    uint32_t classes;
+    __device__ __forceinline__ uint32_t of(uint64_t m) const
+    {
+        const int64_t l = wide ? static_cast<const int64_t *>(p)[m] : static_cast<const int32_t *>(p)[m];
+        return l >= 0 && l < (int64_t)classes ? (uint32_t)l : kNone;
+    }
+};
+
+// ---- the forward product ----------------------------------------------------------------------------------------------------------
+
+struct Top {
+    float top, sum; // the largest of some logits of a row, and the sum of exp(z - top)
+};
+
+__device__ __forceinline__ float power_of(float v, float top) { return __builtin_amdgcn_exp2f((v - top) * kLog2e); }
+
+// Where all logits are -infinity, they count from 0; not-a-number and +infinity end in a sum that is not a number.
+__device__ __forceinline__ float base_of(float top) { return top == -INFINITY ? 0.0f : top; }
+
+__device__ __forceinline__ Top join(Top a, Top b)
+{
+    const float top = fmaxf(a.top, b.top), base = base_of(top);
+    return {top, a.sum * power_of(a.top, base) + b.sum * power_of(b.top, base)};
+}
+
+struct TopArgs : ProductArgs {
+    Labels labels;
+    Top *part;       // [slot][M], a slot being the columns of a wavefront (or of k_loss_top_few's workgroup)
+    float *at_label; // [M]: the label's logit
+};
+
+// A wavefront's 32 FM x 32 FN cells: half a row's lie side by side in a lane, the other half in the lane 32 further on, so that the row's largest and its sum need one exchange each.
+// For each cell an addition, a maximum, a subtraction, a multiplication, an exponential (four times as long) and an addition; the label's cell is looked for only where one of the
+// wavefront's 32 rows has it among its columns.
+template <int FM, int FN> __device__ __forceinline__ void tops(const TopArgs &p, const f32x16 (&acc)[FM][FN], uint32_t m_wave, uint32_t n_wave, uint32_t M)
+{
+    const uint32_t lane = threadIdx.x & 63, half = lane >> 5;
+    if (n_wave >= p.N) return;
+    const bool whole = n_wave + 32 * FN <= p.N;
+    float bias[FN][16];
+    if (p.e.bias) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t n = n_wave + 32 * j + 8 * q + 4 * half;
+                if (whole) {
+                    __builtin_memcpy(&bias[j][4 * q], p.e.bias + n, 16);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) bias[j][4 * q + r] = n + r < p.N ? p.e.bias[n + r] : 0.0f;
+                }
+            }
+    }
+    Top *const part = p.part + (uint64_t)(n_wave / (32 * FN)) * p.M;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const uint32_t m = m_wave + 32 * i + (lane & 31);
+        const uint32_t at = m < M ? p.labels.of(m) - n_wave : kNone; // (kNone - n_wave is beyond the columns, too: classes < 2^25)
+        float v[FN][16], top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) v[j][r] = acc[i][j][r];
+        if (p.e.bias) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) v[j][r] += bias[j][r];
+        }
+        if (!whole) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (n_wave + 32 * j + 8 * (r / 4) + 4 * half + r % 4 >= p.N) v[j][r] = -INFINITY;
+        }
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, v[j][r]);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float base = base_of(top);
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum += power_of(v[j][r], base);
+        sum += __shfl_xor(sum, 32);
+        if (half == 0 && m < M) part[m] = Top{top, sum};
+        if (__any(at < 32 * FN)) {
+            float z = 0.0f;
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) z = at == 32 * j + 8 * (r / 4) + 4 * half + r % 4 ? v[j][r] : z;
+            if (at < 32 * FN && (at >> 2 & 1) == half) p.at_label[m] = z;
+        }
+    }
+}
+
+template <> struct Out<TopArgs> {
+    template <class O, bool PLAIN, int FM> __device__ __forceinline__ static void wide(const TopArgs &p, f32x16 (&acc)[FM][2], f32x4 *, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t)
+    {
+        tops(p, acc, m_wave, n_wave, M);
+    }
+    template <class O, bool PLAIN, int FM, int FN> __device__ __forceinline__ static void narrow(const TopArgs &p, f32x16 (&acc)[FM][FN], f32x4 *, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t)
+    {
+        tops(p, acc, m_wave, n_wave, M);
+    }
+    struct Few {
+        Columns c;
+        uint32_t label;
+        __device__ __forceinline__ void begin(const TopArgs &p, uint32_t m, uint32_t n, uint32_t live)
+        {
+            c = columns_of(p.e, n, p.N);
+            label = m < live ? p.labels.of(m) : kNone;
+        }
+        template <class F> __device__ __forceinline__ void end(const TopArgs &p, uint32_t m, uint32_t live, F &&sums)
+        {
+            float v[8];
+            sums(0, v);
+            Top t{-INFINITY, 0.0f};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = j < c.left ? v[j] + c.bias[j] : -INFINITY;
+                t.top = fmaxf(t.top, v[j]);
+            }
+            t.top = fmaxf(t.top, __shfl_xor(t.top, 1));
+            t.top = fmaxf(t.top, __shfl_xor(t.top, 2));
+            const float base = base_of(t.top);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t.sum += power_of(v[j], base);
+            t.sum += __shfl_xor(t.sum, 1);
+            t.sum += __shfl_xor(t.sum, 2);
+            if (m >= live) return;
+            if ((threadIdx.x & 3) == 0) p.part[(uint64_t)(c.n / 32) * p.M + m] = t;
+            const uint32_t at = label - c.n;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (at == (uint32_t)j) p.at_label[m] = v[j];
+        }
+    };
+};
+
+template <class T> __global__ __launch_bounds__(256) void k_loss_top_few(TopArgs p) { few_tile<T>(p); }
+template <class T> __global__ __launch_bounds__(256, 2) void k_loss_top_anyhow(TopArgs p) { product_tile<T, 64, 64, false, false>(p); }
+template <class T> __global__ __launch_bounds__(256, 2) void k_loss_top_chunks(TopArgs p) { chunks_tile<T, T, 256, 128, false, false>(p); }
+template <> __global__ __launch_bounds__(256, 3) void k_loss_top_chunks<float>(TopArgs p) { chunks_tile<float, float, 128, 128, false, false>(p); }
+template <class T> __global__ __launch_bounds__(512, 2) void k_loss_top_long(TopArgs p) { long_tiles<T, T, false, false>(p); }
+
+// ---- the rows' losses -------------------------------------------------------------------------------------------------------------
+
+struct RowArgs {
+    Rows rows;
+    uint32_t slots, cap;
+    const Top *part;
+    const float *at_label, *weight;
+    Labels labels;
+    float *lse, *row_loss; // row_loss may be null
+    double *sums;          // [workgroups][2]: of weight x loss, of the weights
+    float *loss, *total;   // total may be null
+};
+
+__device__ __forceinline__ void finish_loss(const RowArgs &a, double loss, double total)
+{
+    *a.loss = total != 0.0 ? (float)(loss / total) : 0.0f;
+    if (a.total) *a.total = (float)total;
+}
+
+// R rows at a time, 256 / R lanes to a row.  Reads what the product's tiles left, 8 bytes for 32 or 64 logits.
+template <int R> __global__ __launch_bounds__(256) void k_loss_rows(RowArgs a)
+{
+    constexpr int G = 256 / R;
+    __shared__ Top lds[256];
+    __shared__ double both[2][R < 64 ? 64 : R];
+    const uint32_t live = a.rows.live(), r = threadIdx.x % R, g = threadIdx.x / R;
+    double loss = 0.0, total = 0.0;
+    for (uint64_t m0 = (uint64_t)blockIdx.x * R; m0 < live; m0 += (uint64_t)gridDim.x * R) {
+        const uint64_t m = m0 + r;
+        Top t{-INFINITY, 0.0f};
+        if (m < live)
+            for (uint32_t s = g; s < a.slots; s += G) t = join(t, a.part[(uint64_t)s * a.cap + m]);
+        if (G > 1) {
+            lds[threadIdx.x] = t;
+            __syncthreads();
+#pragma unroll
+            for (int n = G / 2; n > 0; n >>= 1) {
+                if (g < (uint32_t)n) lds[threadIdx.x] = t = join(t, lds[threadIdx.x + n * R]);
+                __syncthreads();
+            }
+        }
+        if (g == 0 && m < live) {
+            const double lse = (double)t.top + log((double)t.sum);
+            a.lse[m] = (float)lse;
+            const bool has = a.labels.of(m) != kNone;
+            const float w = !has ? 0.0f : a.weight ? a.weight[m] : 1.0f;
+            const float each = has ? (float)(lse - (double)a.at_label[m]) : 0.0f;
+            if (a.row_loss) a.row_loss[m] = each;
+            if (w != 0.0f) {
+                loss += (double)w * (double)each;
+                total += (double)w;
+            }
+        }
+    }
+    __syncthreads();
+    if (g == 0) both[0][r] = loss, both[1][r] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < R; ++i) loss += both[0][i], total += both[1][i];
+        if (gridDim.x == 1) {
+            finish_loss(a, loss, total);
+        } else {
+            a.sums[2 * blockIdx.x] = loss;
+            a.sums[2 * blockIdx.x + 1] = total;
+        }
+    }
+}
+
+__global__ __launch_bounds__(64) void k_loss_mean(RowArgs a, uint32_t n)
+{
+    __shared__ double both[2][64];
+    double loss = 0.0, total = 0.0;
+    for (uint32_t i = threadIdx.x; i < n; i += 64) loss += a.sums[2 * i], total += a.sums[2 * i + 1];
+    both[0][threadIdx.x] = loss, both[1][threadIdx.x] = total;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int i = 1; i < 64; ++i) loss += both[0][i], total += both[1][i];
+    finish_loss(a, loss, total);
+}
+
+// ---- dZ ---------------------------------------------------------------------------------------------------------------------------
+
+// what dZ's cells need of their row
+struct RowFactor {
+    float lse, factor; // factor 0: no gradient, whatever the logits are
+    uint32_t label, reserved;
+};
+
+struct FactorArgs {
+    Rows rows;
+    const float *lse, *weight, *total, *dloss; // all but lse may be null
+    Labels labels;
+    const float *tops; // null, or the largest |weight| of each of `n_tops` workgroups
+    uint32_t n_tops;
+    float up;          // a power of two that dZ is held with
+    RowFactor *row;
+    float *power;      // what the products' sums are multiplied by
+};
+
+constexpr uint32_t kWeightBlocks = 64;
+
+// the largest finite |weight| among the rows that count
+__global__ __launch_bounds__(256) void k_loss_weight_top(FactorArgs a, float *tops)
+{
+    __shared__ float lds[256];
+    float top = 0.0f;
+    const uint32_t live = a.rows.live();
+    for (uint64_t m = blockIdx.x * 256ull + threadIdx.x; m < live; m += 256ull * gridDim.x) {
+        const float w = fabsf(a.weight[m]);
+        if (a.labels.of(m) != kNone && w <= 3.402823466e38f) top = fmaxf(top, w);
+    }
+    lds[threadIdx.x] = top;
+    __syncthreads();
+    for (int n = 128; n > 0; n >>= 1) {
+        if (threadIdx.x < (unsigned)n) lds[threadIdx.x] = fmaxf(lds[threadIdx.x], lds[threadIdx.x + n]);
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) tops[blockIdx.x] = lds[0];
+}
+
+__global__ __launch_bounds__(256) void k_loss_factors(FactorArgs a)
+{
+    float up = a.up;
+    if (a.tops) { // the largest |dZ| comes into [2^14, 2^15)
+        float top = 0.0f;
+        for (uint32_t i = 0; i < a.n_tops; ++i) top = fmaxf(top, a.tops[i]);
+        up = ldexpf(1.0f, top > 0.0f ? min(15 - __builtin_amdgcn_frexp_expf(top), 126) : 0);
+    }
+    const uint32_t live = a.rows.live();
+    const uint64_t m = blockIdx.x * 256ull + threadIdx.x;
+    if (m == 0) {
+        const float total = a.total ? *a.total : 1.0f;
+        *a.power = total != 0.0f ? (a.dloss ? *a.dloss : 1.0f) / total / up : 0.0f;
+    }
+    if (m >= live) return;
+    RowFactor f{a.lse[m], 0.0f, a.labels.of(m), 0};
+    const float w = f.label == kNone ? 0.0f : a.weight ? a.weight[m] : 1.0f;
+    if (w != 0.0f) f.factor = w * up;
+    a.row[m] = f;
+}
+
+template <class T> struct DzArgs : ProductArgs { // N = the piece's classes; Y: [M, N rounded up to eight]
+    const RowFactor *row;
+    uint32_t first;   // the piece's first class
+    float *bias_part; // null, or [groups of rows][ld_part]: the sums of dZ over a wavefront's rows
+    int64_t ld_part;
+};
+
+// eight cells of a row; what is beyond the last class is 0
+__device__ __forceinline__ void dz8(const Columns &c, const RowFactor &f, uint32_t first, float (&v)[8])
+{
+    const uint32_t at = f.label - first - c.n;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        v[j] = f.factor * power_of(v[j] + c.bias[j], f.lse);
+        v[j] -= at == (uint32_t)j ? f.factor : 0.0f;
+        v[j] = f.factor != 0.0f && j < c.left ? v[j] : 0.0f;
+    }
+}
+
+// The hand-over through LDS of 4 KB, as for other products' cells: 32 x 32 cells at a time, four lanes have 32 columns of a row.
+template <class T, int FM, int FN> __device__ __forceinline__ void hand_over_dz(const DzArgs<T> &p, f32x16 (&acc)[FM][FN], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M)
+{
+    const uint32_t lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31, g = lane & 3;
+    if (m_wave >= M) return;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const Columns c = columns_of(p.e, n_wave + 32 * j + 8 * g, p.N);
+        float sums[8] = {};
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            RowFactor f[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t m = m_wave + 32 * i + (lane >> 2) + 16 * u;
+                f[u] = p.row[min(m, M - 1)];
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                mine[row * 8 + ((2 * q + half) ^ ((row >> 1) & 7))] = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+            lds_exchange();
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t r = (lane >> 2) + 16 * u, m = m_wave + 32 * i + r;
+                const f32x4 lo = mine[r * 8 + ((2 * g) ^ ((r >> 1) & 7))], hi = mine[r * 8 + ((2 * g + 1) ^ ((r >> 1) & 7))];
+                float v[8];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = lo[k], v[4 + k] = hi[k];
+                if (c.left <= 0 || m >= M) continue;
+                dz8(c, f[u], p.first, v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sums[k] += v[k];
+                store8(static_cast<T *>(p.e.Y) + m * p.e.ld_Y + c.n, 8, v, p.e.stream);
+            }
+            lds_exchange();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (p.bias_part) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+#pragma unroll
+                for (int d = 4; d < 64; d <<= 1) sums[k] += __shfl_xor(sums[k], d);
+            if (lane < 4 && c.left > 0) store8(p.bias_part + m_wave / (32 * FM) * p.ld_part + c.n, 8, sums);
+        }
+    }
+}
+
+template <class T> struct Out<DzArgs<T>> {
+    template <class O, bool PLAIN, int FM> __device__ __forceinline__ static void wide(const DzArgs<T> &p, f32x16 (&acc)[FM][2], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t)
+    {
+        hand_over_dz(p, acc, mine, m_wave, n_wave, M);
+    }
+    template <class O, bool PLAIN, int FM, int FN> __device__ __forceinline__ static void narrow(const DzArgs<T> &p, f32x16 (&acc)[FM][FN], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t)
+    {
+        hand_over_dz(p, acc, mine, m_wave, n_wave, M);
+    }
+    struct Few {
+        Columns c;
+        RowFactor f;
+        __device__ __forceinline__ void begin(const DzArgs<T> &p, uint32_t m, uint32_t n, uint32_t live)
+        {
+            c = columns_of(p.e, n, p.N);
+            f = p.row[min(m, live - 1)];
+        }
+        template <class F> __device__ __forceinline__ void end(const DzArgs<T> &p, uint32_t m, uint32_t live, F &&sums)
+        {
+            float v[8];
+            sums(0, v);
+            if (m >= live) f.factor = 0.0f;
+            dz8(c, f, p.first, v);
+            if (m < live && c.left > 0) store8(static_cast<T *>(p.e.Y) + m * p.e.ld_Y + c.n, 8, v, p.e.stream);
+            if (!p.bias_part) return;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+#pragma unroll
+                for (int d = 4; d < 64; d <<= 1) v[k] += __shfl_xor(v[k], d);
+            if ((threadIdx.x & 63) < 4 && c.left > 0) store8(p.bias_part + m / 16 * p.ld_part + c.n, 8, v);
+        }
+    };
+};
+
+template <class T> __global__ __launch_bounds__(256) void k_loss_dz_few(DzArgs<T> p) { few_tile<T>(p); }
+template <class T> __global__ __launch_bounds__(256, 2) void k_loss_dz_anyhow(DzArgs<T> p) { product_tile<T, 64, 64, false, false>(p); }
+template <class T> __global__ __launch_bounds__(256, 2) void k_loss_dz_chunks(DzArgs<T> p) { chunks_tile<T, T, 256, 128, false, false>(p); }
+template <> __global__ __launch_bounds__(256, 3) void k_loss_dz_chunks<float>(DzArgs<float> p) { chunks_tile<float, float, 128, 128, false, false>(p); }
+template <class T> __global__ __launch_bounds__(512, 2) void k_loss_dz_long(DzArgs<T> p) { long_tiles<T, T, false, false>(p); }
+
+// Parts of dA's sum over the classes, in fp32: those of one piece, where the tiles of [rows, in] alone would leave compute units idle, and those of the pieces.
+template <class T> __global__ __launch_bounds__(256, 2) void k_loss_part_anyhow(ProductArgs p) { product_tile<T, 64, 64, false, true>(p); }
+template <class T> __global__ __launch_bounds__(256, 2) void k_loss_part_chunks(ProductArgs p) { chunks_tile<T, float, 256, 128, false, true>(p); }
+template <> __global__ __launch_bounds__(256, 3) void k_loss_part_chunks<float>(ProductArgs p) { chunks_tile<float, float, 128, 128, false, true>(p); }
+template <class T> __global__ __launch_bounds__(512, 2) void k_loss_part_long(ProductArgs p) { long_tiles<T, float, false, true>(p); }
+
+// dbias = power x the sum over the groups of rows: 32 classes to a workgroup, eight groups side by side, then in order.
+__global__ __launch_bounds__(256) void k_loss_bias(Rows rows, uint32_t group, uint32_t N, const float *part, int64_t ld_part, const float *power, float *out)
+{
+    __shared__ float lds[8][32];
+    const uint32_t n = blockIdx.x * 32 + (threadIdx.x & 31), g = threadIdx.x >> 5, groups = (rows.live() + group - 1) / group;
+    float sum = 0.0f;
+    if (n < N)
+        for (uint32_t i = g; i < groups; i += 8) sum += part[i * ld_part + n];
+    lds[g][threadIdx.x & 31] = sum;
+    __syncthreads();
+    if (g || n >= N) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) sum += lds[i][threadIdx.x];
+    out[n] = sum * *power;
+}
+
+// ---- operands that lie anyhow -----------------------------------------------------------------------------------------------------
+
+// A copy whose rows are whole chunks: [rows, cols] to [rows, ld_to], zeros behind the columns.
+template <class T> __global__ __launch_bounds__(256) void k_loss_pack(const T *from, int64_t ld_from, uint32_t rows, uint32_t cols, T *to, uint32_t groups)
+{
+    const uint64_t i = (uint64_t)block_number() * 256 + threadIdx.x, r = i / groups;
+    const uint32_t g = (uint32_t)(i - r * groups);
+    if (r >= rows) return;
+    float v[8];
+    load8(from + r * ld_from + 8 * g, (int)cols - 8 * (int)g, v);
+    store8(to + (r * groups + g) * 8, 8, v);
+}
+
+// ---- host side --------------------------------------------------------------------------------------------------------------------
+
+enum Kind { kFew, kAnyhow, kChunks, kLong };
+
+// which kernel makes the logits of [M, N], K terms each
+template <class T> Kind kind_of(const ProductArgs &p)
+{
+    const bool chunks = in_chunks<T>(p.a, p.M, p.K) && in_chunks<T>(p.b, p.N, p.K);
+    if (few_tiles<T>(p, chunks)) return kFew;
+    if (!chunks) return kAnyhow;
+    if (sizeof(T) == 4) return kChunks;
+    return tile_blocks<256, 256>(p) >= 256 && p.K * sizeof(T) >= 2048 ? kLong : kChunks;
+}
+
+constexpr uint32_t slot_width(Kind k) { return k == kFew || k == kAnyhow ? 32 : 64; } // columns of a Top
+constexpr uint32_t group_rows(Kind k, bool f32) { return k == kFew ? 16 : k == kAnyhow ? 32 : k == kChunks && f32 ? 64 : 128; } // rows of a sum for dbias
+
+constexpr int64_t kPieceBytes = int64_t(1) << 30; // of dZ
+constexpr double kPackFlops = 2e9;                // products from here on are worth a copy of operands that lie anyhow
+
+struct Shape {
+    int64_t rows;
+    int32_t in, out, dtype;
+    const void *A, *W;
+    int64_t ld_A, ld_W;
+};
+
+// the operands, or where their copies will be
+struct Packed {
+    bool copy_A = false, copy_W = false;
+    uint32_t K = 0; // terms, zeros behind `in` among them
+    Operand a, w;
+};
+
+template <class Take> Packed packed_plan(const Shape &s, Take &&take, size_t (&off)[2])
+{
+    Packed r;
+    r.K = (uint32_t)s.in;
+    r.a = {s.A, s.ld_A, false, false};
+    r.w = {s.W, s.ld_W, false, false};
+    const auto fits = [&](const Operand &o, int64_t rows) {
+        if (s.dtype == ZG_F32) return in_chunks<float>(o, (uint32_t)rows, (uint32_t)s.in);
+        return in_chunks<_Float16>(o, (uint32_t)rows, (uint32_t)s.in);
+    };
+    const bool A = fits(r.a, s.rows), W = fits(r.w, s.out);
+    if ((A && W) || 2.0 * s.rows * s.out * s.in < kPackFlops) return r;
+    const int64_t ld = (s.in + 7) / 8 * 8;
+    if (s.in * type_size(s.dtype) % 16) r.K = (uint32_t)ld; // (else one of the two may be read where it lies)
+    if (!A) r.copy_A = true, off[0] = take((size_t)s.rows * ld * type_size(s.dtype)), r.a = {nullptr, ld, false, true};
+    if (!W) r.copy_W = true, off[1] = take((size_t)s.out * ld * type_size(s.dtype)), r.w = {nullptr, ld, false, true};
+    return r;
+}
+
+template <class F> int with_wide_type(int32_t type, F &&f)
+{
+    if (type == ZG_F32) return f(float());
+    if (type == ZG_F16) return f((_Float16)0);
+    return f((__bf16)0);
+}
+
+int launch_pack(hipStream_t st, int32_t dtype, const void *from, int64_t ld, int64_t rows, int32_t cols, void *to)
+{
+    const uint32_t groups = ((uint32_t)cols + 7) / 8;
+    return with_wide_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        return launch(st, k_loss_pack<T>, grid_of(((uint64_t)rows * groups + 255) / 256), 256, static_cast<const T *>(from), ld, (uint32_t)rows, (uint32_t)cols, static_cast<T *>(to), groups);
+    });
+}
+
+// [rows, in] x [out, in]: the logits' product
+ProductArgs logits_product(const Shape &s, const Packed &pk, const uint32_t *d_rows)
+{
+    ProductArgs p{};
+    p.a = pk.a, p.b = pk.w;
+    p.M = (uint32_t)s.rows, p.N = (uint32_t)s.out, p.K = pk.K;
+    p.rows = {d_rows, p.M};
+    p.splits = 1;
+    p.e.factor = 1.0f;
+    return p;
+}
+
+// Addresses only matter for their alignment here: copies' are null.
+Kind logits_kind(int32_t dtype, const ProductArgs &p) { return (Kind)with_wide_type(dtype, [&](auto t) { return (int)kind_of<decltype(t)>(p); }); }
+
+struct TopPlan {
+    Packed pk;
+    Kind kind;
+    uint32_t slots, row_block, row_grid;
+    size_t off_pack[2], off_part, off_at, off_sums, total;
+};
+
+struct Taker {
+    size_t &total;
+    size_t operator()(size_t bytes) const
+    {
+        const size_t at = total;
+        total = (total + bytes + 255) / 256 * 256;
+        return at;
+    }
+};
+
+TopPlan top_plan(const Shape &s)
+{
+    TopPlan t{};
+    const Taker take{t.total};
+    t.pk = packed_plan(s, take, t.off_pack);
+    t.kind = logits_kind(s.dtype, logits_product(s, t.pk, nullptr));
+    t.slots = ((uint32_t)s.out + slot_width(t.kind) - 1) / slot_width(t.kind);
+    t.off_part = take((size_t)t.slots * s.rows * sizeof(Top));
+    t.off_at = take((size_t)s.rows * sizeof(float));
+    // a workgroup for each of few rows with many parts; whole rows side by side where there are few parts
+    t.row_block = s.rows <= 64 && t.slots > 32 ? 1 : t.slots <= 4 ? 256 : 32;
+    t.row_grid = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(1024, (s.rows + t.row_block - 1) / t.row_block));
+    t.off_sums = take((size_t)t.row_grid * 2 * sizeof(double));
+    return t;
+}
+
+struct DzPlan {
+    Packed pk;
+    Kind kind;
+    int64_t piece, pieces, ld_dz;
+    uint32_t splits_A, slots_A, splits_W; // parts of a piece's sum for dA, parts that there is room for, parts of dW's
+    size_t off_pack[2], off_row, off_power, off_tops, off_dz, off_part_A, off_part_W, off_bias, total;
+};
+
+DzPlan dz_plan(const Shape &s, bool dA, bool dW, bool dbias, bool weight)
+{
+    DzPlan t{};
+    const Taker take{t.total};
+    const int64_t e = (int64_t)type_size(s.dtype), rows = std::max<int64_t>(1, s.rows);
+    t.pk = packed_plan(s, take, t.off_pack);
+    t.piece = std::max<int64_t>(4096, kPieceBytes / (rows * e) / 256 * 256);
+    if (t.piece >= s.out) t.piece = s.out;
+    t.pieces = (s.out + t.piece - 1) / t.piece;
+    t.ld_dz = (t.piece + 7) / 8 * 8;
+    Shape one = s;
+    one.out = (int32_t)t.piece;
+    t.kind = logits_kind(s.dtype, logits_product(one, t.pk, nullptr));
+    t.off_row = take((size_t)s.rows * sizeof(RowFactor));
+    t.off_power = take(sizeof(float));
+    if (weight && s.dtype == ZG_F16) t.off_tops = take(kWeightBlocks * sizeof(float));
+    t.off_dz = take((size_t)s.rows * t.ld_dz * e);
+    const int64_t tiles_A = (rows + 255) / 256 * ((s.in + 127) / 128), tiles_W = (t.piece + 255) / 256 * ((s.in + 127) / 128);
+    t.splits_A = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(512 / tiles_A, t.piece / 1024));
+    t.splits_W = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(512 / tiles_W, (rows + 255) / 256));
+    const int64_t parts = t.pieces * t.splits_A;
+    t.slots_A = (uint32_t)(parts == 1 ? 0 : std::min<int64_t>(parts, t.splits_A + 4));
+    if (dA) t.off_part_A = take((size_t)t.slots_A * s.rows * s.in * sizeof(float));
+    if (dW && t.splits_W > 1) t.off_part_W = take((size_t)t.splits_W * t.piece * s.in * sizeof(float));
+    const uint32_t group = group_rows(t.kind, s.dtype == ZG_F32);
+    if (dbias) t.off_bias = take((size_t)((s.rows + group - 1) / group) * t.ld_dz * sizeof(float));
+    return t;
+}
+
+int check_labels(const char *what, const void *p, int32_t type)
+{
+    if (type != ZG_I32 && type != ZG_I64) return fail(ZG_EINVAL, "label_dtype is not ZG_I32 or ZG_I64");
+    return reinterpret_cast<uintptr_t>(p) % (type == ZG_I64 ? 8 : 4) ? fail(ZG_EINVAL, std::string(what) + " is not aligned to its elements") : ZG_OK;
+}
+
+Span labels_span(const void *p, int64_t rows, int32_t type)
+{
+    Span s = vector_span("d_labels", p, rows);
+    if (type == ZG_I64) s.pitch = s.width = rows * 8, s.size = 8;
+    return s;
+}
+
+template <class A> int check_common(const A *a)
+{
+    if (!a) return fail(ZG_EINVAL, "null argument");
+    ZG_TRY(check_rows(a->rows));
+    ZG_TRY(check_width(a->in));
+    ZG_TRY(check_width(a->out, ZG_MAX_CLASSES));
+    if (!wide_type(a->dtype)) return fail(ZG_EINVAL, "dtype is not ZG_F32, ZG_F16 or ZG_BF16");
+    ZG_TRY(check_labels("d_labels", a->d_labels, a->label_dtype));
+    ZG_TRY(check_vector("d_rows", a->d_rows));
+    ZG_TRY(check_vector("d_bias", a->d_bias));
+    ZG_TRY(check_vector("d_weight", a->d_weight));
+    if (a->rows > 0) {
+        ZG_TRY(check_matrix("d_A", a->d_A, a->ld_A, a->in, a->dtype));
+        ZG_TRY(check_matrix("d_W", a->d_W, a->ld_W, a->in, a->dtype));
+        if (!a->d_labels) return fail(ZG_EINVAL, "d_labels is null");
+    }
+    return ZG_OK;
+}
+
+template <class A> Shape shape_of(const A *a) { return {a->rows, a->in, a->out, a->dtype, a->d_A, a->d_W, a->ld_A, a->ld_W}; }
+
+template <class A> int launch_packs(hipStream_t st, const A *a, char *ws, const size_t (&off)[2], Packed &pk)
+{
+    if (pk.copy_A) {
+        ZG_TRY(launch_pack(st, a->dtype, a->d_A, a->ld_A, a->rows, a->in, ws + off[0]));
+        pk.a.p = ws + off[0];
+    }
+    if (pk.copy_W) {
+        ZG_TRY(launch_pack(st, a->dtype, a->d_W, a->ld_W, a->out, a->in, ws + off[1]));
+        pk.w.p = ws + off[1];
+    }
+    return ZG_OK;
+}
+
+template <class T> int launch_tops(hipStream_t st, Kind kind, const TopArgs &p)
+{
+    if (kind == kFew) return launch(st, k_loss_top_few<T>, grid_of((uint64_t)((p.M + 31) / 32) * ((p.N + 31) / 32)), 256, p);
+    if (kind == kAnyhow) return launch(st, k_loss_top_anyhow<T>, tile_grid<64, 64>(p), 256, p);
+    if constexpr (sizeof(T) == 4) {
+        return launch(st, k_loss_top_chunks<T>, tile_grid<128, 128>(p), 256, p);
+    } else {
+        if (kind == kLong) return launch(st, k_loss_top_long<T>, dim3(256), 512, p);
+        return launch(st, k_loss_top_chunks<T>, tile_grid<256, 128>(p), 256, p);
+    }
+}
+
+template <class T> int launch_dz(hipStream_t st, Kind kind, const DzArgs<T> &p)
+{
+    if (kind == kFew) return launch(st, k_loss_dz_few<T>, grid_of((uint64_t)((p.M + 31) / 32) * ((p.N + 31) / 32)), 256, p);
+    if (kind == kAnyhow) return launch(st, k_loss_dz_anyhow<T>, tile_grid<64, 64>(p), 256, p);
+    if constexpr (sizeof(T) == 4) {
+        return launch(st, k_loss_dz_chunks<T>, tile_grid<128, 128>(p), 256, p);
+    } else {
+        if (kind == kLong) return launch(st, k_loss_dz_long<T>, dim3(256), 512, p);
+        return launch(st, k_loss_dz_chunks<T>, tile_grid<256, 128>(p), 256, p);
+    }
+}
+
+// splits parts of [M, N] in fp32, one behind the other from p.e.Y on
+template <class T> int launch_parts(hipStream_t st, const ProductArgs &p, bool chunks)
+{
+    if (!chunks) return launch(st, k_loss_part_anyhow<T>, tile_grid<64, 64>(p), 256, p);
+    if constexpr (sizeof(T) == 4) {
+        return launch(st, k_loss_part_chunks<T>, tile_grid<128, 128>(p), 256, p);
+    } else {
+        if (tile_blocks<256, 256>(p) >= 256) return launch(st, k_loss_part_long<T>, dim3(256), 512, p);
+        return launch(st, k_loss_part_chunks<T>, tile_grid<256, 128>(p), 256, p);
+    }
+}
+
+} // namespace
+} // namespace zg
+
+using namespace zg;
+
+extern "C" {
+int zg_linear_cross_entropy_workspace(const zg_linear_cross_entropy_args *a, size_t *bytes)
+{
+    return entry([&]() -> int {
+        ZG_TRY(check_common(a));
+        if (!bytes) return fail(ZG_EINVAL, "null argument");
+        *bytes = top_plan(shape_of(a)).total;
+        return ZG_OK;
+    });
+}
+
+int zg_linear_cross_entropy(const zg_linear_cross_entropy_args *a, void *d_workspace, size_t workspace_bytes, void *stream)
+{
+    return entry([&]() -> int {
+        ZG_TRY(check_common(a));
+        if (!a->d_loss) return fail(ZG_EINVAL, "d_loss is null");
+        if (a->rows > 0 && !a->d_lse) return fail(ZG_EINVAL, "d_lse is null");
+        for (const void *v : {(const void *)a->d_loss, (const void *)a->d_total, (const void *)a->d_lse, (const void *)a->d_row_loss}) ZG_TRY(check_vector("an output", v));
+        {
+            const Span A = matrix_span("d_A", a->d_A, a->rows, a->ld_A, a->in, a->dtype), W = matrix_span("d_W", a->d_W, a->rows ? a->out : 0, a->ld_W, a->in, a->dtype);
+            const Span bias = vector_span("d_bias", a->d_bias, a->out), labels = labels_span(a->d_labels, a->rows, a->label_dtype), weight = vector_span("d_weight", a->d_weight, a->rows);
+            const Span count = rows_span(a->d_rows), loss = vector_span("d_loss", a->d_loss, 1), total = vector_span("d_total", a->d_total, 1);
+            const Span lse = vector_span("d_lse", a->d_lse, a->rows), each = vector_span("d_row_loss", a->d_row_loss, a->rows);
+            ZG_TRY(check_apart(loss, {A, W, bias, labels, weight, count, total, lse, each}));
+            ZG_TRY(check_apart(total, {A, W, bias, labels, weight, count, lse, each}));
+            ZG_TRY(check_apart(lse, {A, W, bias, labels, weight, count, each}));
+            ZG_TRY(check_apart(each, {A, W, bias, labels, weight, count}));
+        }
+        TopPlan t = top_plan(shape_of(a));
+        ZG_TRY(check_workspace(d_workspace, workspace_bytes, t.total));
+        const hipStream_t st = static_cast<hipStream_t>(stream);
+        char *const ws = static_cast<char *>(d_workspace);
+        const Labels labels{a->d_labels, a->label_dtype == ZG_I64, (uint32_t)a->out};
+        Top *const part = reinterpret_cast<Top *>(ws + t.off_part);
+        float *const at = reinterpret_cast<float *>(ws + t.off_at);
+        if (a->rows > 0) {
+            ZG_TRY(launch_packs(st, a, ws, t.off_pack, t.pk));
+            TopArgs p{};
+            static_cast<ProductArgs &>(p) = logits_product(shape_of(a), t.pk, a->d_rows);
+            p.e.bias = a->d_bias;
+            p.labels = labels, p.part = part, p.at_label = at;
+            ZG_TRY(with_wide_type(a->dtype, [&](auto v) { return launch_tops<decltype(v)>(st, t.kind, p); }));
+        }
+        RowArgs r{};
+        r.rows = {a->d_rows, (uint32_t)a->rows};
+        r.slots = t.slots, r.cap = (uint32_t)a->rows, r.part = part, r.at_label = at, r.weight = a->d_weight, r.labels = labels;
+        r.lse = a->d_lse, r.row_loss = a->d_row_loss, r.sums = reinterpret_cast<double *>(ws + t.off_sums), r.loss = a->d_loss, r.total = a->d_total;
+        const dim3 grid(t.row_grid);
+        ZG_TRY(t.row_block == 1 ? launch(st, k_loss_rows<1>, grid, 256, r) : t.row_block == 32 ? launch(st, k_loss_rows<32>, grid, 256, r) : launch(st, k_loss_rows<256>, grid, 256, r));
+        return t.row_grid > 1 ? launch(st, k_loss_mean, dim3(1), 64, r, t.row_grid) : ZG_OK;
+    });
+}
+
+int zg_linear_cross_entropy_backward_workspace(const zg_linear_cross_entropy_grad_args *a, size_t *bytes)
+{
+    return entry([&]() -> int {
+        ZG_TRY(check_common(a));
+        if (!bytes) return fail(ZG_EINVAL, "null argument");
+        *bytes = dz_plan(shape_of(a), a->d_dA, a->d_dW, a->d_dbias, a->d_weight).total;
+        return ZG_OK;
+    });
+}
+
+int zg_linear_cross_entropy_backward(const zg_linear_cross_entropy_grad_args *a, void *d_workspace, size_t workspace_bytes, void *stream)
+{
+    return entry([&]() -> int {
+        ZG_TRY(check_common(a));
+        if (a->rows > 0 && !a->d_lse) return fail(ZG_EINVAL, "d_lse is null");
+        for (const void *v : {(const void *)a->d_lse, (const void *)a->d_total, (const void *)a->d_dloss, (const void *)a->d_dbias}) ZG_TRY(check_vector("a vector", v));
+        if (a->d_dA && a->rows > 0) ZG_TRY(check_matrix("d_dA", a->d_dA, a->ld_dA, a->in, a->dtype));
+        if (a->d_dW) ZG_TRY(check_matrix("d_dW", a->d_dW, a->ld_dW, a->in, a->dtype));
+        {
+            const Span A = matrix_span("d_A", a->d_A, a->rows, a->ld_A, a->in, a->dtype), W = matrix_span("d_W", a->d_W, a->rows ? a->out : 0, a->ld_W, a->in, a->dtype);
+            const Span bias = vector_span("d_bias", a->d_bias, a->out), labels = labels_span(a->d_labels, a->rows, a->label_dtype), weight = vector_span("d_weight", a->d_weight, a->rows);
+            const Span count = rows_span(a->d_rows), lse = vector_span("d_lse", a->d_lse, a->rows), total = vector_span("d_total", a->d_total, 1), dloss = vector_span("d_dloss", a->d_dloss, 1);
+            const Span dA = matrix_span("d_dA", a->d_dA, a->rows, a->ld_dA, a->in, a->dtype), dW = matrix_span("d_dW", a->d_dW, a->out, a->ld_dW, a->in, a->dtype);
+            const Span dbias = vector_span("d_dbias", a->d_dbias, a->out);
+            ZG_TRY(check_apart(dA, {A, W, bias, labels, weight, count, lse, total, dloss}));
+            ZG_TRY(check_apart(dW, {A, W, bias, labels, weight, count, lse, total, dloss, dA}));
+            ZG_TRY(check_apart(dbias, {A, W, bias, labels, weight, count, lse, total, dloss, dA, dW}));
+        }
+        const bool want_A = a->d_dA, want_W = a->d_dW, want_b = a->d_dbias;
+        DzPlan t = dz_plan(shape_of(a), want_A, want_W, want_b, a->d_weight);
+        ZG_TRY(check_workspace(d_workspace, workspace_bytes, t.total));
+        if (!want_A && !want_W && !want_b) return ZG_OK;
+        const hipStream_t st = static_cast<hipStream_t>(stream);
+        char *const ws = static_cast<char *>(d_workspace);
+        const Rows rows{a->d_rows, (uint32_t)a->rows};
+        float *const power = reinterpret_cast<float *>(ws + t.off_power);
+        if (a->rows > 0) ZG_TRY(launch_packs(st, a, ws, t.off_pack, t.pk));
+        FactorArgs f{};
+        f.rows = rows;
+        f.lse = a->d_lse, f.weight = a->d_weight, f.total = a->d_total, f.dloss = a->d_dloss;
+        f.labels = {a->d_labels, a->label_dtype == ZG_I64, (uint32_t)a->out};
+        // fp16's range does not hold a softmax over many classes as it is: |dZ| / |weight| <= 1 is brought to the top of it (the other types' does)
+        f.up = a->dtype == ZG_F16 ? 16384.0f : 1.0f;
+        f.row = reinterpret_cast<RowFactor *>(ws + t.off_row), f.power = power;
+        if (a->d_weight && a->dtype == ZG_F16 && a->rows > 0) {
+            float *const tops = reinterpret_cast<float *>(ws + t.off_tops);
+            f.tops = tops, f.n_tops = kWeightBlocks;
+            ZG_TRY(launch(st, k_loss_weight_top, dim3(kWeightBlocks), 256, f, tops));
+        }
+        ZG_TRY(launch(st, k_loss_factors, dim3((unsigned)std::max<int64_t>(1, (a->rows + 255) / 256)), 256, f));
+        const auto run = [&](auto zero) -> int {
+            using T = decltype(zero);
+            T *const dz = reinterpret_cast<T *>(ws + t.off_dz);
+            float *const part_A = reinterpret_cast<float *>(ws + t.off_part_A), *const bias_part = reinterpret_cast<float *>(ws + t.off_bias);
+            const bool parts_A = t.pieces * t.splits_A > 1;
+            const int64_t cells_A = a->rows * a->in;
+            uint32_t filled = 0; // parts of dA that are there
+            for (int64_t first = 0; first < a->out; first += t.piece) {
+                const uint32_t n = (uint32_t)std::min<int64_t>(t.piece, a->out - first), n8 = (n + 7) / 8 * 8;
+                Operand w = t.pk.w;
+                w.p = static_cast<const T *>(w.p) + first * w.ld;
+                if (a->rows > 0) {
+                    Shape s = shape_of(a);
+                    s.out = (int32_t)n;
+                    DzArgs<T> p{};
+                    static_cast<ProductArgs &>(p) = logits_product(s, t.pk, a->d_rows);
+                    p.b = w;
+                    p.e.bias = a->d_bias ? a->d_bias + first : nullptr;
+                    p.e.Y = dz, p.e.ld_Y = t.ld_dz;
+                    p.row = f.row, p.first = (uint32_t)first;
+                    p.bias_part = want_b ? bias_part : nullptr, p.ld_part = t.ld_dz;
+                    ZG_TRY(launch_dz(st, t.kind, p));
+                }
+                if (want_b)
+                    ZG_TRY(launch(st, k_loss_bias, dim3((n + 31) / 32), 256, rows, group_rows(t.kind, sizeof(T) == 4), n, bias_part, t.ld_dz, power, a->d_dbias + first));
+                if (want_W) {
+                    ProductArgs p{};
+                    p.a = {dz, t.ld_dz, true, true};
+                    p.b = t.pk.a, p.b.turned = true;
+                    p.M = n, p.N = (uint32_t)a->in, p.K = (uint32_t)a->rows;
+                    p.rows = rows, p.rows_are_k = 1;
+                    p.splits = t.splits_W;
+                    p.e.factor = 1.0f, p.e.power = power, p.e.type = a->dtype;
+                    p.e.Y = static_cast<T *>(a->d_dW) + first * a->ld_dW, p.e.ld_Y = a->ld_dW;
+                    ZG_TRY(dense_product(st, a->dtype, p, reinterpret_cast<float *>(ws + t.off_part_W)));
+                }
+                if (want_A && a->rows > 0) {
+                    ProductArgs p{};
+                    p.a = {dz, t.ld_dz, false, true};
+                    p.b = w, p.b.turned = true;
+                    p.M = (uint32_t)a->rows, p.N = (uint32_t)a->in;
+                    const bool chunks = in_chunks<T>(p.b, p.N, n8); // (dZ is)
+                    p.K = chunks ? n8 : n, p.b_short = chunks ? n8 - n : 0;
+                    p.rows = rows;
+                    p.e.factor = 1.0f;
+                    if (!parts_A) {
+                        p.splits = 1;
+                        p.e.power = power, p.e.type = a->dtype;
+                        p.e.Y = a->d_dA, p.e.ld_Y = a->ld_dA;
+                        ZG_TRY(dense_product(st, a->dtype, p));
+                    } else {
+                        Epilogue sum{};
+                        sum.factor = 1.0f, sum.type = ZG_F32, sum.Y = part_A, sum.ld_Y = a->in;
+                        if (filled + t.splits_A > t.slots_A) { // no room: what is there becomes the first part
+                            ZG_TRY(dense_join(st, part_A, p.M, p.N, filled, sum, rows));
+                            filled = 1;
+                        }
+                        p.splits = t.splits_A;
+                        p.e.type = ZG_F32, p.e.Y = part_A + filled * cells_A, p.e.ld_Y = a->in, p.e.part = cells_A;
+                        ZG_TRY(launch_parts<T>(st, p, chunks));
+                        filled += t.splits_A;
+                    }
+                }
+            }
+            if (want_A && parts_A && a->rows > 0) {
+                Epilogue e{};
+                e.factor = 1.0f, e.power = power, e.type = a->dtype, e.Y = a->d_dA, e.ld_Y = a->ld_dA;
+                ZG_TRY(dense_join(st, part_A, (uint32_t)a->rows, (uint32_t)a->in, filled, e, rows));
+            }
+            return ZG_OK;
+        };
+        return with_wide_type(a->dtype, run);
+    });
+}
+
+} // extern "C"

@@ -38,7 +38,7 @@ struct Operand {
 struct ProductArgs {
     Operand a, b;
     uint32_t M, N, K;
-    uint32_t b_short; // the last rows that b, turned, does not have of K: 0 there (no parts then)
+    uint32_t b_short; // the last rows that b, turned, does not have of K: 0 there
     Rows rows;
     int32_t rows_are_k; // the device's count bounds K, else M
     uint32_t splits;    // parts that the sum is made in
@@ -50,6 +50,9 @@ struct ProductArgs {
 
 // any product with an epilogue, through zg_linear.hip's kernels; `part`: room for splits x M x N sums where there are parts
 int dense_product(hipStream_t st, int32_t type, const ProductArgs &p, float *part = nullptr);
+
+// what the epilogue makes of the sum of `splits` parts of [M, N], one behind the other from `part` on (the first of them may be the result)
+int dense_join(hipStream_t st, const float *part, uint32_t M, uint32_t N, uint32_t splits, const Epilogue &e, Rows rows);
 
 #ifdef __HIPCC__
 
@@ -766,14 +769,15 @@ template <class A, class B, int b_at, int step_k, int stage, int stages, class O
     A &a;
     B &b;
     u32x4 *lds;
-    uint32_t wave, b_short, k, k_end;
+    uint32_t wave, b_end, k, k_end; // (b_end: of b's k, where it is turned)
     On on;
-    uint32_t into = 0, left = 0;
+    uint32_t into = 0, left = 0, left_b = 0;
     __amdgpu_buffer_rsrc_t ra, rb;
 
     __device__ __forceinline__ void open()
     {
         left = k < k_end ? k_end - k : 0u;
+        if (B::turned) left_b = k < b_end ? min(left, b_end - k) : 0u;
         ra = a.at(k);
         rb = b.at(k);
     }
@@ -781,7 +785,7 @@ template <class A, class B, int b_at, int step_k, int stage, int stages, class O
     {
         u32x4 *const to = lds + into * stage;
         if (l < A::loads) a.fetch(l, ra, left, to, wave);
-        else b.fetch(l - A::loads, rb, B::turned ? left - min(left, b_short) : left, to + b_at, wave);
+        else b.fetch(l - A::loads, rb, B::turned ? left_b : left, to + b_at, wave);
     }
     __device__ __forceinline__ void next()
     {
@@ -837,7 +841,7 @@ template <class T, class O, int BM, int BN, bool A_TURNED, bool B_TURNED, class 
         }
     };
     if constexpr (Args::segments > 1) a.p += p.plane_a(0), b.p += p.plane_b(0);
-    Fetch<A, B, BM * 4, depth, stage, stages, decltype(on)> fetch{a, b, lds, wave, p.b_short, w.k_first, w.k_end, on};
+    Fetch<A, B, BM * 4, depth, stage, stages, decltype(on)> fetch{a, b, lds, wave, p.K - p.b_short, w.k_first, w.k_end, on};
     f32x16 acc[FM][FN] = {};
     uint32_t now = 0;
     if (steps > 0) {
@@ -885,7 +889,7 @@ template <class T, class O, bool A_TURNED, bool B_TURNED, class Args> __device__
             return;
         }
     };
-    Fetch<A, B, BM * CH, depth, stage, stages, decltype(on)> fetch{a, b, lds, wave, p.b_short, 0, 0, on};
+    Fetch<A, B, BM * CH, depth, stage, stages, decltype(on)> fetch{a, b, lds, wave, p.K - p.b_short, 0, 0, on};
     on(fetch);
     fetch.begin();
     Place w;

@@ -38,11 +38,20 @@ class NormResult(NamedTuple):
     scale: Optional[torch.Tensor]  # of an 8-bit y
 
 
+class LossResult(NamedTuple):
+    loss: torch.Tensor   # [1]
+    total: torch.Tensor  # [1], the sum of the weights of the rows that count
+    lse: torch.Tensor    # [rows]
+    row_loss: Optional[torch.Tensor]
+
+
 # The structs of include/zg.h as one pack() each (zg.LinearArgs and so on are the same by field): a call of a few rows takes the GPU less
 # than filling a ctypes structure field by field takes the host.
 _DROP = "dQIIq"
 _PACK = {"zg_linear": "@qq6i13q" + _DROP, "zg_linear_backward": "@qq6i13q" + _DROP, "zg_dropout": "@qq2i6q" + _DROP,
-         "zg_rms_norm": "@qq3if11q" + _DROP, "zg_rms_norm_backward": "@qq2i13q" + _DROP}
+         "zg_rms_norm": "@qq3if11q" + _DROP, "zg_rms_norm_backward": "@qq2i13q" + _DROP,
+         "zg_linear_cross_entropy": "@qq4i11q", "zg_linear_cross_entropy_backward": "@qq4i15q"}
+_WITH_WORKSPACE = {name for name in _PACK if name.endswith("_backward")} | {"zg_linear_cross_entropy"}
 _pack = {name: struct.Struct(f).pack for name, f in _PACK.items()}
 _entries: dict = {}
 
@@ -54,7 +63,7 @@ def _entry(name):
         args = [C.c_char_p]
         if name.endswith("_workspace"):
             args.append(C.POINTER(C.c_size_t))
-        elif name.endswith("_backward"):
+        elif name in _WITH_WORKSPACE:
             args += [C.c_void_p, C.c_size_t, C.c_void_p]
         else:
             args.append(C.c_void_p)
@@ -270,3 +279,56 @@ def rms_norm_backward(dy, h, rstd, *, gain=None, dh=None, dropout: Optional[Drop
                                   dx_at, ld_dx, dr_at, ld_dr, dg_at, *_mask(dropout, m, device)),
          device, stream, made, workspace=True)
     return dx, dr, dgain
+
+
+def _labels(t, rows, device):
+    """(type, address)"""
+    if t.dtype not in (_I32, torch.int64) or t.numel() != rows or t.device != device or not t.is_contiguous():
+        raise ValueError(f"labels are {list(t.shape)} of {t.dtype} on {t.device}: {rows} contiguous elements of int32 or int64 on {device} are wanted")
+    return zg.I32 if t.dtype is _I32 else zg.I64, t.data_ptr()
+
+
+def linear_cross_entropy(a, w, labels, *, bias=None, weight=None, rows=None, loss=None, total=None, lse=None, row_loss=False, stream=None) -> LossResult:
+    """Softmax cross entropy of the logits a w^T + bias, which are not kept: a: [rows, in], w: [classes, in] (one type), bias: float32 [classes], labels: int32 or int64
+    [rows]; a row whose label is outside 0..classes-1 has none.  loss = sum of weight (lse - logit of the label) / total over the rows that have a label, total = sum of their
+    weight (float32 [rows], default ones); 0 where no row counts.  `row_loss` (True or a tensor) returns each row's lse - logit of the label, 0 without a label.
+    All results are float32; lse and total are what `linear_cross_entropy_backward` needs."""
+    _no_history(a, w, bias, weight)
+    (m, k), device = _shape(a, "a")
+    n, dtype = w.shape[0], a.dtype
+    made = []
+    if loss is None and total is None:
+        both = torch.empty(2, dtype=_F32, device=device)
+        made.append(both)
+        loss, total = both[:1], both[1:]
+        loss_at = both.data_ptr()
+        total_at = loss_at + 4
+    else:
+        loss, loss_at = _out_vector(loss, "loss", 1, device, made)
+        total, total_at = _out_vector(total, "total", 1, device, made)
+    lse, lse_at = _out_vector(lse, "lse", m, device, made)
+    row_loss, each_at = _out_vector(None if row_loss is True else row_loss, "row_loss", m, device, made) if row_loss is not False and row_loss is not None else (None, 0)
+    kind, labels_at = _labels(labels, m, device)
+    _run("zg_linear_cross_entropy", (m, _vector(rows, "rows", 1, _I32, device), k, n, _type(dtype, "a"), kind, *_matrix(a, "a", m, k, dtype, device),
+                                     *_matrix(w, "w", n, k, dtype, device), _vector(bias, "bias", n, _F32, device), labels_at,
+                                     _vector(weight, "weight", m, _F32, device), loss_at, total_at, lse_at, each_at), device, stream, made, workspace=True)
+    return LossResult(loss, total, lse, row_loss)
+
+
+def linear_cross_entropy_backward(a, w, labels, lse, *, bias=None, weight=None, total=None, dloss=None, rows=None, need=(True, True, True), da=None, dw=None,
+                                  dbias=None, stream=None):
+    """Gradients (da, dw, dbias) of `linear_cross_entropy`'s loss, times dloss (float32 [1], default 1); `need` says which are wanted, the others are None.  lse and total
+    are the forward pass' (total=None: gradients of the weighted sum, not of the mean)."""
+    _no_history(a, w, bias, weight, lse, total, dloss)
+    (m, k), device = _shape(a, "a")
+    n, dtype = w.shape[0], a.dtype
+    made = []
+    da, da_at, ld_da = _out(da, "da", m, k, dtype, device, made) if need[0] or da is not None else _NONE3
+    dw, dw_at, ld_dw = _out(dw, "dw", n, k, dtype, device, made) if need[1] or dw is not None else _NONE3
+    dbias, db_at = _out_vector(dbias, "dbias", n, device, made) if need[2] or dbias is not None else (None, 0)
+    kind, labels_at = _labels(labels, m, device)
+    _run("zg_linear_cross_entropy_backward", (m, _vector(rows, "rows", 1, _I32, device), k, n, _type(dtype, "a"), kind, *_matrix(a, "a", m, k, dtype, device),
+                                              *_matrix(w, "w", n, k, dtype, device), _vector(bias, "bias", n, _F32, device), labels_at,
+                                              _vector(weight, "weight", m, _F32, device), _vector(lse, "lse", m, _F32, device), _vector(total, "total", 1, _F32, device),
+                                              _vector(dloss, "dloss", 1, _F32, device), da_at, ld_da, dw_at, ld_dw, db_at), device, stream, made, workspace=True)
+    return da, dw, dbias

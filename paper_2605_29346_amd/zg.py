@@ -19,7 +19,7 @@ OK, EINVAL, ENOMEM, EHIP, ESTATE = 0, -1, -2, -3, -4
 I32, I64 = 0, 1
 F32, F16, BF16, F8 = 2, 3, 4, 5
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
-MAX_WIDTH, MAX_NORM_WIDTH = 32768, 16384
+MAX_WIDTH, MAX_NORM_WIDTH, MAX_CLASSES = 32768, 16384, 1 << 24
 GRAPH_VALIDATE = 1
 PLAN_EAGER, PLAN_REPLACE, PLAN_SAFE_TWIN, PLAN_FUSED_INPUT, PLAN_AUTO_FALLBACK = 1, 2, 4, 8, 16
 PLAN_X_ONE_PASS, PLAN_X_TWO_PASS = 32, 64
@@ -41,7 +41,8 @@ EXPORTS = ["zg_strerror", "zg_last_error", "zg_graph_create", "zg_graph_create_s
            "zg_step_status", "zg_envelope_model_graph", "zg_envelope_from_pilot", "zg_pilot_update", "zg_build_id",
            "zg_calibration_copy", "zg_envelope_model_graph_static", "zg_plan_replay_features", "zg_step_timed",
            "zg_linear", "zg_linear_backward_workspace", "zg_linear_backward", "zg_dropout", "zg_rms_norm",
-           "zg_rms_norm_backward_workspace", "zg_rms_norm_backward"]
+           "zg_rms_norm_backward_workspace", "zg_rms_norm_backward", "zg_linear_cross_entropy_workspace", "zg_linear_cross_entropy",
+           "zg_linear_cross_entropy_backward_workspace", "zg_linear_cross_entropy_backward"]
 
 
 class Envelope(C.Structure):
@@ -112,6 +113,16 @@ class NormGradArgs(C.Structure):
         ("d_rstd", C.c_void_p), ("d_gain", C.c_void_p)] + _matrices("dh", "dx", "dr") + [("d_dgain", C.c_void_p), ("drop", Drop)]
 
 
+class LossArgs(C.Structure):
+    _fields_ = _ROWS + [("in_", C.c_int32), ("out", C.c_int32), ("dtype", C.c_int32), ("label_dtype", C.c_int32)] + _matrices("A", "W") + [
+        ("d_" + n, C.c_void_p) for n in ("bias", "labels", "weight", "loss", "total", "lse", "row_loss")]
+
+
+class LossGradArgs(C.Structure):
+    _fields_ = _ROWS + [("in_", C.c_int32), ("out", C.c_int32), ("dtype", C.c_int32), ("label_dtype", C.c_int32)] + _matrices("A", "W") + [
+        ("d_" + n, C.c_void_p) for n in ("bias", "labels", "weight", "lse", "total", "dloss")] + _matrices("dA", "dW") + [("d_dbias", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -173,6 +184,10 @@ def lib() -> C.CDLL:
         L.zg_rms_norm.argtypes = [P(NormArgs), vp]
         L.zg_rms_norm_backward_workspace.argtypes = [P(NormGradArgs), P(C.c_size_t)]
         L.zg_rms_norm_backward.argtypes = [P(NormGradArgs), vp, C.c_size_t, vp]
+        L.zg_linear_cross_entropy_workspace.argtypes = [P(LossArgs), P(C.c_size_t)]
+        L.zg_linear_cross_entropy.argtypes = [P(LossArgs), vp, C.c_size_t, vp]
+        L.zg_linear_cross_entropy_backward_workspace.argtypes = [P(LossGradArgs), P(C.c_size_t)]
+        L.zg_linear_cross_entropy_backward.argtypes = [P(LossGradArgs), vp, C.c_size_t, vp]
         for name in EXPORTS:
             if name not in ("zg_strerror", "zg_last_error", "zg_normal_quantile", "zg_build_id"):
                 getattr(L, name).restype = C.c_int
