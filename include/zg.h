@@ -568,6 +568,48 @@ typedef struct {
 int zg_linear_cross_entropy_backward_workspace(const zg_linear_cross_entropy_grad_args *a, size_t *bytes);
 int zg_linear_cross_entropy_backward(const zg_linear_cross_entropy_grad_args *a, void *d_workspace, size_t workspace_bytes, void *stream);
 
+/* O = X after `steps` Newton-Schulz steps on X = G / (|G| + eps), |G| the Frobenius norm: with (a, b, c) = coefficients[3 s .. 3 s + 2] in step s,
+ *   X <- a X + b (X X^T) X + c (X X^T)^2 X,
+ * which takes each singular value v to a v + b v^3 + c v^5 (3.4445, -4.7750, 2.0315 five times: all but the smallest into 0.7 .. 1.2).
+ * G: [rows, cols] of type dtype, O: of type out_dtype (may be G); rows, cols: 1..ZG_MAX_WIDTH.  coefficients is host memory, read before the call returns; coefficients under which the
+ * largest singular value, 1 at first, may grow beyond 1024 in a step are refused.  The norm is summed in 64 bits.
+ * Between the products X and what they are made of is held in 22 significant bits (two fp16 planes, relative to the largest value there can be), and the products are made of those, their sums being fp32.
+ * A ZG_BF16 result of at least 256 rows and columns and at most 6 steps has its products' operands rounded to fp16 (X itself stays in 22 bits): 1.0e-3 .. 1.8e-3 of the result's length, its own rounding being 1.7e-3. */
+#define ZG_MAX_NEWTON_STEPS 32
+typedef struct {
+    int32_t rows, cols;
+    int32_t dtype, out_dtype;
+    int32_t steps;
+    float eps; /* >= 0 */
+    const float *coefficients; /* host, [steps][3] */
+    const void *d_G;
+    int64_t ld_G;
+    void *d_O;
+    int64_t ld_O;
+} zg_orthogonalize_args;
+int zg_orthogonalize_workspace(const zg_orthogonalize_args *a, size_t *bytes);
+int zg_orthogonalize(const zg_orthogonalize_args *a, void *d_workspace, size_t workspace_bytes, void *stream);
+
+/* An update of weights by their orthogonalised momentum:
+ *   M <- momentum M + G,   U = momentum M + G where nesterov is not 0, else M,   W <- (1 - lr decay) W - lr scale orthogonalize(U).
+ * W: [rows, cols] of type dtype, G of type grad_dtype, M of fp32; none of them may lie on another.  The products are as exact as zg_orthogonalize's for a result of W's type; W is rounded once. */
+typedef struct {
+    int32_t rows, cols;
+    int32_t dtype, grad_dtype;
+    int32_t steps, nesterov;
+    float lr, momentum, decay, scale;
+    float eps, reserved;
+    const float *coefficients; /* host, [steps][3] */
+    const void *d_G;
+    int64_t ld_G;
+    float *d_M;
+    int64_t ld_M;
+    void *d_W;
+    int64_t ld_W;
+} zg_muon_args;
+int zg_muon_step_workspace(const zg_muon_args *a, size_t *bytes);
+int zg_muon_step(const zg_muon_args *a, void *d_workspace, size_t workspace_bytes, void *stream);
+
 /* ---- measurement helpers ----------------------------------------------------------------------
  * Identifier of the sources the library was built from (a hash the build step passes in); lets a caller
  * detect a stale binary.  Library-owned string. */

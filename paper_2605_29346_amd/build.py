@@ -12,7 +12,8 @@ from typing import Optional
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libzg.so")
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("zg_host.cpp", "zg_device.hip", "zg_rows.hip", "zg_linear.hip", "zg_loss.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("zg_host.cpp", "zg_device.hip", "zg_rows.hip", "zg_linear.hip", "zg_loss.hip",
+                                                         "zg_orthogonal.hip")]
 HEADERS = [os.path.join(HERE, "csrc", "zg_internal.h"), os.path.join(HERE, "csrc", "zg_floyd.h"),
            os.path.join(HERE, "csrc", "zg_dense.h"), os.path.join(HERE, "csrc", "zg_product.h"), os.path.join(ROOT, "include", "zg.h")]
 

@@ -119,6 +119,7 @@ template <int FM, int FN> __device__ __forceinline__ void tops(const TopArgs &p,
 }
 
 template <> struct Out<TopArgs> {
+    static constexpr bool turns = false;
     template <class O, bool PLAIN, int FM> __device__ __forceinline__ static void wide(const TopArgs &p, f32x16 (&acc)[FM][2], f32x4 *, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t)
     {
         tops(p, acc, m_wave, n_wave, M);
@@ -376,6 +377,7 @@ template <class T, int FM, int FN> __device__ __forceinline__ void hand_over_dz(
 }
 
 template <class T> struct Out<DzArgs<T>> {
+    static constexpr bool turns = false;
     template <class O, bool PLAIN, int FM> __device__ __forceinline__ static void wide(const DzArgs<T> &p, f32x16 (&acc)[FM][2], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t)
     {
         hand_over_dz(p, acc, mine, m_wave, n_wave, M);

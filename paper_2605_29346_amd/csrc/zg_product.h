@@ -45,7 +45,7 @@ struct ProductArgs {
     Epilogue e;
 
     static constexpr bool symmetric = false; // C is, and only tiles that reach down to its diagonal are made
-    static constexpr int segments = 1;       // products over K that are summed, each of other planes of the operands
+    static constexpr int segments = 1;       // products over K that are summed: of other planes of the operands (plane_a, plane_b: bytes from p to them)
 };
 
 // any product with an epilogue, through zg_linear.hip's kernels; `part`: room for splits x M x N sums where there are parts
@@ -433,6 +433,7 @@ template <class O, bool PLAIN, int FM, int FN> __device__ __forceinline__ void h
 
 // What becomes of the sums of a product with these Args.
 template <class Args> struct Out {
+    static constexpr bool turns = false; // (of k_few's kind: whether results go out a second time, turned)
     template <class O, bool PLAIN, int FM> __device__ __forceinline__ static void wide(const Args &p, f32x16 (&acc)[FM][2], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M, uint32_t split)
     {
         hand_over<O, PLAIN>(p, acc, mine, m_wave, n_wave, M, split);
@@ -459,6 +460,13 @@ struct Place {
     uint32_t m0, n0, split, k_first, k_end;
 };
 
+// number t of the tiles on and below the diagonal: row r of tiles has r + 1 of them (the root is right to a unit in the last place, t < 2^21)
+__device__ __forceinline__ uint32_t row_of_triangle(uint32_t t)
+{
+    const uint32_t row = (uint32_t)((__builtin_amdgcn_sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+    return row * (row + 1) / 2 > t ? row - 1 : (row + 1) * (row + 2) / 2 <= t ? row + 1 : row;
+}
+
 template <int BM, int BN, bool SYMMETRIC = false> struct Tiles {
     uint32_t M, k_all, nt, splits, part_k;
     uint64_t in_part, next, end; // of this workgroup: the next tile, the end of its XCD's run
@@ -484,11 +492,9 @@ template <int BM, int BN, bool SYMMETRIC = false> struct Tiles {
         const auto same = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane(v); };
         w.split = splits > 1 ? same((uint32_t)(next / in_part)) : 0u;
         const uint32_t t = same((uint32_t)(next - w.split * in_part));
-        if constexpr (SYMMETRIC) { // row r of tiles has r + 1 of them (the root is right to a unit in the last place, t < 2^21)
+        if constexpr (SYMMETRIC) {
             static_assert(BM == BN, "");
-            uint32_t row = (uint32_t)((__builtin_amdgcn_sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
-            row = row * (row + 1) / 2 > t ? row - 1 : (row + 1) * (row + 2) / 2 <= t ? row + 1 : row;
-            row = same(row);
+            const uint32_t row = same(row_of_triangle(t));
             w.m0 = row * BM;
             w.n0 = (t - row * (row + 1) / 2) * BN;
         } else {
@@ -927,7 +933,8 @@ template <class T, class Args> __device__ __forceinline__ void few_tile(const Ar
     constexpr int K = chunk_k<T>, ahead = 4, stride = 36; // floats to a row of LDS: rows start in different groups of banks
     __shared__ float lds[4][32 * stride];
     const uint32_t live = min(p.M, p.rows.live()), nt = (p.N + 31) / 32;
-    const uint32_t number = block_number(), m0 = number / nt * 32, n0 = number % nt * 32;
+    const uint32_t number = block_number(), tile_row = Args::symmetric ? row_of_triangle(number) : number / nt;
+    const uint32_t m0 = tile_row * 32, n0 = (number - (Args::symmetric ? tile_row * (tile_row + 1) / 2 : tile_row * nt)) * 32;
     if (m0 >= live) return;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     Along<T> a, b;
@@ -938,30 +945,66 @@ template <class T, class Args> __device__ __forceinline__ void few_tile(const Ar
     typename Out<Args>::Few out;
     out.begin(p, row < 32 ? m0 + row : live, n0 + 8 * group, live);
     f32x16 acc = {};
-    for (uint32_t k0 = wave * 2 * K; k0 < p.K; k0 += ahead * 8 * K) {
-        u32x4 x[ahead], y[ahead];
+    if constexpr (Args::segments == 1) {
+        for (uint32_t k0 = wave * 2 * K; k0 < p.K; k0 += ahead * 8 * K) {
+            u32x4 x[ahead], y[ahead];
 #pragma unroll
-        for (int i = 0; i < ahead; ++i) {
-            const uint32_t k = k0 + i * 8 * K + half * K;
-            x[i] = a.at(k);
-            y[i] = b.at(k);
+            for (int i = 0; i < ahead; ++i) {
+                const uint32_t k = k0 + i * 8 * K + half * K;
+                x[i] = a.at(k);
+                y[i] = b.at(k);
+            }
+#pragma unroll
+            for (int i = 0; i < ahead; ++i) multiply(T(), y[i], x[i], acc);
         }
+    } else { // pairs: the high planes at p, the low ones behind
+        Along<T> la = a, lb = b;
+        la.row = reinterpret_cast<const T *>(reinterpret_cast<const char *>(a.row) + p.plane_a(0));
+        lb.row = reinterpret_cast<const T *>(reinterpret_cast<const char *>(b.row) + p.plane_b(2));
+        for (uint32_t k0 = wave * 2 * K; k0 < p.K; k0 += ahead * 8 * K) {
+            u32x4 x[ahead], y[ahead], lx[ahead], ly[ahead];
 #pragma unroll
-        for (int i = 0; i < ahead; ++i) multiply(T(), y[i], x[i], acc);
+            for (int i = 0; i < ahead; ++i) {
+                const uint32_t k = k0 + i * 8 * K + half * K;
+                x[i] = a.at(k), y[i] = b.at(k);
+                lx[i] = la.at(k), ly[i] = lb.at(k);
+            }
+#pragma unroll
+            for (int i = 0; i < ahead; ++i) {
+                multiply(T(), y[i], lx[i], acc);
+                multiply(T(), ly[i], x[i], acc);
+                multiply(T(), y[i], x[i], acc);
+            }
+        }
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q)
         *reinterpret_cast<f32x4 *>(&lds[wave][(lane & 31) * stride + 8 * q + 4 * half]) = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
     __syncthreads();
-    if (row >= 32) return;
-    out.end(p, m0 + row, live, [&](int, float(&v)[8]) {
+    const auto sums = [&](int, float(&v)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = 0.0f;
 #pragma unroll
         for (int w = 0; w < 4; ++w)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += lds[w][row * stride + 8 * group + j];
-    });
+    };
+    if constexpr (Out<Args>::turns) { // the results go out turned, too
+        float v[8];
+        if (row < 32) {
+            out.end(p, m0 + row, live, sums, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) lds[0][row * stride + 8 * group + j] = v[j]; // (a lane's own cells)
+        }
+        __syncthreads();
+        if (row >= 32 || (Args::symmetric && m0 == n0)) return;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = lds[0][(8 * group + j) * stride + row];
+        out.turned(p, n0 + row, m0 + 8 * group, v);
+    } else {
+        if (row >= 32) return;
+        out.end(p, m0 + row, live, sums);
+    }
 }
 
 // ---- which kernel takes a product ------------------------------------------------------------------------------------------------

@@ -8,6 +8,7 @@ it); nothing synchronises.  Autograd does not see the calls: operands that requi
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import struct
 from dataclasses import dataclass
 from typing import NamedTuple, Optional
@@ -50,8 +51,9 @@ class LossResult(NamedTuple):
 _DROP = "dQIIq"
 _PACK = {"zg_linear": "@qq6i13q" + _DROP, "zg_linear_backward": "@qq6i13q" + _DROP, "zg_dropout": "@qq2i6q" + _DROP,
          "zg_rms_norm": "@qq3if11q" + _DROP, "zg_rms_norm_backward": "@qq2i13q" + _DROP,
-         "zg_linear_cross_entropy": "@qq4i11q", "zg_linear_cross_entropy_backward": "@qq4i15q"}
-_WITH_WORKSPACE = {name for name in _PACK if name.endswith("_backward")} | {"zg_linear_cross_entropy"}
+         "zg_linear_cross_entropy": "@qq4i11q", "zg_linear_cross_entropy_backward": "@qq4i15q", "zg_orthogonalize": "@5if5q",
+         "zg_muon_step": "@6i6f7q"}
+_WITH_WORKSPACE = {name for name in _PACK if name.endswith("_backward")} | {"zg_linear_cross_entropy", "zg_orthogonalize", "zg_muon_step"}
 _pack = {name: struct.Struct(f).pack for name, f in _PACK.items()}
 _entries: dict = {}
 
@@ -332,3 +334,52 @@ def linear_cross_entropy_backward(a, w, labels, lse, *, bias=None, weight=None, 
                                               _vector(weight, "weight", m, _F32, device), _vector(lse, "lse", m, _F32, device), _vector(total, "total", 1, _F32, device),
                                               _vector(dloss, "dloss", 1, _F32, device), da_at, ld_da, dw_at, ld_dw, db_at), device, stream, made, workspace=True)
     return da, dw, dbias
+
+
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)  # takes singular values from 0.02 on into 0.7 .. 1.2 in five steps
+
+
+@functools.lru_cache(maxsize=64)
+def _coefficients(coefficients, steps):
+    """Host floats [steps][3] of one triple, or of a triple for each step."""
+    each = coefficients if coefficients and isinstance(coefficients[0], tuple) else (coefficients,) * steps
+    if len(each) != steps or any(len(k) != 3 for k in each):
+        raise ValueError(f"coefficients are {coefficients}: (a, b, c), or one such triple for each of {steps} steps, is wanted")
+    return (C.c_float * (3 * steps))(*(float(v) for k in each for v in k))
+
+
+def _steps(coefficients, steps):
+    if not isinstance(steps, int) or not 1 <= steps <= zg.MAX_NEWTON_STEPS:
+        raise ValueError(f"steps is {steps!r}: 1..{zg.MAX_NEWTON_STEPS} is wanted")
+    coefficients = tuple(coefficients)
+    return _coefficients(tuple(map(tuple, coefficients)) if coefficients and not isinstance(coefficients[0], (int, float)) else coefficients, steps)
+
+
+def orthogonalize(g, *, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, out_dtype=None, out=None, stream=None):
+    """g / (|g| + eps) after `steps` Newton-Schulz steps x <- a x + b (x x^T) x + c (x x^T)^2 x, which bring its singular values near one; `coefficients`: (a, b, c), or a triple
+    for each step.  Result of `out_dtype` (default: g's type); `out` may be g.  Products are made of 22 significant bits (fp16 operands for a bfloat16 result of 256 rows and columns or more in at
+    most 6 steps), their sums in 32."""
+    _no_history(g)
+    (m, n), device = _shape(g, "g")
+    dtype = g.dtype
+    kind = out_dtype or (out.dtype if out is not None else dtype)
+    k = _steps(coefficients, steps)
+    made = []
+    out, at, ld = _out(out, "out", m, n, kind, device, made, g if kind is dtype else None)
+    _run("zg_orthogonalize", (m, n, _type(dtype, "g"), _type(kind, "out_dtype"), steps, eps, C.addressof(k), *_matrix(g, "g", m, n, dtype, device), at, ld), device, stream, made,
+         workspace=True)
+    return out
+
+
+def muon_step(w, m, g, *, lr, momentum=0.95, nesterov=True, decay=0.0, scale=None, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, stream=None):
+    """Updates a layer's weights w and their momentum m (float32) in place: m <- momentum m + g, u = momentum m + g (`nesterov`) or m,
+    w <- (1 - lr decay) w - lr scale orthogonalize(u).  scale: default max(1, rows / cols) ** 0.5.  Returns w."""
+    _no_history(w, m, g)
+    (rows, cols), device = _shape(w, "w")
+    k = _steps(coefficients, steps)
+    if scale is None:
+        scale = max(1.0, rows / cols) ** 0.5
+    _run("zg_muon_step", (rows, cols, _type(w.dtype, "w"), _type(g.dtype, "g"), steps, int(nesterov), lr, momentum, decay, scale, eps, 0.0, C.addressof(k),
+                          *_matrix(g, "g", rows, cols, g.dtype, device), *_matrix(m, "m", rows, cols, _F32, device), *_matrix(w, "w", rows, cols, w.dtype, device)),
+         device, stream, workspace=True)
+    return w

@@ -19,7 +19,7 @@ OK, EINVAL, ENOMEM, EHIP, ESTATE = 0, -1, -2, -3, -4
 I32, I64 = 0, 1
 F32, F16, BF16, F8 = 2, 3, 4, 5
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
-MAX_WIDTH, MAX_NORM_WIDTH, MAX_CLASSES = 32768, 16384, 1 << 24
+MAX_WIDTH, MAX_NORM_WIDTH, MAX_CLASSES, MAX_NEWTON_STEPS = 32768, 16384, 1 << 24, 32
 GRAPH_VALIDATE = 1
 PLAN_EAGER, PLAN_REPLACE, PLAN_SAFE_TWIN, PLAN_FUSED_INPUT, PLAN_AUTO_FALLBACK = 1, 2, 4, 8, 16
 PLAN_X_ONE_PASS, PLAN_X_TWO_PASS = 32, 64
@@ -42,7 +42,8 @@ EXPORTS = ["zg_strerror", "zg_last_error", "zg_graph_create", "zg_graph_create_s
            "zg_calibration_copy", "zg_envelope_model_graph_static", "zg_plan_replay_features", "zg_step_timed",
            "zg_linear", "zg_linear_backward_workspace", "zg_linear_backward", "zg_dropout", "zg_rms_norm",
            "zg_rms_norm_backward_workspace", "zg_rms_norm_backward", "zg_linear_cross_entropy_workspace", "zg_linear_cross_entropy",
-           "zg_linear_cross_entropy_backward_workspace", "zg_linear_cross_entropy_backward"]
+           "zg_linear_cross_entropy_backward_workspace", "zg_linear_cross_entropy_backward", "zg_orthogonalize_workspace", "zg_orthogonalize",
+           "zg_muon_step_workspace", "zg_muon_step"]
 
 
 class Envelope(C.Structure):
@@ -123,6 +124,15 @@ class LossGradArgs(C.Structure):
         ("d_" + n, C.c_void_p) for n in ("bias", "labels", "weight", "lse", "total", "dloss")] + _matrices("dA", "dW") + [("d_dbias", C.c_void_p)]
 
 
+class OrthogonalizeArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "cols", "dtype", "out_dtype", "steps")] + [("eps", C.c_float), ("coefficients", C.c_void_p)] + _matrices("G", "O")
+
+
+class MuonArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "cols", "dtype", "grad_dtype", "steps", "nesterov")] + [
+        (n, C.c_float) for n in ("lr", "momentum", "decay", "scale", "eps", "reserved")] + [("coefficients", C.c_void_p)] + _matrices("G", "M", "W")
+
+
 _lib = None
 
 
@@ -188,6 +198,10 @@ def lib() -> C.CDLL:
         L.zg_linear_cross_entropy.argtypes = [P(LossArgs), vp, C.c_size_t, vp]
         L.zg_linear_cross_entropy_backward_workspace.argtypes = [P(LossGradArgs), P(C.c_size_t)]
         L.zg_linear_cross_entropy_backward.argtypes = [P(LossGradArgs), vp, C.c_size_t, vp]
+        L.zg_orthogonalize_workspace.argtypes = [P(OrthogonalizeArgs), P(C.c_size_t)]
+        L.zg_orthogonalize.argtypes = [P(OrthogonalizeArgs), vp, C.c_size_t, vp]
+        L.zg_muon_step_workspace.argtypes = [P(MuonArgs), P(C.c_size_t)]
+        L.zg_muon_step.argtypes = [P(MuonArgs), vp, C.c_size_t, vp]
         for name in EXPORTS:
             if name not in ("zg_strerror", "zg_last_error", "zg_normal_quantile", "zg_build_id"):
                 getattr(L, name).restype = C.c_int

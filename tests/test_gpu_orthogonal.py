@@ -1,0 +1,87 @@
+"""Orthogonalised matrices and updates on the GPU against the steps in 64 bits (orthogonal_util), at the sizes, shapes, strides and values where they can go wrong."""
+import zlib
+
+import pytest
+import torch
+
+import orthogonal_util as O
+from paper_2605_29346_amd import layers, zg
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+SENTINEL = 77.0
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    zg.lib()
+
+
+def _gen(*key):
+    return torch.Generator(device="cuda").manual_seed(zlib.crc32(repr(key).encode()))  # (the same in every process)
+
+
+def _matrix(g, rows, cols, kind, pad=0, shift=0, scale=1.0):
+    flat = (torch.randn(rows * (cols + pad) + shift, device="cuda", generator=g) * scale).to(kind)
+    return flat[shift:].view(rows, cols + pad)[:, :cols]
+
+
+def _buffer(rows, cols, kind, pad=0):
+    whole = torch.full((rows + 2, cols + pad), SENTINEL, device="cuda").to(kind)
+    return whole, whole[1:-1, :cols]
+
+
+def _untouched(whole, rows, cols, what):
+    ok = torch.full_like(whole[:1, :1].float(), SENTINEL).to(whole.dtype)
+    for part in (whole[:1], whole[1 + rows:], whole[:, cols:]):
+        assert bool((part == ok).all()), f"{what}: something was written outside"
+
+
+SIZES = [  # rows, cols, pad, shift
+    (1, 1, 0, 0), (1, 50, 0, 0), (50, 1, 1, 1), (2, 3, 0, 0), (7, 5, 1, 0), (16, 16, 0, 0), (31, 33, 3, 1), (33, 31, 0, 0), (47, 256, 0, 0), (64, 64, 8, 0), (100, 1000, 0, 0), (1000, 100, 0, 0),
+    (255, 255, 1, 1), (256, 256, 0, 0), (257, 300, 0, 0), (300, 257, 2, 3), (600, 1201, 3, 0), (1201, 600, 0, 0), (8, 4096, 0, 0), (1025, 1100, 0, 0), (1536, 1280, 0, 0)]
+
+
+@pytest.mark.parametrize("kinds", [(F32, F32), (F16, F16), (BF16, BF16), (F32, BF16), (BF16, F32)], ids=str)
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_orthogonalize(size, kinds):
+    rows, cols, pad, shift = size
+    kind, out = kinds
+    m = _matrix(_gen(size, str(kinds)), rows, cols, kind, pad, shift, 1e-3)
+    whole, o = _buffer(rows, cols, out, pad)
+    got = layers.orthogonalize(m, out_dtype=out, out=o)
+    assert got is o
+    O.check(o, m, out)
+    _untouched(whole, rows, cols, "o")
+
+
+@pytest.mark.parametrize("kinds", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)], ids=str)  # of w and of g
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_muon_step(size, kinds):
+    rows, cols, pad, shift = size
+    kind, grad = kinds
+    gen = _gen(size, str(kinds), "muon")
+    g, m = _matrix(gen, rows, cols, grad, pad, shift), _matrix(gen, rows, cols, F32, pad, shift, 3.0)
+    for nesterov, lr, decay, scale in ((True, 0.02, 0.1, None), (False, 0.5, 0.0, 0.25)):
+        whole_w, w = _buffer(rows, cols, kind, pad)
+        whole_m, mm = _buffer(rows, cols, F32, pad)
+        w.copy_(_matrix(gen, rows, cols, kind, scale=cols**-0.5))
+        mm.copy_(m)
+        before = w.double()
+        layers.muon_step(w, mm, g, lr=lr, momentum=0.9, nesterov=nesterov, decay=decay, scale=scale)
+        momentum = torch.tensor(0.9, device="cuda")
+        new = momentum * m + g.float()
+        assert torch.equal(mm, new)
+        u = momentum * new + g.float() if nesterov else new
+        s = max(1.0, rows / cols) ** 0.5 if scale is None else scale
+        want = (1 - lr * decay) * before - lr * s * O.exact(u)
+        off = lr * s * (O.emulated(u, kind) - O.exact(u)).norm()
+        err = (w.double() - want).abs() - O.U[kind] * want.abs()
+        cells = want.numel() ** 0.5
+        assert float(err.max()) <= float(O.CELL * off / cells + 4 * 2.0**-24 * (before.abs().max() + lr * s * 1.3))
+        assert float(err.clamp_min(0).norm()) <= float(O.SLACK * off + 4 * 2.0**-24 * (before.norm() + lr * s * cells))
+        _untouched(whole_w, rows, cols, "w")
+        _untouched(whole_m, rows, cols, "m")
