@@ -1,10 +1,10 @@
 // A matrix whose singular values are brought near one by Newton-Schulz products, and the weights' update that uses it.
 //
-// X = G / (|G| + eps); a step is A = X X^T, B = b A + c A^2, X = a X + B X (on the shorter side; X^T X and X B where G is tall): singular values s become a s + b s^3 + c s^5.
-// Between the steps X is held as two fp16 planes (x = high + low: 22 bits) at a power of two, once as G lies (P) and once turned (Q), so that every product's operands lie along their sums:
-//   wide:  A = P P^T,  P' = a P + B Q^T        tall:  A = Q Q^T,  P' = a P + P B^T        (B is symmetric)
-// and leaves its tile turned beside itself.  A and B are symmetric: only the tiles that reach down to the diagonal are made, and go out mirrored.  A bfloat16 result is made with the high planes as operands
-// (one rounding of 2^-12 of each); others with both planes of both operands, three products: high x high, high x low and low x high.
+// X = G / (|G| + eps), turned where G is tall; a step is A = X X^T, B = b A + c A^2, X = a X + B X: singular values s become a s + b s^3 + c s^5.
+// Between the products X, A and B are held as fp16 planes (x = high + low: 22 bits) at a power of two; X always has both, as it is added to what the products make of it.  A bfloat16 result is made with the
+// high planes as operands (one rounding of 2^-12 of each); others with both planes of both operands, three products: low x high, high x low and high x high.  A and B are symmetric: only
+// the tiles that reach down to the diagonal are made, and go out mirrored.  The sums of B X run across the rows of X: tiles of 256 x 256 turn them as they are read from LDS, smaller ones, which that would
+// hold up (1024 x 4096: 24 -> 30 us; pairs of 1024 x 2048 in tiles of 64 x 64: 27 -> 48), have X turned beside it.
 #include "zg_product.h"
 
 namespace zg {
@@ -14,7 +14,7 @@ typedef _Float16 f16;
 
 // ---- the products -----------------------------------------------------------------------------------------------------------------
 
-// What a product is for: A or B (symmetric), X between two steps (goes out turned, too), or the result.
+// What a product is for: A or B (symmetric), X between two steps, or the result.
 enum { kSquare, kStep, kResult };
 
 template <int SEGMENTS, int KIND> struct StepArgs : ProductArgs { // v = alpha sum + beta R
@@ -26,17 +26,17 @@ template <int SEGMENTS, int KIND> struct StepArgs : ProductArgs { // v = alpha s
     int64_t ld_R;
     f16 *H, *L; // v's planes; L may be null
     int64_t ld_H;
-    f16 *TH, *TL; // the same turned (of kSquare: H and L); TL may be null
+    f16 *TH, *TL; // the same turned (kSquare: H and L); TL may be null, of kStep TH, too
     int64_t ld_T;
-    void *O; // kResult: O = v, or O = keep O + v
+    void *O; // kResult: O = v, or O = keep O + v, turned where G is tall
     int64_t ld_O;
     int32_t type_O;
-    bool update;
+    bool update, turn;
     float keep;
 
-    // low x high, high x high, high x low
+    // low x high, high x low, high x high: the sums are small until the last
     __device__ __forceinline__ int64_t plane_a(int segment) const { return segment == 0 ? low_a : 0; }
-    __device__ __forceinline__ int64_t plane_b(int segment) const { return segment == 2 ? low_b : 0; }
+    __device__ __forceinline__ int64_t plane_b(int segment) const { return segment == 1 ? low_b : 0; }
 };
 
 // eight cells' planes; zeros behind the first n
@@ -53,10 +53,9 @@ __device__ __forceinline__ void put_planes(f16 *h, f16 *l, int64_t at, int n, co
     if (l) __builtin_memcpy(l + at, low, 16);
 }
 
-// cells (m, n .. n + 7) from their sums to where they go; v becomes what they are
-template <int SEGMENTS, int KIND> __device__ __forceinline__ void step8(const StepArgs<SEGMENTS, KIND> &p, uint32_t m, uint32_t n, float (&v)[8])
+// v of cells (m, n .. n + 7) from their sums
+template <class Args> __device__ __forceinline__ void value8(const Args &p, uint32_t m, uint32_t n, float (&v)[8])
 {
-    const int left = (int)(p.N - n);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] *= p.alpha;
     if (p.R) { // (its rows are whole chunks)
@@ -66,18 +65,35 @@ template <int SEGMENTS, int KIND> __device__ __forceinline__ void step8(const St
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = fmaf(p.beta, r[j], fmaf(p.beta, l[j], v[j]));
     }
-    if constexpr (KIND == kResult) {
-        if (p.update) {
-            float w[8];
-            load8(p.O, p.type_O, m * p.ld_O + n, left, w);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = fmaf(p.keep, w[j], v[j]);
-        }
-        store8(p.O, p.type_O, m * p.ld_O + n, left, v);
-    } else {
-        put_planes(p.H, p.L, m * p.ld_H + n, left, v);
-    }
 }
+
+// v of eight cells of a row of O, the first `left` of which there are
+template <class Args> __device__ __forceinline__ void result8(const Args &p, uint32_t row, uint32_t col, int left, float (&v)[8])
+{
+    if (p.update) {
+        float w[8];
+        load8(p.O, p.type_O, row * p.ld_O + col, left, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = fmaf(p.keep, w[j], v[j]);
+    }
+    store8(p.O, p.type_O, row * p.ld_O + col, left, v);
+}
+
+template <int SEGMENTS, int KIND> __device__ __forceinline__ void straight8(const StepArgs<SEGMENTS, KIND> &p, uint32_t m, uint32_t n, float (&v)[8])
+{
+    value8(p, m, n, v);
+    if constexpr (KIND != kResult) put_planes(p.H, p.L, m * p.ld_H + n, (int)(p.N - n), v);
+    else if (!p.turn) result8(p, m, n, (int)(p.N - n), v);
+}
+
+// cells (m .. m + 7, n)
+template <int SEGMENTS, int KIND> __device__ __forceinline__ void turned8(const StepArgs<SEGMENTS, KIND> &p, uint32_t m, uint32_t n, float (&v)[8])
+{
+    if constexpr (KIND != kResult) put_planes(p.TH, p.TL, n * p.ld_T + m, (int)(p.M - m), v);
+    else result8(p, n, m, (int)(p.M - m), v);
+}
+
+template <class Args> __device__ __forceinline__ bool goes_turned(const Args &p) { return p.TH || p.turn; }
 
 // Through LDS of 4 KB, 32 x 32 cells at a time: four lanes have 32 columns of a row, then four lanes have 32 rows of a column.
 template <int SEGMENTS, int KIND, int FM, int FN>
@@ -101,10 +117,10 @@ __device__ __forceinline__ void hand_over_step(const StepArgs<SEGMENTS, KIND> &p
                 const f32x4 lo = mine[r * 8 + ((2 * g) ^ ((r >> 1) & 7))], hi = mine[r * 8 + ((2 * g + 1) ^ ((r >> 1) & 7))];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[u][k] = lo[k], v[u][4 + k] = hi[k];
-                if (m0 + r < p.M && n0 + 8 * g < p.N) step8(p, m0 + r, n0 + 8 * g, v[u]);
+                if (m0 + r < p.M && n0 + 8 * g < p.N) straight8(p, m0 + r, n0 + 8 * g, v[u]);
             }
             lds_exchange();
-            if (KIND != kResult && !(KIND == kSquare && m0 == n0)) {
+            if (KIND == kSquare ? m0 != n0 : goes_turned(p)) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const uint32_t r = (lane >> 2) + 16 * u;
@@ -122,7 +138,7 @@ __device__ __forceinline__ void hand_over_step(const StepArgs<SEGMENTS, KIND> &p
                         const uint32_t r = 8 * g + k;
                         t[k] = cells[(r * 8 + ((c >> 2) ^ ((r >> 1) & 7))) * 4 + (c & 3)];
                     }
-                    if (n0 + c < p.N && m0 + 8 * g < p.M) put_planes(p.TH, p.TL, (n0 + c) * p.ld_T + m0 + 8 * g, (int)(p.M - m0 - 8 * g), t);
+                    if (n0 + c < p.N && m0 + 8 * g < p.M) turned8(p, m0 + 8 * g, n0 + c, t);
                 }
                 lds_exchange();
             }
@@ -132,7 +148,7 @@ __device__ __forceinline__ void hand_over_step(const StepArgs<SEGMENTS, KIND> &p
 
 template <int SEGMENTS, int KIND> struct Out<StepArgs<SEGMENTS, KIND>> {
     using Args = StepArgs<SEGMENTS, KIND>;
-    static constexpr bool turns = KIND != kResult;
+    static constexpr bool turns = true;
     template <class O, bool PLAIN, int FM> __device__ __forceinline__ static void wide(const Args &p, f32x16 (&acc)[FM][2], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t, uint32_t)
     {
         hand_over_step(p, acc, mine, m_wave, n_wave);
@@ -147,23 +163,23 @@ template <int SEGMENTS, int KIND> struct Out<StepArgs<SEGMENTS, KIND>> {
         template <class F> __device__ __forceinline__ void end(const Args &p, uint32_t m, uint32_t live, F &&sums, float (&v)[8])
         {
             sums(0, v);
-            if (m < live && n < p.N) step8(p, m, n, v);
-        }
-        template <class F> __device__ __forceinline__ void end(const Args &p, uint32_t m, uint32_t live, F &&sums)
-        {
-            float v[8];
-            end(p, m, live, sums, v);
+            if (m < live && n < p.N) straight8(p, m, n, v);
         }
         __device__ __forceinline__ void turned(const Args &p, uint32_t c, uint32_t m, float (&v)[8])
         {
-            if (c < p.N && m < p.M) put_planes(p.TH, p.TL, c * p.ld_T + m, (int)(p.M - m), v);
+            if (goes_turned(p) && c < p.N && m < p.M) turned8(p, m, c, v);
         }
     };
 };
 
+// Tiles of 64 x 64: four wavefronts, three workgroups to a compute unit, or two groups of four that share a tile's sums, one to a compute unit; of 128 x 128: one to a compute unit, four steps of
+// 128 bytes on their way, or three with three of 64; of 256 x 256.  (What each is for, and what it takes, stands at time_of.)
 template <int SEGMENTS, int KIND> __global__ __launch_bounds__(256) void k_step_few(StepArgs<SEGMENTS, KIND> p) { few_tile<f16>(p); }
-template <int SEGMENTS, int KIND> __global__ __launch_bounds__(256, 3) void k_step_chunks(StepArgs<SEGMENTS, KIND> p) { chunks_tile<f16, f16, 128, 128, false, false>(p); }
-template <int SEGMENTS, int KIND> __global__ __launch_bounds__(512, 2) void k_step_long(StepArgs<SEGMENTS, KIND> p) { long_tiles<f16, f16, false, false>(p); }
+template <int SEGMENTS> __global__ __launch_bounds__(512, 1) void k_step_shared(StepArgs<SEGMENTS, kSquare> p) { chunks_tile<f16, f16, 64, 64, false, false, 8, 3, 2>(p); }
+template <int SEGMENTS, int KIND> __global__ __launch_bounds__(256, 3) void k_step_64(StepArgs<SEGMENTS, KIND> p) { chunks_tile<f16, f16, 64, 64, false, false, 8, 3>(p); }
+template <int SEGMENTS, int KIND> __global__ __launch_bounds__(256, 1) void k_step_128(StepArgs<SEGMENTS, KIND> p) { chunks_tile<f16, f16, 128, 128, false, false, 8, 4>(p); }
+template <int SEGMENTS, int KIND> __global__ __launch_bounds__(256, 3) void k_step_dense(StepArgs<SEGMENTS, KIND> p) { chunks_tile<f16, f16, 128, 128, false, false>(p); }
+template <int SEGMENTS, int KIND> __global__ __launch_bounds__(512, 2) void k_step_256(StepArgs<SEGMENTS, KIND> p) { long_tiles<f16, f16, false, KIND != kSquare>(p); }
 
 // ---- what the steps begin with ------------------------------------------------------------------------------------------------------
 
@@ -178,8 +194,8 @@ struct StartArgs {
     double eps;
     double *sums; // [workgroups of k_start_norm]
     uint32_t n_sums;
-    float power; // of two, that P and Q are held with
-    f16 *P, *P_low, *Q, *Q_low; // Q_low may be null
+    float power; // of two, that the planes are held with
+    f16 *P, *P_low, *Q, *Q_low; // the matrix' planes, and those of it turned: any may be null
     int64_t ld_P, ld_Q;
 };
 
@@ -239,7 +255,7 @@ template <class T> __global__ __launch_bounds__(256) void k_start_norm(StartArgs
     if (threadIdx.x == 0) a.sums[blockIdx.x] = lds[0];
 }
 
-// P and Q: 64 x 64 elements to a workgroup, turned through LDS.
+// The planes: 64 x 64 elements to a workgroup, turned through LDS.
 template <class T> __global__ __launch_bounds__(256) void k_start_planes(StartArgs a)
 {
     __shared__ double sums[256];
@@ -263,11 +279,12 @@ template <class T> __global__ __launch_bounds__(256) void k_start_planes(StartAr
             start8<T>(a, r0 + r, c0 + c, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = (float)((double)v[j] * factor);
-            put_planes(a.P, a.P_low, (uint64_t)(r0 + r) * a.ld_P + c0 + c, (int)(a.cols - c0 - c), v);
+            if (a.P) put_planes(a.P, a.P_low, (uint64_t)(r0 + r) * a.ld_P + c0 + c, (int)(a.cols - c0 - c), v);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) lds[r][c + j] = v[j];
     }
+    if (!a.Q) return;
     __syncthreads();
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -337,13 +354,49 @@ int check_steps(const Common &c)
     return ZG_OK;
 }
 
+// How a product is made, and about how long that takes, in us, as measured on an MI355X: `k` terms, a pair's three products being three times as many; small tiles' cost is what they read, once a
+// pair's two planes.  fp16, [M, N] x K terms, few / 64 / shared / 128 / dense / 256: symmetric 256 x 256 4.3 / 4.8 / 5.1 / 9 / 9 / 14; 512 x 512 5.4 / 5.9 / 5.9 / 11 / 11 / 20;
+// 1024 x 1024 14 / 8.2 / 7.8 / 15 / 16 / 30, over 4096 terms 48 / 21 / 16 / 36 / 41 / 82; 2048 73 / 23 / 30 / 24 / 25 / 49; 4096 557 / 154 / - / 127 / 128 / 101;
+// whole 1024 x 2048 x 1024 36 / 14 / 20 / 20 / 21 / 37; 1024 x 4096 x 1024 67 / 27 / 37 / 24 / 24 / 39; 2048 x 2048 x 2048 128 / 41 / 54 / 32 / 33 / 58; 4096 1019 / 314 / - / 211 / 218 / 161.
+enum Way { kFew, kShared, k64, k128, kDense, k256, kWays };
+
+uint64_t tiles_of(uint32_t M, uint32_t N, bool symmetric, uint32_t tile)
+{
+    const uint64_t m = (M + tile - 1) / tile, n = (N + tile - 1) / tile;
+    return symmetric ? n * (n + 1) / 2 : m * n;
+}
+
+double time_of(Way way, uint32_t M, uint32_t N, uint32_t K, bool symmetric, bool pairs)
+{
+    const double k = (double)K * (pairs ? 3 : 1);
+    const auto tiles = [&](uint32_t tile) { return (double)tiles_of(M, N, symmetric, tile); };
+    switch (way) {
+    case kFew: return 3.2 + tiles(32) * (1.3e-3 + (tiles(32) > 1024 ? 1.8e-6 : 2.5e-6) * 8.0 * K * (pairs ? 2 : 1));
+    case kShared: return symmetric && tiles(64) <= 256 ? 5.0 + 2.9e-3 * k : 1e30;
+    case k64: return 5.0 + k * std::max(3.9e-3, 5.0e-3 * tiles(64) / 256);
+    case k128: return tiles(128) <= 256 ? 6.0 + k * (7.4e-3 + 7.0e-3 * tiles(128) / 256) : 1e30;
+    case kDense: return 6.0 + k * 15.0e-3 * std::max(1.0, tiles(128) / 256);
+    default: return 8.0 + k * std::ceil(tiles(256) / 256) * (19.0e-3 + 17.0e-3 * std::min(1.0, tiles(256) / 256));
+    }
+}
+
+Way way_of(uint32_t M, uint32_t N, uint32_t K, bool symmetric, bool pairs)
+{
+    Way best = kFew;
+    for (int w = kFew + 1; w < kWays; ++w)
+        if (time_of((Way)w, M, N, K, symmetric, pairs) < time_of(best, M, N, K, symmetric, pairs)) best = (Way)w;
+    return best;
+}
+
 struct StepPlan {
-    bool wide, pairs;
-    uint32_t small, large; // the sides
-    int64_t ld_P, ld_Q, ld_A;
+    bool tall, pairs;
+    uint32_t small, large; // the sides: X is [small, large]
+    Way way_gram, way_square, way_step;
+    bool turned; // X is held turned beside itself
+    int64_t ld_X, ld_T, ld_A;
     uint32_t n_sums;
-    size_t off_sums, off_P[2], off_Q[2], off_A, off_B, total;
-    int64_t plane_P, plane_Q, plane_A; // elements
+    size_t off_sums, off_X[2], off_T[2], off_A, off_B, total;
+    int64_t plane_X, plane_T, plane_A; // elements
 };
 
 StepPlan step_plan(const Common &c)
@@ -355,28 +408,36 @@ StepPlan step_plan(const Common &c)
         return at;
     };
     const auto up = [](int64_t n) { return (n + 7) / 8 * 8; };
-    t.wide = c.rows <= c.cols;
+    t.tall = c.rows > c.cols;
     t.small = (uint32_t)std::min(c.rows, c.cols), t.large = (uint32_t)std::max(c.rows, c.cols);
     t.pairs = c.type != ZG_BF16 || t.small < 256 || c.steps > 6;
-    t.ld_P = up(c.cols), t.ld_Q = up(c.rows), t.ld_A = up(t.small);
-    t.plane_P = c.rows * t.ld_P, t.plane_Q = c.cols * t.ld_Q, t.plane_A = t.small * t.ld_A;
+    t.way_gram = way_of(t.small, t.small, t.large, true, t.pairs);
+    t.way_square = way_of(t.small, t.small, t.small, true, t.pairs);
+    t.way_step = way_of(t.small, t.large, t.small, false, t.pairs);
+    t.turned = t.way_step != k256;
+    t.ld_X = up(t.large), t.ld_T = t.ld_A = up(t.small);
+    t.plane_X = t.small * t.ld_X, t.plane_T = t.large * t.ld_T, t.plane_A = t.small * t.ld_A;
     t.n_sums = (uint32_t)std::min<int64_t>(kNormBlocks, ((int64_t)c.rows * ((c.cols + 7) / 8) + 255) / 256);
     t.off_sums = take(t.n_sums * sizeof(double));
-    for (int i = 0; i < 2; ++i) t.off_P[i] = take((size_t)t.plane_P * 2 * sizeof(f16)), t.off_Q[i] = take((size_t)t.plane_Q * (t.pairs ? 2 : 1) * sizeof(f16));
-    t.off_A = take((size_t)t.plane_A * 2 * sizeof(f16));
-    t.off_B = take((size_t)t.plane_A * 2 * sizeof(f16));
+    for (int i = 0; i < 2; ++i) {
+        t.off_X[i] = take((size_t)t.plane_X * 2 * sizeof(f16));
+        if (t.turned) t.off_T[i] = take((size_t)t.plane_T * (t.pairs ? 2 : 1) * sizeof(f16));
+    }
+    t.off_A = take((size_t)t.plane_A * (t.pairs ? 2 : 1) * sizeof(f16));
+    t.off_B = take((size_t)t.plane_A * (t.pairs ? 2 : 1) * sizeof(f16));
     return t;
 }
 
-template <int SEGMENTS, int KIND> int launch_step(hipStream_t st, const StepArgs<SEGMENTS, KIND> &p)
+template <int SEGMENTS, int KIND> int launch_step(hipStream_t st, Way way, const StepArgs<SEGMENTS, KIND> &p)
 {
-    const auto blocks = [&](uint32_t tile) -> uint64_t {
-        const uint64_t m = (p.M + tile - 1) / tile, n = (p.N + tile - 1) / tile;
-        return KIND == kSquare ? n * (n + 1) / 2 : m * n;
-    };
-    if (blocks(128) < 128) return launch(st, k_step_few<SEGMENTS, KIND>, grid_of(blocks(32)), 256, p);
-    if (blocks(256) < 256) return launch(st, k_step_chunks<SEGMENTS, KIND>, grid_of((blocks(128) + 7) / 8 * 8), 256, p);
-    return launch(st, k_step_long<SEGMENTS, KIND>, dim3(256), 512, p);
+    const auto grid = [&](uint32_t tile) { return grid_of((tiles_of(p.M, p.N, KIND == kSquare, tile) + 7) / 8 * 8); };
+    if (way == kFew) return launch(st, k_step_few<SEGMENTS, KIND>, grid_of(tiles_of(p.M, p.N, KIND == kSquare, 32)), 256, p);
+    if constexpr (KIND == kSquare)
+        if (way == kShared) return launch(st, k_step_shared<SEGMENTS>, grid(64), 512, p);
+    if (way == k64) return launch(st, k_step_64<SEGMENTS, KIND>, grid(64), 256, p);
+    if (way == k128) return launch(st, k_step_128<SEGMENTS, KIND>, grid(128), 256, p);
+    if (way == kDense) return launch(st, k_step_dense<SEGMENTS, KIND>, grid(128), 256, p);
+    return launch(st, k_step_256<SEGMENTS, KIND>, dim3(256), 512, p);
 }
 
 struct Result {
@@ -388,13 +449,12 @@ struct Result {
 
 template <int SEGMENTS> int run_steps(hipStream_t st, const Common &c, const StepPlan &t, char *ws, const Result &out)
 {
-    f16 *P[2], *Q[2], *const A = reinterpret_cast<f16 *>(ws + t.off_A), *const B = reinterpret_cast<f16 *>(ws + t.off_B);
-    for (int i = 0; i < 2; ++i) P[i] = reinterpret_cast<f16 *>(ws + t.off_P[i]), Q[i] = reinterpret_cast<f16 *>(ws + t.off_Q[i]);
+    const auto at_ws = [&](size_t off) { return reinterpret_cast<f16 *>(ws + off); };
+    f16 *const A = at_ws(t.off_A), *const B = at_ws(t.off_B);
     const bool pairs = SEGMENTS > 1;
-    const int64_t low_P = t.plane_P * (int64_t)sizeof(f16), low_Q = t.plane_Q * (int64_t)sizeof(f16), low_A = t.plane_A * (int64_t)sizeof(f16);
     const auto up = [](uint32_t n) { return (n + 7) / 8 * 8; };
-    const auto start = [&](auto &p, Operand a, int64_t low_a, Operand b, int64_t low_b, uint32_t M, uint32_t N, uint32_t K) {
-        p.a = a, p.b = b, p.low_a = low_a, p.low_b = low_b;
+    const auto start = [&](auto &p, Operand a, int64_t plane_a, Operand b, int64_t plane_b, uint32_t M, uint32_t N, uint32_t K) {
+        p.a = a, p.b = b, p.low_a = plane_a * (int64_t)sizeof(f16), p.low_b = plane_b * (int64_t)sizeof(f16);
         p.M = M, p.N = N, p.K = up(K);
         p.rows = {nullptr, M};
         p.splits = 1;
@@ -406,40 +466,44 @@ template <int SEGMENTS> int run_steps(hipStream_t st, const Common &c, const Ste
         const float *const k = c.coefficients + 3 * s;
         const Bounds next = bounds_of(top, k);
         const int ea = exponent_for(top * top), eb = exponent_for(next.b), en = exponent_for(next.x);
-        const Operand of_P{P[at], t.ld_P, false, true}, of_Q{Q[at], t.ld_Q, false, true};
+        f16 *const X = at_ws(t.off_X[at]), *const X_next = at_ws(t.off_X[at ^ 1]);
+        const Operand of_X{X, t.ld_X, false, true};
         {
             StepArgs<SEGMENTS, kSquare> p{}; // A = X X^T
-            const Operand x = t.wide ? of_P : of_Q;
-            start(p, x, t.wide ? low_P : low_Q, x, t.wide ? low_P : low_Q, t.small, t.small, t.large);
+            start(p, of_X, t.plane_X, of_X, t.plane_X, t.small, t.small, t.large);
             p.alpha = std::ldexp(1.0f, ea - 2 * ex);
             p.H = p.TH = A, p.L = p.TL = pairs ? A + t.plane_A : nullptr, p.ld_H = p.ld_T = t.ld_A;
-            ZG_TRY(launch_step(st, p));
+            ZG_TRY(launch_step(st, t.way_gram, p));
         }
         {
             StepArgs<SEGMENTS, kSquare> p{}; // B = b A + c A^2
-            start(p, of_A, low_A, of_A, low_A, t.small, t.small, t.small);
+            start(p, of_A, t.plane_A, of_A, t.plane_A, t.small, t.small, t.small);
             p.alpha = std::ldexp(k[2], eb - 2 * ea), p.beta = std::ldexp(k[1], eb - ea);
             p.R = A, p.R_low = pairs ? A + t.plane_A : nullptr, p.ld_R = t.ld_A;
             p.H = p.TH = B, p.L = p.TL = pairs ? B + t.plane_A : nullptr, p.ld_H = p.ld_T = t.ld_A;
-            ZG_TRY(launch_step(st, p));
+            ZG_TRY(launch_step(st, t.way_square, p));
         }
-        const auto last = [&](auto &p, double factor, int exponent) { // a P + B Q^T, or a P + P B^T
-            if (t.wide) start(p, of_B, low_A, of_Q, low_Q, (uint32_t)c.rows, (uint32_t)c.cols, t.small);
-            else start(p, of_P, low_P, of_B, low_A, (uint32_t)c.rows, (uint32_t)c.cols, t.small);
+        const auto next_X = [&](auto &p, double factor, int exponent) { // a X + B X
+            if (t.turned) {
+                start(p, of_B, t.plane_A, Operand{at_ws(t.off_T[at]), t.ld_T, false, true}, t.plane_T, t.small, t.large, t.small);
+            } else {
+                start(p, of_B, t.plane_A, Operand{X, t.ld_X, true, true}, t.plane_X, t.small, t.large, t.small);
+                p.b_short = p.K - t.small;
+            }
             p.alpha = (float)std::ldexp(factor, exponent - eb - ex), p.beta = (float)std::ldexp(factor * k[0], exponent - ex);
-            p.R = P[at], p.R_low = P[at] + t.plane_P, p.ld_R = t.ld_P;
+            p.R = X, p.R_low = X + t.plane_X, p.ld_R = t.ld_X;
         };
         if (s + 1 < c.steps) {
             StepArgs<SEGMENTS, kStep> p{};
-            last(p, 1.0, en);
-            p.H = P[at ^ 1], p.L = P[at ^ 1] + t.plane_P, p.ld_H = t.ld_P;
-            p.TH = Q[at ^ 1], p.TL = pairs ? Q[at ^ 1] + t.plane_Q : nullptr, p.ld_T = t.ld_Q;
-            ZG_TRY(launch_step(st, p));
+            next_X(p, 1.0, en);
+            p.H = X_next, p.L = X_next + t.plane_X, p.ld_H = t.ld_X;
+            if (t.turned) p.TH = at_ws(t.off_T[at ^ 1]), p.TL = pairs ? p.TH + t.plane_T : nullptr, p.ld_T = t.ld_T;
+            ZG_TRY(launch_step(st, t.way_step, p));
         } else {
             StepArgs<SEGMENTS, kResult> p{};
-            last(p, out.factor, 0);
-            p.O = out.O, p.ld_O = out.ld, p.type_O = c.type, p.update = out.update, p.keep = out.keep;
-            ZG_TRY(launch_step(st, p));
+            next_X(p, out.factor, 0);
+            p.O = out.O, p.ld_O = out.ld, p.type_O = c.type, p.update = out.update, p.keep = out.keep, p.turn = t.tall;
+            ZG_TRY(launch_step(st, t.way_step, p));
         }
         top = next.x, ex = en;
     }
@@ -452,13 +516,15 @@ int run(hipStream_t st, const Common &c, StartArgs a, char *ws, const Result &ou
     a.rows = (uint32_t)c.rows, a.cols = (uint32_t)c.cols;
     a.eps = c.eps, a.sums = reinterpret_cast<double *>(ws + t.off_sums), a.n_sums = t.n_sums;
     a.power = std::ldexp(1.0f, exponent_for(1.0));
-    a.P = reinterpret_cast<f16 *>(ws + t.off_P[0]), a.P_low = a.P + t.plane_P, a.ld_P = t.ld_P;
-    a.Q = reinterpret_cast<f16 *>(ws + t.off_Q[0]), a.Q_low = t.pairs ? a.Q + t.plane_Q : nullptr, a.ld_Q = t.ld_Q;
+    f16 *const X = reinterpret_cast<f16 *>(ws + t.off_X[0]), *const T = t.turned ? reinterpret_cast<f16 *>(ws + t.off_T[0]) : nullptr;
+    f16 *const X_low = X + t.plane_X, *const T_low = t.turned && t.pairs ? T + t.plane_T : nullptr;
+    a.P = t.tall ? T : X, a.P_low = t.tall ? T_low : X_low, a.ld_P = t.tall ? t.ld_T : t.ld_X;
+    a.Q = t.tall ? X : T, a.Q_low = t.tall ? X_low : T_low, a.ld_Q = t.tall ? t.ld_X : t.ld_T;
     const dim3 planes = grid_of((uint64_t)((c.rows + 63) / 64) * ((c.cols + 63) / 64));
     const auto begin = [&](auto zero) -> int {
-        using T = decltype(zero);
-        ZG_TRY(launch(st, k_start_norm<T>, dim3(t.n_sums), 256, a));
-        return launch(st, k_start_planes<T>, planes, 256, a);
+        using T_ = decltype(zero);
+        ZG_TRY(launch(st, k_start_norm<T_>, dim3(t.n_sums), 256, a));
+        return launch(st, k_start_planes<T_>, planes, 256, a);
     };
     ZG_TRY(c.dtype == ZG_F32 ? begin(float()) : c.dtype == ZG_F16 ? begin((f16)0) : begin((__bf16)0));
     return t.pairs ? run_steps<3>(st, c, t, ws, out) : run_steps<1>(st, c, t, ws, out);

@@ -45,6 +45,7 @@ struct ProductArgs {
     Epilogue e;
 
     static constexpr bool symmetric = false; // C is, and only tiles that reach down to its diagonal are made
+    static constexpr int high = 1;           // rows of tiles that a run of tiles goes through side by side
     static constexpr int segments = 1;       // products over K that are summed: of other planes of the operands (plane_a, plane_b: bytes from p to them)
 };
 
@@ -467,8 +468,8 @@ __device__ __forceinline__ uint32_t row_of_triangle(uint32_t t)
     return row * (row + 1) / 2 > t ? row - 1 : (row + 1) * (row + 2) / 2 <= t ? row + 1 : row;
 }
 
-template <int BM, int BN, bool SYMMETRIC = false> struct Tiles {
-    uint32_t M, k_all, nt, splits, part_k;
+template <int BM, int BN, bool SYMMETRIC = false, int HIGH = 1> struct Tiles {
+    uint32_t M, k_all, nt, mt, splits, part_k;
     uint64_t in_part, next, end; // of this workgroup: the next tile, the end of its XCD's run
 
     __device__ __forceinline__ Tiles(const ProductArgs &p, uint32_t depth)
@@ -478,7 +479,8 @@ template <int BM, int BN, bool SYMMETRIC = false> struct Tiles {
         k_all = p.rows_are_k ? min(p.K, live) : p.K;
         nt = (p.N + BN - 1) / BN;
         splits = p.splits;
-        in_part = (uint64_t)((M + BM - 1) / BM) * nt;
+        mt = (M + BM - 1) / BM;
+        in_part = (uint64_t)mt * nt;
         if constexpr (SYMMETRIC) in_part = (uint64_t)nt * (nt + 1) / 2;
         part_k = __builtin_amdgcn_readfirstlane(((k_all + splits - 1) / splits + depth - 1) / depth * depth);
         const uint64_t tiles = in_part * splits, share = (tiles + 7) / 8;
@@ -497,6 +499,10 @@ template <int BM, int BN, bool SYMMETRIC = false> struct Tiles {
             const uint32_t row = same(row_of_triangle(t));
             w.m0 = row * BM;
             w.n0 = (t - row * (row + 1) / 2) * BN;
+        } else if constexpr (HIGH > 1) {
+            const uint32_t block = same(t / (HIGH * nt)), high = min((uint32_t)HIGH, mt - block * HIGH), in_block = t - block * (HIGH * nt), col = same(in_block / high);
+            w.m0 = (block * HIGH + in_block - col * high) * BM;
+            w.n0 = col * BN;
         } else {
             const uint32_t row = same(t / nt);
             w.m0 = row * BM;
@@ -516,7 +522,7 @@ template <class T, int BM, int BN, bool A_TURNED, bool B_TURNED, class Args> __d
 {
     constexpr int K = chunk_k<T>, depth = 8 * K, FM = BM / 64, FN = BN / 64;
     __shared__ u32x4 lds[2][(BM + BN) * 8];
-    Tiles<BM, BN, Args::symmetric> tiles(p, depth);
+    Tiles<BM, BN, Args::symmetric, Args::high> tiles(p, depth);
     Place w;
     if (!tiles.take(w)) return;
     const uint32_t k_end = w.k_end, M = tiles.M;
@@ -586,7 +592,7 @@ template <class T, int tile, int waves, int CH, bool TURNED> struct Feed;
 template <class T, int tile, int waves, int CH> struct Feed<T, tile, waves, CH, false> {
     static constexpr int K = 16 / (int)sizeof(T), loads = tile * CH / (64 * waves);
     static constexpr bool turned = false;
-    static_assert(CH == 4 || loads % 4 == 0, "");
+    static_assert(CH == 4 || loads % 2 == 0, "");
     const char *p;
     uint32_t from[loads], chunk;
 
@@ -594,10 +600,11 @@ template <class T, int tile, int waves, int CH> struct Feed<T, tile, waves, CH, 
     // which chunk a lane has in its lth load: the rows of one load are 64 / CH further on than those of the one before
     __device__ __forceinline__ uint32_t chunk_at(int l) const { return CH == 4 ? chunk : chunk ^ (2 * l & 7); }
 
+    __device__ __forceinline__ static const char *first_of(const Operand &o, uint32_t first) { return static_cast<const char *>(o.p) + first * (uint64_t)o.ld * sizeof(T); }
     __device__ __forceinline__ void start(const Operand &o, uint32_t first, uint32_t rows, uint32_t wave, uint32_t lane)
     {
         const uint64_t ld = (uint64_t)o.ld * sizeof(T);
-        p = static_cast<const char *>(o.p) + first * ld;
+        p = first_of(o, first);
         chunk = (lane % CH) ^ turn(wave * loads * 64 / CH + lane / CH);
 #pragma unroll
         for (int l = 0; l < loads; ++l) {
@@ -631,12 +638,14 @@ template <class T, int tile, int waves, int CH> struct Feed<T, tile, waves, CH, 
     uint32_t from[loads], k_of[loads];
 
     // 16-bit rows of four k that are read together start 64 bytes apart in the banks
+    static_assert(sizeof(T) != 2 || row >= 16, "");
     __device__ __forceinline__ static uint32_t turn(uint32_t k) { return sizeof(T) == 2 ? (k & 3) << 2 : 0; }
 
+    __device__ __forceinline__ static const char *first_of(const Operand &o, uint32_t first) { return static_cast<const char *>(o.p) + (uint64_t)first * sizeof(T); }
     __device__ __forceinline__ void start(const Operand &o, uint32_t first, uint32_t rows, uint32_t wave, uint32_t lane)
     {
         ld = (uint64_t)o.ld * sizeof(T);
-        p = static_cast<const char *>(o.p) + (uint64_t)first * sizeof(T);
+        p = first_of(o, first);
 #pragma unroll
         for (int l = 0; l < loads; ++l) {
             const uint32_t s = (wave * loads + l) * 64 + lane, i = ((s % row) ^ turn(s / row)) * K;
@@ -821,57 +830,83 @@ template <class A, class B, int b_at, int step_k, int stage, int stages, class O
 // to a compute unit): bound by the matrix instructions, 285127 x 256 x 256 with ReLU and Z 370 us, 100 TFLOP/s, 65536 x 1024 x 1024 1005 us, 137.
 // 16 and 8 bits (256 x 128, two): by matrix instructions, the epilogue's vector instructions and stores in part beside each other, bf16
 // 65537 x 1024 x 1024 with GELU, dropout, residual and Z 266 us, 8 bits 65536 x 1024 x 2048 with SiLU 305 us, 8192 x 8192 x 8192 841 us, 1310 TFLOP/s.
-template <class T, class O, int BM, int BN, bool A_TURNED, bool B_TURNED, class Args> __device__ __forceinline__ void chunks_tile(const Args &p)
+template <class T, class O, int BM, int BN, bool A_TURNED, bool B_TURNED, int CH = 4, int stages = 3, int GROUPS = 1, class Args> __device__ __forceinline__ void chunks_tile(const Args &p)
 {
-    using A = Feed<T, BM, 4, 4, A_TURNED>;
-    using B = Feed<T, BN, 4, 4, B_TURNED>;
-    constexpr int depth = 4 * A::K, FM = BM / 64, FN = BN / 64, stages = 3, stage = (BM + BN) * 4;
-    __shared__ u32x4 lds[stages * stage];
-    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    using A = Feed<T, BM, 4, CH, A_TURNED>;
+    using B = Feed<T, BN, 4, CH, B_TURNED>;
+    constexpr int depth = CH * A::K, FM = BM / 64, FN = BN / 64, stage = (BM + BN) * CH;
+    static_assert(GROUPS == 1 || (FM == 1 && FN == 1 && stages * stage * 4 >= 4 * 16 * 64), "");
+    __shared__ u32x4 all_lds[GROUPS * stages * stage];
+    const uint32_t lane = threadIdx.x & 63, wave_of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = GROUPS == 1 ? 0 : wave_of_all >> 2;
+    const uint32_t wave = GROUPS == 1 ? wave_of_all : wave_of_all & 3;
+    u32x4 *const lds = all_lds + group * (stages * stage);
     const uint32_t wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2), am = wm + (lane & 31), bn = wn + (lane & 31);
-    Tiles<BM, BN, Args::symmetric> tiles(p, depth);
+    Tiles<BM, BN, Args::symmetric, Args::high> tiles(p, depth);
     Place w;
     if (!tiles.take(w)) return;
     A a;
     B b;
     a.start(p.a, w.m0, tiles.M, wave, lane);
     b.start(p.b, w.n0, p.N, wave, lane);
-    const uint32_t steps = (w.k_end - w.k_first + depth - 1) / depth * Args::segments;
+    uint32_t steps = (w.k_end - w.k_first + depth - 1) / depth;
+    if constexpr (GROUPS > 1) { // of k, each group has a run
+        steps = (steps + GROUPS - 1) / GROUPS;
+        w.k_first += group * steps * depth;
+        w.k_end = min(w.k_end, w.k_first + steps * depth); // (below k_first: nothing)
+    }
+    steps *= Args::segments;
     int segment = 0;
     const auto on = [&](auto &fetch) { // to the next segment
         if constexpr (Args::segments > 1) {
             if (++segment == Args::segments) return;
-            a.p = static_cast<const char *>(p.a.p) + w.m0 * (uint64_t)p.a.ld * sizeof(T) + p.plane_a(segment);
-            b.p = static_cast<const char *>(p.b.p) + w.n0 * (uint64_t)p.b.ld * sizeof(T) + p.plane_b(segment);
+            a.p = A::first_of(p.a, w.m0) + p.plane_a(segment);
+            b.p = B::first_of(p.b, w.n0) + p.plane_b(segment);
             fetch.k = w.k_first, fetch.k_end = w.k_end;
         }
     };
     if constexpr (Args::segments > 1) a.p += p.plane_a(0), b.p += p.plane_b(0);
-    Fetch<A, B, BM * 4, depth, stage, stages, decltype(on)> fetch{a, b, lds, wave, p.K - p.b_short, w.k_first, w.k_end, on};
+    Fetch<A, B, BM * CH, depth, stage, stages, decltype(on)> fetch{a, b, lds, wave, p.K - p.b_short, w.k_first, w.k_end, on};
     f32x16 acc[FM][FN] = {};
     uint32_t now = 0;
     if (steps > 0) {
         fetch.begin();
-        multiply_steps<T, A, B, FM, FN, 4, stages>(acc, lds, BM * 4, stage, steps, am, bn, now, fetch);
+        multiply_steps<T, A, B, FM, FN, CH, stages>(acc, lds, BM * CH, stage, steps, am, bn, now, fetch);
         wait_loads<0>();
     }
     __syncthreads(); // the buffers are free
-    Out<Args>::template wide<O, B_TURNED>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 512, w.m0 + wm, w.n0 + wn, tiles.M, w.split);
+    if constexpr (GROUPS > 1) { // the groups' sums, in order
+        float *const cells = reinterpret_cast<float *>(all_lds);
+        if (group > 0) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) cells[(((group - 1) * 4 + wave) * 16 + r) * 64 + lane] = acc[0][0][r];
+        }
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int i = 0; i < GROUPS - 1; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[0][0][r] += cells[((i * 4 + wave) * 16 + r) * 64 + lane];
+        // (through the 4 KB that group 1's wavefront of the same number left for this one)
+        Out<Args>::template narrow<O, B_TURNED>(p, acc, reinterpret_cast<f32x4 *>(cells + wave * 1024), w.m0 + wm, w.n0 + wn, tiles.M, w.split);
+        return;
+    }
+    if constexpr (FN == 2) Out<Args>::template wide<O, B_TURNED>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 512, w.m0 + wm, w.n0 + wn, tiles.M, w.split);
+    else Out<Args>::template narrow<O, B_TURNED>(p, acc, reinterpret_cast<f32x4 *>(lds) + wave * 256, w.m0 + wm, w.n0 + wn, tiles.M, w.split);
 }
 
 // Eight wavefronts, 256 x 256 cells, one workgroup to a compute unit, which takes one tile after the other; two buffers of eight chunks (128 bytes) of k.  For 16-bit types.  The next tile's
 // first steps are on their way while this one's cells are handed over, through LDS of their own.  Bound by what is between the matrix
 // instructions (counters: they run for 0.38 to 0.43 of the time over 1024 terms): bf16 65536 x 1024 x 1024 162 us, 850 TFLOP/s, 4096 x 16384 x 4096 433 us, 1270.
-template <class T, class O, bool A_TURNED, bool B_TURNED, class Args> __device__ __forceinline__ void long_tiles(const Args &p)
+template <class T, class O, bool A_TURNED, bool B_TURNED, int WAVES = 8, class Args> __device__ __forceinline__ void long_tiles(const Args &p)
 {
-    constexpr int BM = 256, BN = 256, FM = 4, FN = 2, CH = 8, stages = 2, stage = (BM + BN) * CH;
-    using A = Feed<T, BM, 8, CH, A_TURNED>;
-    using B = Feed<T, BN, 8, CH, B_TURNED>;
+    constexpr int BM = 256, BN = 256, FM = 4, FN = WAVES == 8 ? 2 : 4, CH = 8, stages = 2, stage = (BM + BN) * CH;
+    using A = Feed<T, BM, WAVES, CH, A_TURNED>;
+    using B = Feed<T, BN, WAVES, CH, B_TURNED>;
     constexpr int depth = CH * A::K;
     __shared__ u32x4 lds[stages * stage + 8 * 256];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t wm = (wave >> 2) * 128, wn = (wave & 3) * 64, am = wm + (lane & 31), bn = wn + (lane & 31);
-    Tiles<BM, BN, Args::symmetric> tiles(p, depth), ahead = tiles;
+    const uint32_t wm = (wave >> (WAVES == 8 ? 2 : 1)) * 128, wn = (wave & (WAVES == 8 ? 3 : 1)) * 32 * FN, am = wm + (lane & 31), bn = wn + (lane & 31);
+    Tiles<BM, BN, Args::symmetric, Args::high> tiles(p, depth), ahead = tiles;
     A a{}; // (a workgroup without a tile asks for zeros)
     B b{};
     Place h;
@@ -880,8 +915,8 @@ template <class T, class O, bool A_TURNED, bool B_TURNED, class Args> __device__
         if constexpr (Args::segments > 1) {
             if (segment + 1 < Args::segments) {
                 ++segment;
-                a.p = static_cast<const char *>(p.a.p) + h.m0 * (uint64_t)p.a.ld * sizeof(T) + p.plane_a(segment);
-                b.p = static_cast<const char *>(p.b.p) + h.n0 * (uint64_t)p.b.ld * sizeof(T) + p.plane_b(segment);
+                a.p = A::first_of(p.a, h.m0) + p.plane_a(segment);
+                b.p = B::first_of(p.b, h.n0) + p.plane_b(segment);
                 fetch.k = h.k_first, fetch.k_end = h.k_end;
                 return;
             }
@@ -959,8 +994,9 @@ template <class T, class Args> __device__ __forceinline__ void few_tile(const Ar
         }
     } else { // pairs: the high planes at p, the low ones behind
         Along<T> la = a, lb = b;
+        f32x16 low = {};
         la.row = reinterpret_cast<const T *>(reinterpret_cast<const char *>(a.row) + p.plane_a(0));
-        lb.row = reinterpret_cast<const T *>(reinterpret_cast<const char *>(b.row) + p.plane_b(2));
+        lb.row = reinterpret_cast<const T *>(reinterpret_cast<const char *>(b.row) + p.plane_b(1));
         for (uint32_t k0 = wave * 2 * K; k0 < p.K; k0 += ahead * 8 * K) {
             u32x4 x[ahead], y[ahead], lx[ahead], ly[ahead];
 #pragma unroll
@@ -971,11 +1007,12 @@ template <class T, class Args> __device__ __forceinline__ void few_tile(const Ar
             }
 #pragma unroll
             for (int i = 0; i < ahead; ++i) {
-                multiply(T(), y[i], lx[i], acc);
-                multiply(T(), ly[i], x[i], acc);
+                multiply(T(), y[i], lx[i], low);
+                multiply(T(), ly[i], x[i], low);
                 multiply(T(), y[i], x[i], acc);
             }
         }
+        acc += low;
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q)

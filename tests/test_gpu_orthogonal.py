@@ -42,7 +42,7 @@ def _untouched(whole, rows, cols, what):
 
 SIZES = [  # rows, cols, pad, shift
     (1, 1, 0, 0), (1, 50, 0, 0), (50, 1, 1, 1), (2, 3, 0, 0), (7, 5, 1, 0), (16, 16, 0, 0), (31, 33, 3, 1), (33, 31, 0, 0), (47, 256, 0, 0), (64, 64, 8, 0), (100, 1000, 0, 0), (1000, 100, 0, 0),
-    (255, 255, 1, 1), (256, 256, 0, 0), (257, 300, 0, 0), (300, 257, 2, 3), (600, 1201, 3, 0), (1201, 600, 0, 0), (8, 4096, 0, 0), (1025, 1100, 0, 0), (1536, 1280, 0, 0)]
+    (255, 255, 1, 1), (256, 256, 0, 0), (257, 300, 0, 0), (300, 257, 2, 3), (600, 1201, 3, 0), (1201, 600, 0, 0), (8, 4096, 0, 0), (1025, 1100, 0, 0), (1536, 1280, 0, 0), (2050, 700, 1, 0), (2100, 2300, 0, 0), (700, 5003, 0, 0)]
 
 
 @pytest.mark.parametrize("kinds", [(F32, F32), (F16, F16), (BF16, BF16), (F32, BF16), (BF16, F32)], ids=str)
