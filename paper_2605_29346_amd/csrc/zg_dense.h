@@ -27,19 +27,24 @@ template <class F> int entry(F &&body) noexcept
     }
 }
 
-template <class... P, class... A> int launch(hipStream_t st, void (*kernel)(P...), dim3 grid, unsigned block, const A &...given)
+template <class... P, class... A> int launch_lds(hipStream_t st, void (*kernel)(P...), dim3 grid, unsigned block, size_t lds, const A &...given)
 {
     if (grid.x == 0 || grid.y == 0 || grid.z == 0) return ZG_OK;
     std::tuple<P...> a{given...};
     void *args[sizeof...(P)];
     std::apply([&](auto &...v) { int i = 0; ((args[i++] = const_cast<void *>(static_cast<const void *>(&v))), ...); }, a);
     // (what the launch returned, and not hipGetLastError: that may be an earlier error of the caller's own)
-    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(block), args, 0, st);
+    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(block), args, lds, st);
     if (e != hipSuccess) {
         (void)hipGetLastError();
         return fail(ZG_EHIP, std::string("hipLaunchKernel: ") + hipGetErrorString(e));
     }
     return ZG_OK;
+}
+
+template <class... P, class... A> int launch(hipStream_t st, void (*kernel)(P...), dim3 grid, unsigned block, const A &...given)
+{
+    return launch_lds(st, kernel, grid, block, 0, given...);
 }
 
 // A launch's lanes in one dimension number less than 2^32: beyond 2^21 workgroups the grid has a second one (with workgroups to spare, which

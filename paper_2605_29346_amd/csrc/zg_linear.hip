@@ -23,42 +23,45 @@ template <class T, class O, bool A_TURNED, bool B_TURNED> __global__ __launch_bo
 
 template <class T> __global__ __launch_bounds__(256) void k_few(ProductArgs p) { few_tile<T>(p); }
 
-// The sum over the parts, and what happens to it (16 parts of 1024 x 1024: 19 us, 3.5 TB/s; 256 of 256 x 200: 12 us): eight groups of eight cells to a workgroup, every 32nd part to a lane, then the lanes in order.
+// The sum over the parts, and what happens to it (16 parts of 1024 x 1024: 19 us, 3.5 TB/s; 256 of 256 x 200: 12 us): groups of eight cells, each with `lanes` lanes (a power of two up to 32) that have every so
+// manieth part each; then the lanes in order.  Up to 32 parts are added one after the other whatever the lanes are.
 struct JoinArgs {
     const float *part;
-    uint32_t M, N, splits;
+    uint32_t M, N, splits, lanes;
     Epilogue e;
     Rows rows; // the device's count bounds M
 };
 
 __global__ __launch_bounds__(256) void k_join(JoinArgs p)
 {
-    __shared__ float lds[32][8][8 + 1];
-    const uint32_t groups = (p.N + 7) / 8, g = threadIdx.x & 7, lane = threadIdx.x >> 3;
-    const uint64_t i = block_number() * 8ull + g, cells = (uint64_t)p.M * p.N;
+    __shared__ float lds[256][8 + 1];
+    const uint32_t groups = (p.N + 7) / 8, in_block = 256 / p.lanes, g = threadIdx.x % in_block, lane = threadIdx.x / in_block;
+    const uint64_t i = (uint64_t)block_number() * in_block + g, cells = (uint64_t)p.M * p.N;
     const bool there = i < (uint64_t)min(p.M, p.rows.live()) * groups;
     const uint32_t m = there ? (uint32_t)(i / groups) : 0u, n = there ? (uint32_t)(i % groups) * 8 : 0u;
     float v[8] = {};
     if (there)
-        for (uint32_t s = lane; s < p.splits; s += 32) {
+        for (uint32_t s = lane; s < p.splits; s += p.lanes) {
             float w[8];
             load8(p.part + s * cells + (uint64_t)m * p.N + n, (int)(p.N - n), w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += w[j];
         }
+    if (p.lanes > 1) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) lds[lane][g][j] = v[j];
-    __syncthreads();
+        for (int j = 0; j < 8; ++j) lds[threadIdx.x][j] = v[j];
+        __syncthreads();
+    }
     if (lane || !there) return;
     const Columns c = columns_of(p.e, n, p.N);
     Needs<AnyType, 1> needs;
     needs.ask(p.e, c.n, c.left, m, 1, p.M);
     finish(p.e, c, needs, m, 1, p.M, [&](int, float(&sum)[8]) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
-        for (uint32_t s = 0; s < min(p.splits, 32u); ++s)
+        for (int j = 0; j < 8; ++j) sum[j] = v[j];
+        for (uint32_t s = 1; s < min(p.splits, p.lanes); ++s)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[j] += lds[s][g][j];
+            for (int j = 0; j < 8; ++j) sum[j] += lds[s * in_block + g][j];
     });
 }
 
@@ -292,8 +295,11 @@ int dense_product(hipStream_t st, int32_t type, const ProductArgs &p, float *par
 
 int dense_join(hipStream_t st, const float *part, uint32_t M, uint32_t N, uint32_t splits, const Epilogue &e, Rows rows)
 {
+    // Lanes enough to fill the chip, no more than there are parts: 2 parts of 16384 x 1024 with one lane 36 us, with 32 212.
     const uint64_t groups = (uint64_t)M * ((N + 7) / 8);
-    return launch(st, k_join, grid_of((groups + 7) / 8), 256, JoinArgs{part, M, N, splits, e, rows});
+    uint32_t lanes = 1;
+    while (lanes < 32 && lanes < splits && (groups * lanes < (1 << 18) || splits > 32)) lanes *= 2;
+    return launch(st, k_join, grid_of((groups * lanes + 255) / 256), 256, JoinArgs{part, M, N, splits, lanes, e, rows});
 }
 
 } // namespace zg

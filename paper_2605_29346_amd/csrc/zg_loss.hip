@@ -36,6 +36,9 @@ __device__ __forceinline__ float power_of(float v, float top) { return __builtin
 // Where all logits are -infinity, they count from 0; not-a-number and +infinity end in a sum that is not a number.
 __device__ __forceinline__ float base_of(float top) { return top == -INFINITY ? 0.0f : top; }
 
+// Up to here z log2 e is far inside fp32; beyond, exp(z - top) is made from the difference.
+constexpr float kPlainTop = 1e30f;
+
 __device__ __forceinline__ Top join(Top a, Top b)
 {
     const float top = fmaxf(a.top, b.top), base = base_of(top);
@@ -43,13 +46,14 @@ __device__ __forceinline__ Top join(Top a, Top b)
 }
 
 struct TopArgs : ProductArgs {
+    static constexpr int high = 8;
     Labels labels;
     Top *part;       // [slot][M], a slot being the columns of a wavefront (or of k_loss_top_few's workgroup)
     float *at_label; // [M]: the label's logit
 };
 
 // A wavefront's 32 FM x 32 FN cells: half a row's lie side by side in a lane, the other half in the lane 32 further on, so that the row's largest and its sum need one exchange each.
-// For each cell an addition, a maximum, a subtraction, a multiplication, an exponential (four times as long) and an addition; the label's cell is looked for only where one of the
+// For each cell the bias, half of a maximum of three, a multiplication and addition in one, an exponential (four times as long) and an addition; the label's cell is looked for only where one of the
 // wavefront's 32 rows has it among its columns.
 template <int FM, int FN> __device__ __forceinline__ void tops(const TopArgs &p, const f32x16 (&acc)[FM][FN], uint32_t m_wave, uint32_t n_wave, uint32_t M)
 {
@@ -99,22 +103,27 @@ template <int FM, int FN> __device__ __forceinline__ void tops(const TopArgs &p,
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, v[j][r]);
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float base = base_of(top);
+        const float base = base_of(top), base2 = base * kLog2e; // (base2's rounding is that of a logit of base's size)
         float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sum += power_of(v[j][r], base);
-        sum += __shfl_xor(sum, 32);
-        if (half == 0 && m < M) part[m] = Top{top, sum};
-        if (__any(at < 32 * FN)) {
-            float z = 0.0f;
+            for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(fmaf(v[j][r], kLog2e, -base2));
+        const bool far = fabsf(base) > kPlainTop;
+        if (__any(at < 32 * FN || far)) { // what is rare
+            float z = 0.0f, far_sum = 0.0f;
 #pragma unroll
             for (int j = 0; j < FN; ++j)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) z = at == 32 * j + 8 * (r / 4) + 4 * half + r % 4 ? v[j][r] : z;
+                for (int r = 0; r < 16; ++r) {
+                    z = at == 32 * j + 8 * (r / 4) + 4 * half + r % 4 ? v[j][r] : z;
+                    far_sum += power_of(v[j][r], base);
+                }
             if (at < 32 * FN && (at >> 2 & 1) == half) p.at_label[m] = z;
+            sum = far ? far_sum : sum;
         }
+        sum += __shfl_xor(sum, 32);
+        if (half == 0 && m < M) part[m] = Top{top, sum};
     }
 }
 
@@ -169,6 +178,86 @@ template <class T> __global__ __launch_bounds__(256, 2) void k_loss_top_chunks(T
 template <> __global__ __launch_bounds__(256, 3) void k_loss_top_chunks<float>(TopArgs p) { chunks_tile<float, float, 128, 128, false, false>(p); }
 template <class T> __global__ __launch_bounds__(512, 2) void k_loss_top_long(TopArgs p) { long_tiles<T, T, false, false>(p); }
 
+template <class T> __global__ __launch_bounds__(256, 2) void k_loss_top_narrow(TopArgs p) { chunks_tile<T, T, 256, 64, false, false>(p); }
+template <> __global__ __launch_bounds__(256, 4) void k_loss_top_narrow<float>(TopArgs p) { chunks_tile<float, float, 128, 64, false, false>(p); }
+
+// A chunk's products, summed in fp32.
+template <class T> __device__ __forceinline__ float dot_chunk(u32x4 a, u32x4 b, float sum)
+{
+    constexpr int K = chunk_k<T>;
+    T x[K], y[K];
+    __builtin_memcpy(x, &a, 16);
+    __builtin_memcpy(y, &b, 16);
+#pragma unroll
+    for (int k = 0; k < K; ++k) sum = fmaf((float)x[k], (float)y[k], sum);
+    return sum;
+}
+
+// Up to R rows against all classes, operands in whole chunks, A's rows in LDS: a wavefront has 32 classes, 16 at a time, two to eight lanes, which read lines of 128 bytes of their rows.  Bound by
+// memory, which W passes once.
+template <class T, int R> __global__ __launch_bounds__(256) void k_loss_top_rows(TopArgs p)
+{
+    constexpr int K = chunk_k<T>, ahead = R == 1 ? 8 : 4;
+    extern __shared__ u32x4 rows[]; // [R][K / chunk_k]
+    const uint32_t lane = threadIdx.x & 63, live = min(p.M, p.rows.live()), chunks = p.K / K;
+    if (live == 0) return;
+    for (uint32_t i = threadIdx.x; i < chunks * R; i += 256) rows[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(p.a.p) + min(i / chunks, live - 1) * p.a.ld + (i % chunks) * K);
+    __syncthreads();
+    const uint32_t slot = __builtin_amdgcn_readfirstlane(block_number() * 4 + (threadIdx.x >> 6)), n0 = slot * 32;
+    if (n0 >= p.N) return;
+    float z[R] = {};
+#pragma unroll 1
+    for (uint32_t c0 = 0; c0 < 32 && n0 + c0 < p.N; c0 += 16) {
+        const T *w[2];
+        float sum[2][R] = {};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) w[h] = static_cast<const T *>(p.b.p) + (uint64_t)min(n0 + c0 + 8 * h + (lane >> 3), p.N - 1) * p.b.ld;
+        for (uint32_t q0 = lane & 7; q0 < chunks; q0 += 8 * ahead) {
+            u32x4 x[ahead][2];
+#pragma unroll
+            for (int i = 0; i < ahead; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) x[i][h] = q0 + 8 * i < chunks ? *reinterpret_cast<const u32x4 *>(w[h] + (q0 + 8 * i) * K) : u32x4{};
+#pragma unroll
+            for (int i = 0; i < ahead; ++i)
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const u32x4 a = rows[r * chunks + min(q0 + 8 * i, chunks - 1)];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float more = dot_chunk<T>(a, x[i][h], sum[h][r]);
+                        sum[h][r] = q0 + 8 * i < chunks ? more : sum[h][r]; // (what A holds in another place may be no number)
+                    }
+                }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+#pragma unroll
+                for (int d = 1; d < 8; d <<= 1) sum[h][r] += __shfl_xor(sum[h][r], d);
+                const float there = __shfl(sum[h][r], (lane & 7) * 8); // class lane % 8's
+                z[r] = (lane & 31) >> 3 == c0 / 8 + h ? there : z[r];
+            }
+    }
+    const uint32_t n = n0 + (lane & 31);
+    const bool there = lane < 32 && n < p.N;
+    const float bias = p.e.bias && there ? p.e.bias[n] : 0.0f;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if ((uint32_t)r >= live) break;
+        z[r] = there ? z[r] + bias : -INFINITY;
+        float top = z[r];
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        float sum = power_of(z[r], base_of(top));
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+        if (lane == 0) p.part[(uint64_t)slot * p.M + r] = Top{top, sum};
+        if (there && p.labels.of(r) == n) p.at_label[r] = z[r];
+    }
+}
+
 // ---- the rows' losses -------------------------------------------------------------------------------------------------------------
 
 struct RowArgs {
@@ -188,19 +277,27 @@ __device__ __forceinline__ void finish_loss(const RowArgs &a, double loss, doubl
     if (a.total) *a.total = (float)total;
 }
 
-// R rows at a time, 256 / R lanes to a row.  Reads what the product's tiles left, 8 bytes for 32 or 64 logits.
-template <int R> __global__ __launch_bounds__(256) void k_loss_rows(RowArgs a)
+// R rows at a time, G lanes to a row, four of its slots at a time.  Reads what the product's tiles left, 8 bytes for 32 or 64 logits.
+template <int R, int G> __global__ __launch_bounds__(R * G) void k_loss_rows(RowArgs a)
 {
-    constexpr int G = 256 / R;
-    __shared__ Top lds[256];
-    __shared__ double both[2][R < 64 ? 64 : R];
+    __shared__ Top lds[R * G];
+    __shared__ double both[2][R];
     const uint32_t live = a.rows.live(), r = threadIdx.x % R, g = threadIdx.x / R;
     double loss = 0.0, total = 0.0;
     for (uint64_t m0 = (uint64_t)blockIdx.x * R; m0 < live; m0 += (uint64_t)gridDim.x * R) {
         const uint64_t m = m0 + r;
         Top t{-INFINITY, 0.0f};
         if (m < live)
-            for (uint32_t s = g; s < a.slots; s += G) t = join(t, a.part[(uint64_t)s * a.cap + m]);
+            for (uint32_t s = g; s < a.slots; s += 4 * G) {
+                Top u[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[i] = s + i * G < a.slots ? a.part[(uint64_t)(s + i * G) * a.cap + m] : Top{-INFINITY, 0.0f};
+                const float top = fmaxf(fmaxf(fmaxf(u[0].top, u[1].top), fmaxf(u[2].top, u[3].top)), t.top), base = base_of(top);
+                t.sum *= power_of(t.top, base);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t.sum += u[i].sum * power_of(u[i].top, base);
+                t.top = top;
+            }
         if (G > 1) {
             lds[threadIdx.x] = t;
             __syncthreads();
@@ -223,18 +320,32 @@ template <int R> __global__ __launch_bounds__(256) void k_loss_rows(RowArgs a)
             }
         }
     }
-    __syncthreads();
     if (g == 0) both[0][r] = loss, both[1][r] = total;
     __syncthreads();
+#pragma unroll
+    for (int n = R / 2; n > 0; n >>= 1) {
+        if (threadIdx.x < (unsigned)n) both[0][r] += both[0][r + n], both[1][r] += both[1][r + n];
+        __syncthreads();
+    }
     if (threadIdx.x == 0) {
-        for (int i = 1; i < R; ++i) loss += both[0][i], total += both[1][i];
         if (gridDim.x == 1) {
-            finish_loss(a, loss, total);
+            finish_loss(a, both[0][0], both[1][0]);
         } else {
-            a.sums[2 * blockIdx.x] = loss;
-            a.sums[2 * blockIdx.x + 1] = total;
+            a.sums[2 * blockIdx.x] = both[0][0];
+            a.sums[2 * blockIdx.x + 1] = both[1][0];
         }
     }
+}
+
+// the shape of k_loss_rows: few parts to a row need a lane each; many of a few rows as many as a workgroup has
+enum RowShape { kRowsOne, kRows8, kRows32, kRowsWide, kRowsAll };
+constexpr int rows_of(RowShape s) { return s == kRowsOne ? 1 : s == kRows8 ? 8 : s == kRows32 ? 32 : s == kRowsWide ? 256 : 1024; }
+
+RowShape row_shape(int64_t rows, uint32_t slots)
+{
+    if (slots <= 4) return rows <= 8192 ? kRowsAll : kRowsWide; // (one workgroup needs no second launch)
+    if (rows <= 64) return kRowsOne;
+    return rows < 16384 && slots >= 128 ? kRows8 : kRows32;
 }
 
 __global__ __launch_bounds__(64) void k_loss_mean(RowArgs a, uint32_t n)
@@ -254,21 +365,19 @@ __global__ __launch_bounds__(64) void k_loss_mean(RowArgs a, uint32_t n)
 // what dZ's cells need of their row
 struct RowFactor {
     float lse, factor; // factor 0: no gradient, whatever the logits are
-    uint32_t label, reserved;
+    uint32_t label;
 };
 
 struct FactorArgs {
     Rows rows;
     const float *lse, *weight, *total, *dloss; // all but lse may be null
     Labels labels;
-    const float *tops; // null, or the largest |weight| of each of `n_tops` workgroups
-    uint32_t n_tops;
-    float up;          // a power of two that dZ is held with
-    RowFactor *row;
+    const float *tops; // null, or the largest |weight| of each of kWeightBlocks workgroups
+    float up;          // a power of two that dZ is held with, where tops is null
     float *power;      // what the products' sums are multiplied by
 };
 
-constexpr uint32_t kWeightBlocks = 64;
+constexpr uint32_t kWeightBlocks = 64; // a wavefront's lanes
 
 // the largest finite |weight| among the rows that count
 __global__ __launch_bounds__(256) void k_loss_weight_top(FactorArgs a, float *tops)
@@ -289,43 +398,61 @@ __global__ __launch_bounds__(256) void k_loss_weight_top(FactorArgs a, float *to
     if (threadIdx.x == 0) tops[blockIdx.x] = lds[0];
 }
 
-__global__ __launch_bounds__(256) void k_loss_factors(FactorArgs a)
+// the power of two that dZ is held with: the largest |dZ| comes into [2^14, 2^15)
+__device__ __forceinline__ float up_of(const FactorArgs &a)
 {
-    float up = a.up;
-    if (a.tops) { // the largest |dZ| comes into [2^14, 2^15)
-        float top = 0.0f;
-        for (uint32_t i = 0; i < a.n_tops; ++i) top = fmaxf(top, a.tops[i]);
-        up = ldexpf(1.0f, top > 0.0f ? min(15 - __builtin_amdgcn_frexp_expf(top), 126) : 0);
-    }
-    const uint32_t live = a.rows.live();
-    const uint64_t m = blockIdx.x * 256ull + threadIdx.x;
-    if (m == 0) {
-        const float total = a.total ? *a.total : 1.0f;
-        *a.power = total != 0.0f ? (a.dloss ? *a.dloss : 1.0f) / total / up : 0.0f;
-    }
-    if (m >= live) return;
-    RowFactor f{a.lse[m], 0.0f, a.labels.of(m), 0};
-    const float w = f.label == kNone ? 0.0f : a.weight ? a.weight[m] : 1.0f;
-    if (w != 0.0f) f.factor = w * up;
-    a.row[m] = f;
+    if (!a.tops) return a.up;
+    float top = a.tops[threadIdx.x & 63];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    return ldexpf(1.0f, top > 0.0f ? min(15 - __builtin_amdgcn_frexp_expf(top), 126) : 0);
 }
 
-template <class T> struct DzArgs : ProductArgs { // N = the piece's classes; Y: [M, N rounded up to eight]
-    const RowFactor *row;
+// by one lane of the first launch that makes dZ, whatever rows there are
+__device__ __forceinline__ void put_power(const FactorArgs &a)
+{
+    if (block_number() != 0 || threadIdx.x >= 64) return;
+    const float up = up_of(a), total = a.total ? *a.total : 1.0f;
+    if (threadIdx.x == 0) *a.power = total != 0.0f ? (float)((a.dloss ? (double)*a.dloss : 1.0) / (double)total / (double)up) : 0.0f;
+}
+
+__device__ __forceinline__ RowFactor factor_of(const FactorArgs &a, uint32_t m, float up)
+{
+    RowFactor f{a.lse[m], 0.0f, a.labels.of(m)};
+    const float w = a.weight ? a.weight[m] : 1.0f;
+    if (f.label != kNone && w != 0.0f) f.factor = w * up;
+    return f;
+}
+
+template <class T> struct DzArgs : ProductArgs {
+    static constexpr int high = 8;
+    // N = the piece's classes; Y: [M, N rounded up to eight]
+    FactorArgs f;
     uint32_t first;   // the piece's first class
     float *bias_part; // null, or [groups of rows][ld_part]: the sums of dZ over a wavefront's rows
     int64_t ld_part;
 };
 
-// eight cells of a row; what is beyond the last class is 0
-__device__ __forceinline__ void dz8(const Columns &c, const RowFactor &f, uint32_t first, float (&v)[8])
+// Eight cells of a row; what is beyond the last class is 0.  Mostly a cell takes the bias, a multiplication and addition in one, an exponential and the factor; what else there may be, in any row of the
+// wavefront, is looked after in a branch of its own.
+__device__ __forceinline__ void dz8(const Columns &c, const RowFactor &f, uint32_t first, bool bias, float (&v)[8])
 {
     const uint32_t at = f.label - first - c.n;
+    if (bias) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        v[j] = f.factor * power_of(v[j] + c.bias[j], f.lse);
-        v[j] -= at == (uint32_t)j ? f.factor : 0.0f;
-        v[j] = f.factor != 0.0f && j < c.left ? v[j] : 0.0f;
+        for (int j = 0; j < 8; ++j) v[j] += c.bias[j];
+    }
+    if (__any(at < 8 || f.factor == 0.0f || c.left < 8 || !(fabsf(f.lse) < kPlainTop))) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = f.factor * power_of(v[j], f.lse);
+            v[j] -= at == (uint32_t)j ? f.factor : 0.0f;
+            v[j] = f.factor != 0.0f && j < c.left ? v[j] : 0.0f;
+        }
+    } else {
+        const float base2 = f.lse * kLog2e; // (its rounding is that of a logit of lse's size)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = f.factor * __builtin_amdgcn_exp2f(fmaf(v[j], kLog2e, -base2));
     }
 }
 
@@ -334,6 +461,7 @@ template <class T, int FM, int FN> __device__ __forceinline__ void hand_over_dz(
 {
     const uint32_t lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31, g = lane & 3;
     if (m_wave >= M) return;
+    const float up = up_of(p.f);
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         const Columns c = columns_of(p.e, n_wave + 32 * j + 8 * g, p.N);
@@ -342,10 +470,7 @@ template <class T, int FM, int FN> __device__ __forceinline__ void hand_over_dz(
         for (int i = 0; i < FM; ++i) {
             RowFactor f[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint32_t m = m_wave + 32 * i + (lane >> 2) + 16 * u;
-                f[u] = p.row[min(m, M - 1)];
-            }
+            for (int u = 0; u < 2; ++u) f[u] = factor_of(p.f, min(m_wave + 32 * i + (lane >> 2) + 16 * u, M - 1), up);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 mine[row * 8 + ((2 * q + half) ^ ((row >> 1) & 7))] = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
@@ -358,7 +483,7 @@ template <class T, int FM, int FN> __device__ __forceinline__ void hand_over_dz(
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] = lo[k], v[4 + k] = hi[k];
                 if (c.left <= 0 || m >= M) continue;
-                dz8(c, f[u], p.first, v);
+                dz8(c, f[u], p.first, p.e.bias, v);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) sums[k] += v[k];
                 store8(static_cast<T *>(p.e.Y) + m * p.e.ld_Y + c.n, 8, v, p.e.stream);
@@ -392,14 +517,14 @@ template <class T> struct Out<DzArgs<T>> {
         __device__ __forceinline__ void begin(const DzArgs<T> &p, uint32_t m, uint32_t n, uint32_t live)
         {
             c = columns_of(p.e, n, p.N);
-            f = p.row[min(m, live - 1)];
+            f = factor_of(p.f, min(m, live - 1), up_of(p.f));
         }
         template <class F> __device__ __forceinline__ void end(const DzArgs<T> &p, uint32_t m, uint32_t live, F &&sums)
         {
             float v[8];
             sums(0, v);
             if (m >= live) f.factor = 0.0f;
-            dz8(c, f, p.first, v);
+            dz8(c, f, p.first, p.e.bias, v);
             if (m < live && c.left > 0) store8(static_cast<T *>(p.e.Y) + m * p.e.ld_Y + c.n, 8, v, p.e.stream);
             if (!p.bias_part) return;
 #pragma unroll
@@ -411,11 +536,19 @@ template <class T> struct Out<DzArgs<T>> {
     };
 };
 
-template <class T> __global__ __launch_bounds__(256) void k_loss_dz_few(DzArgs<T> p) { few_tile<T>(p); }
-template <class T> __global__ __launch_bounds__(256, 2) void k_loss_dz_anyhow(DzArgs<T> p) { product_tile<T, 64, 64, false, false>(p); }
-template <class T> __global__ __launch_bounds__(256, 2) void k_loss_dz_chunks(DzArgs<T> p) { chunks_tile<T, T, 256, 128, false, false>(p); }
-template <> __global__ __launch_bounds__(256, 3) void k_loss_dz_chunks<float>(DzArgs<float> p) { chunks_tile<float, float, 128, 128, false, false>(p); }
-template <class T> __global__ __launch_bounds__(512, 2) void k_loss_dz_long(DzArgs<T> p) { long_tiles<T, T, false, false>(p); }
+template <class T> __global__ __launch_bounds__(256) void k_loss_dz_few(DzArgs<T> p) { put_power(p.f); few_tile<T>(p); }
+template <class T> __global__ __launch_bounds__(256, 2) void k_loss_dz_anyhow(DzArgs<T> p) { put_power(p.f); product_tile<T, 64, 64, false, false>(p); }
+template <class T> __global__ __launch_bounds__(256, 2) void k_loss_dz_chunks(DzArgs<T> p) { put_power(p.f); chunks_tile<T, T, 256, 128, false, false>(p); }
+template <> __global__ __launch_bounds__(256, 3) void k_loss_dz_chunks<float>(DzArgs<float> p) { put_power(p.f); chunks_tile<float, float, 128, 128, false, false>(p); }
+template <class T> __global__ __launch_bounds__(512, 2) void k_loss_dz_long(DzArgs<T> p) { put_power(p.f); long_tiles<T, T, false, false>(p); }
+
+__global__ __launch_bounds__(64) void k_loss_power(FactorArgs f) { put_power(f); } // (without rows, nobody makes dZ)
+
+template <class T> __global__ __launch_bounds__(256, 2) void k_loss_dz_narrow(DzArgs<T> p) { put_power(p.f); chunks_tile<T, T, 256, 64, false, false>(p); }
+template <> __global__ __launch_bounds__(256, 4) void k_loss_dz_narrow<float>(DzArgs<float> p) { put_power(p.f); chunks_tile<float, float, 128, 64, false, false>(p); }
+
+// Parts of dW's sum over the rows for few classes, fp32.
+__global__ __launch_bounds__(256, 4) void k_loss_part_narrow(ProductArgs p) { chunks_tile<float, float, 64, 128, true, true>(p); }
 
 // Parts of dA's sum over the classes, in fp32: those of one piece, where the tiles of [rows, in] alone would leave compute units idle, and those of the pieces.
 template <class T> __global__ __launch_bounds__(256, 2) void k_loss_part_anyhow(ProductArgs p) { product_tile<T, 64, 64, false, true>(p); }
@@ -423,20 +556,22 @@ template <class T> __global__ __launch_bounds__(256, 2) void k_loss_part_chunks(
 template <> __global__ __launch_bounds__(256, 3) void k_loss_part_chunks<float>(ProductArgs p) { chunks_tile<float, float, 128, 128, false, true>(p); }
 template <class T> __global__ __launch_bounds__(512, 2) void k_loss_part_long(ProductArgs p) { long_tiles<T, float, false, true>(p); }
 
-// dbias = power x the sum over the groups of rows: 32 classes to a workgroup, eight groups side by side, then in order.
-__global__ __launch_bounds__(256) void k_loss_bias(Rows rows, uint32_t group, uint32_t N, const float *part, int64_t ld_part, const float *power, float *out)
+// dbias = power x the sum over the groups of rows: C classes to a workgroup, 1024 / C groups side by side, then in order.
+template <int C> __global__ __launch_bounds__(1024) void k_loss_bias(Rows rows, uint32_t group, uint32_t N, const float *part, int64_t ld_part, const float *power, float *out)
 {
-    __shared__ float lds[8][32];
-    const uint32_t n = blockIdx.x * 32 + (threadIdx.x & 31), g = threadIdx.x >> 5, groups = (rows.live() + group - 1) / group;
+    constexpr int G = 1024 / C;
+    __shared__ float lds[G][C];
+    const uint32_t c = threadIdx.x % C, n = blockIdx.x * C + c, g = threadIdx.x / C, groups = (rows.live() + group - 1) / group;
     float sum = 0.0f;
     if (n < N)
-        for (uint32_t i = g; i < groups; i += 8) sum += part[i * ld_part + n];
-    lds[g][threadIdx.x & 31] = sum;
+        for (uint32_t i = g; i < groups; i += G) sum += part[i * ld_part + n];
+    lds[g][c] = sum;
     __syncthreads();
-    if (g || n >= N) return;
-#pragma unroll
-    for (int i = 1; i < 8; ++i) sum += lds[i][threadIdx.x];
-    out[n] = sum * *power;
+    for (int k = G / 2; k > 0; k >>= 1) {
+        if (g < (uint32_t)k) lds[g][c] += lds[g + k][c];
+        __syncthreads();
+    }
+    if (g == 0 && n < N) out[n] = lds[0][c] * *power;
 }
 
 // ---- operands that lie anyhow -----------------------------------------------------------------------------------------------------
@@ -454,22 +589,27 @@ template <class T> __global__ __launch_bounds__(256) void k_loss_pack(const T *f
 
 // ---- host side --------------------------------------------------------------------------------------------------------------------
 
-enum Kind { kFew, kAnyhow, kChunks, kLong };
+enum Kind { kFew, kAnyhow, kChunks, kLong, kNarrow, kRow };
+
+constexpr uint32_t kRowBytes = 16 << 10; // of a row of A, up to four of which k_loss_top_rows has in LDS
 
 // which kernel makes the logits of [M, N], K terms each
-template <class T> Kind kind_of(const ProductArgs &p)
+template <class T> Kind kind_of(const ProductArgs &p, bool tops)
 {
     const bool chunks = in_chunks<T>(p.a, p.M, p.K) && in_chunks<T>(p.b, p.N, p.K);
+    if (tops && chunks && p.M <= 4 && p.K * sizeof(T) <= kRowBytes) return kRow;
     if (few_tiles<T>(p, chunks)) return kFew;
     if (!chunks) return kAnyhow;
+    if (p.N <= 64) return kNarrow;
     if (sizeof(T) == 4) return kChunks;
     return tile_blocks<256, 256>(p) >= 256 && p.K * sizeof(T) >= 2048 ? kLong : kChunks;
 }
 
-constexpr uint32_t slot_width(Kind k) { return k == kFew || k == kAnyhow ? 32 : 64; } // columns of a Top
-constexpr uint32_t group_rows(Kind k, bool f32) { return k == kFew ? 16 : k == kAnyhow ? 32 : k == kChunks && f32 ? 64 : 128; } // rows of a sum for dbias
+constexpr uint32_t slot_width(Kind k) { return k == kChunks || k == kLong ? 64 : 32; } // columns of a Top
+constexpr uint32_t group_rows(Kind k, bool f32) { return k == kFew ? 16 : k == kAnyhow ? 32 : f32 ? 64 : 128; } // rows of a sum for dbias
 
-constexpr int64_t kPieceBytes = int64_t(1) << 30; // of dZ
+// Of dZ.  More has it go through memory twice, less makes dA of more parts: 16384 x 1024 x 65536 bf16, all gradients, with 2^27 .. 2^31 bytes 7.5, 7.2, 6.9, 7.0, 7.0 ms.
+constexpr int64_t kPieceBytes = int64_t(1) << 29;
 constexpr double kPackFlops = 2e9;                // products from here on are worth a copy of operands that lie anyhow
 
 struct Shape {
@@ -534,12 +674,13 @@ ProductArgs logits_product(const Shape &s, const Packed &pk, const uint32_t *d_r
 }
 
 // Addresses only matter for their alignment here: copies' are null.
-Kind logits_kind(int32_t dtype, const ProductArgs &p) { return (Kind)with_wide_type(dtype, [&](auto t) { return (int)kind_of<decltype(t)>(p); }); }
+Kind logits_kind(int32_t dtype, const ProductArgs &p, bool tops) { return (Kind)with_wide_type(dtype, [&](auto t) { return (int)kind_of<decltype(t)>(p, tops); }); }
 
 struct TopPlan {
     Packed pk;
     Kind kind;
-    uint32_t slots, row_block, row_grid;
+    uint32_t slots, row_grid;
+    RowShape shape;
     size_t off_pack[2], off_part, off_at, off_sums, total;
 };
 
@@ -558,13 +699,12 @@ TopPlan top_plan(const Shape &s)
     TopPlan t{};
     const Taker take{t.total};
     t.pk = packed_plan(s, take, t.off_pack);
-    t.kind = logits_kind(s.dtype, logits_product(s, t.pk, nullptr));
+    t.kind = logits_kind(s.dtype, logits_product(s, t.pk, nullptr), true);
     t.slots = ((uint32_t)s.out + slot_width(t.kind) - 1) / slot_width(t.kind);
     t.off_part = take((size_t)t.slots * s.rows * sizeof(Top));
     t.off_at = take((size_t)s.rows * sizeof(float));
-    // a workgroup for each of few rows with many parts; whole rows side by side where there are few parts
-    t.row_block = s.rows <= 64 && t.slots > 32 ? 1 : t.slots <= 4 ? 256 : 32;
-    t.row_grid = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(1024, (s.rows + t.row_block - 1) / t.row_block));
+    t.shape = row_shape(s.rows, t.slots);
+    t.row_grid = t.shape == kRowsAll ? 1 : (uint32_t)std::max<int64_t>(1, std::min<int64_t>(1024, (s.rows + rows_of(t.shape) - 1) / rows_of(t.shape)));
     t.off_sums = take((size_t)t.row_grid * 2 * sizeof(double));
     return t;
 }
@@ -574,7 +714,7 @@ struct DzPlan {
     Kind kind;
     int64_t piece, pieces, ld_dz;
     uint32_t splits_A, slots_A, splits_W; // parts of a piece's sum for dA, parts that there is room for, parts of dW's
-    size_t off_pack[2], off_row, off_power, off_tops, off_dz, off_part_A, off_part_W, off_bias, total;
+    size_t off_pack[2], off_power, off_tops, off_dz, off_part_A, off_part_W, off_bias, total;
 };
 
 DzPlan dz_plan(const Shape &s, bool dA, bool dW, bool dbias, bool weight)
@@ -589,10 +729,9 @@ DzPlan dz_plan(const Shape &s, bool dA, bool dW, bool dbias, bool weight)
     t.ld_dz = (t.piece + 7) / 8 * 8;
     Shape one = s;
     one.out = (int32_t)t.piece;
-    t.kind = logits_kind(s.dtype, logits_product(one, t.pk, nullptr));
-    t.off_row = take((size_t)s.rows * sizeof(RowFactor));
+    t.kind = logits_kind(s.dtype, logits_product(one, t.pk, nullptr), false);
     t.off_power = take(sizeof(float));
-    if (weight && s.dtype == ZG_F16) t.off_tops = take(kWeightBlocks * sizeof(float));
+    if (weight) t.off_tops = take(kWeightBlocks * sizeof(float));
     t.off_dz = take((size_t)s.rows * t.ld_dz * e);
     const int64_t tiles_A = (rows + 255) / 256 * ((s.in + 127) / 128), tiles_W = (t.piece + 255) / 256 * ((s.in + 127) / 128);
     t.splits_A = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(512 / tiles_A, t.piece / 1024));
@@ -657,6 +796,12 @@ template <class T> int launch_tops(hipStream_t st, Kind kind, const TopArgs &p)
 {
     if (kind == kFew) return launch(st, k_loss_top_few<T>, grid_of((uint64_t)((p.M + 31) / 32) * ((p.N + 31) / 32)), 256, p);
     if (kind == kAnyhow) return launch(st, k_loss_top_anyhow<T>, tile_grid<64, 64>(p), 256, p);
+    if (kind == kNarrow) return launch(st, k_loss_top_narrow<T>, sizeof(T) == 4 ? tile_grid<128, 64>(p) : tile_grid<256, 64>(p), 256, p);
+    if (kind == kRow) {
+        const dim3 grid = grid_of(((uint64_t)p.N + 127) / 128);
+        const uint32_t row = p.K * sizeof(T);
+        return p.M == 1 ? launch_lds(st, k_loss_top_rows<T, 1>, grid, 256, row, p) : launch_lds(st, k_loss_top_rows<T, 4>, grid, 256, 4 * row, p);
+    }
     if constexpr (sizeof(T) == 4) {
         return launch(st, k_loss_top_chunks<T>, tile_grid<128, 128>(p), 256, p);
     } else {
@@ -669,6 +814,7 @@ template <class T> int launch_dz(hipStream_t st, Kind kind, const DzArgs<T> &p)
 {
     if (kind == kFew) return launch(st, k_loss_dz_few<T>, grid_of((uint64_t)((p.M + 31) / 32) * ((p.N + 31) / 32)), 256, p);
     if (kind == kAnyhow) return launch(st, k_loss_dz_anyhow<T>, tile_grid<64, 64>(p), 256, p);
+    if (kind == kNarrow) return launch(st, k_loss_dz_narrow<T>, sizeof(T) == 4 ? tile_grid<128, 64>(p) : tile_grid<256, 64>(p), 256, p);
     if constexpr (sizeof(T) == 4) {
         return launch(st, k_loss_dz_chunks<T>, tile_grid<128, 128>(p), 256, p);
     } else {
@@ -742,7 +888,13 @@ int zg_linear_cross_entropy(const zg_linear_cross_entropy_args *a, void *d_works
         r.slots = t.slots, r.cap = (uint32_t)a->rows, r.part = part, r.at_label = at, r.weight = a->d_weight, r.labels = labels;
         r.lse = a->d_lse, r.row_loss = a->d_row_loss, r.sums = reinterpret_cast<double *>(ws + t.off_sums), r.loss = a->d_loss, r.total = a->d_total;
         const dim3 grid(t.row_grid);
-        ZG_TRY(t.row_block == 1 ? launch(st, k_loss_rows<1>, grid, 256, r) : t.row_block == 32 ? launch(st, k_loss_rows<32>, grid, 256, r) : launch(st, k_loss_rows<256>, grid, 256, r));
+        switch (t.shape) {
+        case kRowsOne: ZG_TRY(launch(st, k_loss_rows<1, 1024>, grid, 1024, r)); break;
+        case kRows8: ZG_TRY(launch(st, k_loss_rows<8, 128>, grid, 1024, r)); break;
+        case kRows32: ZG_TRY(launch(st, k_loss_rows<32, 32>, grid, 1024, r)); break;
+        case kRowsWide: ZG_TRY(launch(st, k_loss_rows<256, 1>, grid, 256, r)); break;
+        case kRowsAll: ZG_TRY(launch(st, k_loss_rows<1024, 1>, grid, 1024, r)); break;
+        }
         return t.row_grid > 1 ? launch(st, k_loss_mean, dim3(1), 64, r, t.row_grid) : ZG_OK;
     });
 }
@@ -788,15 +940,15 @@ int zg_linear_cross_entropy_backward(const zg_linear_cross_entropy_grad_args *a,
         f.rows = rows;
         f.lse = a->d_lse, f.weight = a->d_weight, f.total = a->d_total, f.dloss = a->d_dloss;
         f.labels = {a->d_labels, a->label_dtype == ZG_I64, (uint32_t)a->out};
-        // fp16's range does not hold a softmax over many classes as it is: |dZ| / |weight| <= 1 is brought to the top of it (the other types' does)
+        // fp16's range does not hold a softmax over many classes as it is: |dZ| <= 1 is brought to the top of it.  Weights may be of any size: the largest is brought there, whatever the type.
         f.up = a->dtype == ZG_F16 ? 16384.0f : 1.0f;
-        f.row = reinterpret_cast<RowFactor *>(ws + t.off_row), f.power = power;
-        if (a->d_weight && a->dtype == ZG_F16 && a->rows > 0) {
+        f.power = power;
+        if (a->d_weight && a->rows > 0) {
             float *const tops = reinterpret_cast<float *>(ws + t.off_tops);
-            f.tops = tops, f.n_tops = kWeightBlocks;
+            f.tops = tops;
             ZG_TRY(launch(st, k_loss_weight_top, dim3(kWeightBlocks), 256, f, tops));
         }
-        ZG_TRY(launch(st, k_loss_factors, dim3((unsigned)std::max<int64_t>(1, (a->rows + 255) / 256)), 256, f));
+        if (a->rows == 0) ZG_TRY(launch(st, k_loss_power, dim3(1), 64, f));
         const auto run = [&](auto zero) -> int {
             using T = decltype(zero);
             T *const dz = reinterpret_cast<T *>(ws + t.off_dz);
@@ -816,12 +968,15 @@ int zg_linear_cross_entropy_backward(const zg_linear_cross_entropy_grad_args *a,
                     p.b = w;
                     p.e.bias = a->d_bias ? a->d_bias + first : nullptr;
                     p.e.Y = dz, p.e.ld_Y = t.ld_dz;
-                    p.row = f.row, p.first = (uint32_t)first;
+                    p.f = f, p.first = (uint32_t)first;
                     p.bias_part = want_b ? bias_part : nullptr, p.ld_part = t.ld_dz;
                     ZG_TRY(launch_dz(st, t.kind, p));
                 }
-                if (want_b)
-                    ZG_TRY(launch(st, k_loss_bias, dim3((n + 31) / 32), 256, rows, group_rows(t.kind, sizeof(T) == 4), n, bias_part, t.ld_dz, power, a->d_dbias + first));
+                if (want_b) {
+                    const uint32_t group = group_rows(t.kind, sizeof(T) == 4);
+                    if (n < 1024) ZG_TRY(launch(st, k_loss_bias<8>, dim3((n + 7) / 8), 1024, rows, group, n, bias_part, t.ld_dz, power, a->d_dbias + first));
+                    else ZG_TRY(launch(st, k_loss_bias<32>, dim3((n + 31) / 32), 1024, rows, group, n, bias_part, t.ld_dz, power, a->d_dbias + first));
+                }
                 if (want_W) {
                     ProductArgs p{};
                     p.a = {dz, t.ld_dz, true, true};
@@ -831,7 +986,16 @@ int zg_linear_cross_entropy_backward(const zg_linear_cross_entropy_grad_args *a,
                     p.splits = t.splits_W;
                     p.e.factor = 1.0f, p.e.power = power, p.e.type = a->dtype;
                     p.e.Y = static_cast<T *>(a->d_dW) + first * a->ld_dW, p.e.ld_Y = a->ld_dW;
-                    ZG_TRY(dense_product(st, a->dtype, p, reinterpret_cast<float *>(ws + t.off_part_W)));
+                    float *const part = reinterpret_cast<float *>(ws + t.off_part_W);
+                    if (sizeof(T) == 4 && n <= 64 && p.splits > 1 && in_chunks<T>(p.b, p.N, p.K)) { // (dense_product's tiles have 128 classes: 98765 rows x 47 x 256 61 us)
+                        const Epilogue result = p.e;
+                        p.e = Epilogue{};
+                        p.e.factor = 1.0f, p.e.type = ZG_F32, p.e.Y = part, p.e.ld_Y = p.N, p.e.part = (int64_t)p.M * p.N;
+                        ZG_TRY(launch(st, k_loss_part_narrow, tile_grid<64, 128>(p), 256, p));
+                        ZG_TRY(dense_join(st, part, p.M, p.N, p.splits, result, {nullptr, p.M}));
+                    } else {
+                        ZG_TRY(dense_product(st, a->dtype, p, part));
+                    }
                 }
                 if (want_A && a->rows > 0) {
                     ProductArgs p{};

@@ -85,3 +85,116 @@ def test_muon_step(size, kinds):
         assert float(err.clamp_min(0).norm()) <= float(O.SLACK * off + 4 * 2.0**-24 * (before.norm() + lr * s * cells))
         _untouched(whole_w, rows, cols, "w")
         _untouched(whole_m, rows, cols, "m")
+
+
+@pytest.mark.parametrize("kind", [F32, F16, BF16])
+@pytest.mark.parametrize("size", [(40, 60), (300, 260), (600, 520)], ids=str)
+def test_values_of_every_size(size, kind):
+    """Matrices of zeros, of one direction, of very large and very small values (their squares are beyond fp32), with empty rows and columns."""
+    g = _gen(size, str(kind), "values")
+    rows, cols = size
+    assert not layers.orthogonalize(torch.zeros(rows, cols, dtype=kind, device="cuda")).any()
+    base = _matrix(g, rows, cols, F32)
+    base[rows // 3:rows // 2] = 0
+    base[:, cols // 3:cols // 2] = 0
+    for scale in {F32: (1.0, 1e30, 1e-30), F16: (1.0, 1e3, 1e-3), BF16: (1.0, 1e30, 1e-30)}[kind]:
+        m = (base * scale).to(kind)
+        o = layers.orthogonalize(m, eps=1e-38)
+        O.check(o, m, kind, eps=1e-38, what=str(scale))
+        assert not o[rows // 3:rows // 2].any() and not o[:, cols // 3:cols // 2].any()
+    one = (torch.randn(rows, 1, device="cuda", generator=g) * torch.randn(1, cols, device="cuda", generator=g)).to(kind)
+    O.check(layers.orthogonalize(one), one, kind)
+    tiny = torch.full((rows, cols), 1e-3, device="cuda").to(kind)  # eps counts where the matrix is small
+    O.check(layers.orthogonalize(tiny, eps=10.0), tiny, kind, eps=10.0)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_what_is_not_finite_shows(bad):
+    for size in ((40, 60), (300, 260)):
+        m = _matrix(_gen(size), *size, F32)
+        m[3, 5] = bad
+        assert not torch.isfinite(layers.orthogonalize(m)).all()
+
+
+@pytest.mark.parametrize("coefficients,steps", [((1.5, -0.5, 0.0), 12), ((1.5, -0.5, 0.0), 1), ((1.875, -1.25, 0.375), 8), (O.MUON, 10), ([(4.0, -6.0, 2.5), (2.0, -1.5, 0.5), (1.5, -0.5, 0.0)], 3),
+                                                ((0.0, 0.0, 0.0), 2), ((2.0, 0.0, 0.0), 6)], ids=str)
+@pytest.mark.parametrize("kind", [F32, BF16])
+def test_other_coefficients(kind, coefficients, steps):
+    for size in ((50, 70), (300, 280)):
+        m = _matrix(_gen(size, steps), *size, kind)
+        triples = coefficients if isinstance(coefficients, tuple) else tuple(coefficients)
+        o = layers.orthogonalize(m, coefficients=coefficients, steps=steps)
+        O.check(o, m, kind, steps, list(triples) if isinstance(triples[0], tuple) else triples)
+
+
+def test_the_result_may_be_the_matrix():
+    for size in ((40, 60), (300, 260), (1030, 500)):
+        m = _matrix(_gen(size, "in place"), *size, BF16)
+        want = layers.orthogonalize(m)
+        assert layers.orthogonalize(m, out=m) is m and torch.equal(m, want)
+
+
+def test_a_tall_matrix_is_a_wide_one_turned():
+    for size in ((70, 50), (700, 300), (1100, 1030)):
+        m = _matrix(_gen(size, "turned"), *size, F32)
+        assert torch.equal(layers.orthogonalize(m), layers.orthogonalize(m.t().contiguous()).t())
+
+
+def test_an_update_is_its_parts():
+    g = _gen("parts")
+    w, m, d = _matrix(g, 300, 400, F32), _matrix(g, 300, 400, F32), _matrix(g, 300, 400, F32)
+    new = 0.5 * m + d  # (halves are exact: one rounding, as in the kernel)
+    o = layers.orthogonalize(0.5 * new + d)
+    want = 0.75 * w.double() - 0.25 * o.double()
+    got = layers.muon_step(w, m, d, lr=0.25, momentum=0.5, decay=1.0, scale=1.0)
+    assert torch.equal(m, new)
+    # (o is rounded in between: half a unit of fp32, times 0.25, and so is w)
+    assert float((got.double() - want).abs().max()) <= 2 * 2.0**-24 * float(want.abs().max() + o.abs().max())
+
+
+def test_one_call_gives_the_same_bits_each_time_on_any_stream_and_in_a_graph():
+    g = _gen("bits")
+    for size, kind in (((130, 90), F32), ((600, 1030), BF16), ((1030, 260), F32)):
+        x = _matrix(g, *size, kind)
+        want = layers.orthogonalize(x)
+        for stream in (None, torch.cuda.Stream()):
+            got = layers.orthogonalize(x, stream=stream)
+            torch.cuda.synchronize()
+            assert torch.equal(got, want)
+        w0, m0 = _matrix(g, *size, kind), _matrix(g, *size, F32)
+        w, m = w0.clone(), m0.clone()
+        eager_w, eager_m = w0.clone(), m0.clone()
+        layers.muon_step(w, m, x, lr=0.1)
+        layers.muon_step(eager_w, eager_m, x, lr=0.1)
+        w.copy_(w0), m.copy_(m0)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            layers.muon_step(w, m, x, lr=0.1)
+            out = layers.orthogonalize(x)
+        eager_w.copy_(w0), eager_m.copy_(m0)
+        for _ in range(4):
+            graph.replay()
+            layers.muon_step(eager_w, eager_m, x, lr=0.1)
+            torch.cuda.synchronize()
+            assert torch.equal(w, eager_w) and torch.equal(m, eager_m) and torch.equal(out, want)
+
+
+def test_calls_on_two_streams_at_once():
+    g = _gen("two")
+    a, b = _matrix(g, 700, 900, BF16), _matrix(g, 300, 280, F32)
+    want = layers.orthogonalize(a), layers.orthogonalize(b)
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = [(layers.orthogonalize(a, stream=s), layers.orthogonalize(b, stream=t)) for _ in range(10)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want[0]) and torch.equal(y, want[1]) for x, y in got)
+
+
+def test_rows_more_than_2_to_the_32_elements_apart():
+    rows, cols, ld = 1100, 300, 1 << 22
+    store = torch.empty(rows * ld, dtype=BF16, device="cuda").view(rows, ld)
+    far, out = store[:, :cols], store[:, 1024:1024 + cols]
+    far.copy_(_matrix(_gen("far"), rows, cols, F32))
+    near = far.contiguous()
+    layers.orthogonalize(far, out=out)
+    assert torch.equal(out, layers.orthogonalize(near))
