@@ -59,6 +59,8 @@ def _check_loss(r, want, live, what=""):
         R.check(getattr(r, name), *want[name], f"{name} {what}")
 
 
+ROUTES = [  # sizes that the library's rules send to the kernels that those above do not reach (test_step_routes)
+    (100, 64, 5000, 0, 0), (70000, 264, 64, 0, 0), (99000, 64, 47, 0, 0), (30000, 133, 129, 1, 0), (8193, 133, 257, 1, 0), (700, 133, 2100, 0, 1), (3001, 301, 1303, 3, 0), (9000, 1032, 2064, 0, 0), (4500, 1032, 3080, 0, 0)]
 SIZES = [  # rows, in, classes, pad, shift
     (1, 1, 1, 0, 0), (1, 1, 2, 0, 0), (1, 256, 512, 0, 0), (1, 1024, 5003, 0, 0), (2, 7, 5, 1, 1), (3, 301, 47, 2, 0), (16, 128, 33, 0, 0), (17, 64, 64, 0, 0), (31, 40, 8, 0, 0),
     (65, 1000, 129, 8, 0), (64, 128, 128, 0, 0), (127, 96, 255, 8, 8), (257, 200, 257, 0, 0), (300, 602, 41, 0, 1), (611, 256, 16, 0, 0), (515, 33, 1000, 3, 1), (700, 512, 3001, 0, 0),
@@ -95,6 +97,26 @@ def test_gradients(size, kind):
             R.check(x, y, bound, f"{what} {i}")
         _untouched(whole_a, rows, k, "da")
         _untouched(whole_w, n, k, "dw")
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", ROUTES, ids=str)
+def test_other_kernels(size, kind):
+    rows, k, n, pad, shift = size
+    g = _gen(size, str(kind), "routes")
+    a, w, labels, bias, weight = _inputs(g, rows, k, n, kind, pad, shift)
+    weight = weight if pad else None
+    live = rows - rows // 11
+    dev = torch.tensor([live], dtype=torch.int32, device="cuda")
+    r = layers.linear_cross_entropy(a, w, labels, bias=bias, weight=weight, rows=dev, row_loss=True)
+    _check_loss(r, L.loss(a, w, labels, bias, weight, live), live)
+    whole_a, da = _buffer(rows, k, kind)
+    whole_w, dw = _buffer(n, k, kind)
+    db = layers.linear_cross_entropy_backward(a, w, labels, r.lse, bias=bias, weight=weight, total=r.total, rows=dev, da=da, dw=dw)[2]
+    for x, (y, bound), what in zip((da[:live], dw, db), L.gradients(a, w, labels, kind, bias, weight, live), ("da", "dw", "dbias")):
+        R.check(x, y, bound, what)
+    _untouched(whole_a, live, k, "da")
+    _untouched(whole_w, n, k, "dw")
 
 
 @pytest.mark.parametrize("kind", KINDS)

@@ -40,6 +40,7 @@ def _untouched(whole, rows, cols, what):
         assert bool((part == ok).all()), f"{what}: something was written outside"
 
 
+ROUTES = [(2300, 2310, 0, 0), (3000, 2900, 0, 0), (4000, 4010, 0, 0)]  # sizes that the library's rules send to the kernels that those below do not reach (test_step_routes)
 SIZES = [  # rows, cols, pad, shift
     (1, 1, 0, 0), (1, 50, 0, 0), (50, 1, 1, 1), (2, 3, 0, 0), (7, 5, 1, 0), (16, 16, 0, 0), (31, 33, 3, 1), (33, 31, 0, 0), (47, 256, 0, 0), (64, 64, 8, 0), (100, 1000, 0, 0), (1000, 100, 0, 0),
     (255, 255, 1, 1), (256, 256, 0, 0), (257, 300, 0, 0), (300, 257, 2, 3), (600, 1201, 3, 0), (1201, 600, 0, 0), (8, 4096, 0, 0), (1025, 1100, 0, 0), (1536, 1280, 0, 0), (2050, 700, 1, 0), (2100, 2300, 0, 0), (700, 5003, 0, 0)]
@@ -56,6 +57,12 @@ def test_orthogonalize(size, kinds):
     assert got is o
     O.check(o, m, out)
     _untouched(whole, rows, cols, "o")
+
+
+@pytest.mark.parametrize("kinds", [(F32, F32), (BF16, BF16)], ids=str)
+@pytest.mark.parametrize("size", ROUTES, ids=str)
+def test_other_kernels(size, kinds):
+    test_orthogonalize(size, kinds)
 
 
 @pytest.mark.parametrize("kinds", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)], ids=str)  # of w and of g
