@@ -179,7 +179,7 @@ template <> __global__ __launch_bounds__(256, 3) void k_loss_top_chunks<float>(T
 template <class T> __global__ __launch_bounds__(512, 2) void k_loss_top_long(TopArgs p) { long_tiles<T, T, false, false>(p); }
 
 template <class T> __global__ __launch_bounds__(256, 2) void k_loss_top_narrow(TopArgs p) { chunks_tile<T, T, 256, 64, false, false>(p); }
-template <> __global__ __launch_bounds__(256, 4) void k_loss_top_narrow<float>(TopArgs p) { chunks_tile<float, float, 128, 64, false, false>(p); }
+template <> __global__ __launch_bounds__(256, 4) void k_loss_top_narrow<float>(TopArgs p) { chunks_tile<float, float, 64, 64, false, false, 8, 2>(p); }
 
 // A chunk's products, summed in fp32.
 template <class T> __device__ __forceinline__ float dot_chunk(u32x4 a, u32x4 b, float sum)
@@ -461,16 +461,20 @@ template <class T, int FM, int FN> __device__ __forceinline__ void hand_over_dz(
 {
     const uint32_t lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31, g = lane & 3;
     if (m_wave >= M) return;
-    const float up = up_of(p.f);
+    RowFactor f[FM][2]; // (all at once: a load between the stores would wait for them)
+    {
+        const float up = up_of(p.f);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) f[i][u] = factor_of(p.f, min(m_wave + 32 * i + (lane >> 2) + 16 * u, M - 1), up);
+    }
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         const Columns c = columns_of(p.e, n_wave + 32 * j + 8 * g, p.N);
         float sums[8] = {};
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            RowFactor f[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) f[u] = factor_of(p.f, min(m_wave + 32 * i + (lane >> 2) + 16 * u, M - 1), up);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 mine[row * 8 + ((2 * q + half) ^ ((row >> 1) & 7))] = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
@@ -483,7 +487,7 @@ template <class T, int FM, int FN> __device__ __forceinline__ void hand_over_dz(
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] = lo[k], v[4 + k] = hi[k];
                 if (c.left <= 0 || m >= M) continue;
-                dz8(c, f[u], p.first, p.e.bias, v);
+                dz8(c, f[i][u], p.first, p.e.bias, v);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) sums[k] += v[k];
                 store8(static_cast<T *>(p.e.Y) + m * p.e.ld_Y + c.n, 8, v, p.e.stream);
@@ -545,13 +549,13 @@ template <class T> __global__ __launch_bounds__(512, 2) void k_loss_dz_long(DzAr
 __global__ __launch_bounds__(64) void k_loss_power(FactorArgs f) { put_power(f); } // (without rows, nobody makes dZ)
 
 template <class T> __global__ __launch_bounds__(256, 2) void k_loss_dz_narrow(DzArgs<T> p) { put_power(p.f); chunks_tile<T, T, 256, 64, false, false>(p); }
-template <> __global__ __launch_bounds__(256, 4) void k_loss_dz_narrow<float>(DzArgs<float> p) { put_power(p.f); chunks_tile<float, float, 128, 64, false, false>(p); }
+template <> __global__ __launch_bounds__(256, 4) void k_loss_dz_narrow<float>(DzArgs<float> p) { put_power(p.f); chunks_tile<float, float, 64, 64, false, false, 8, 2>(p); }
 
 // Parts of dW's sum over the rows for few classes, fp32.
 __global__ __launch_bounds__(256, 4) void k_loss_part_narrow(ProductArgs p) { chunks_tile<float, float, 64, 128, true, true>(p); }
 
 // Parts of dA's sum over the classes, in fp32: those of one piece, where the tiles of [rows, in] alone would leave compute units idle, and those of the pieces.
-template <class T> __global__ __launch_bounds__(256, 2) void k_loss_part_anyhow(ProductArgs p) { product_tile<T, 64, 64, false, true>(p); }
+template <class T> __global__ __launch_bounds__(256, 2) void k_loss_part_anyhow(ProductArgs p) { product_tile<T, 64, 64, false, true>(p); } // (or of dA itself where that is small)
 template <class T> __global__ __launch_bounds__(256, 2) void k_loss_part_chunks(ProductArgs p) { chunks_tile<T, float, 256, 128, false, true>(p); }
 template <> __global__ __launch_bounds__(256, 3) void k_loss_part_chunks<float>(ProductArgs p) { chunks_tile<float, float, 128, 128, false, true>(p); }
 template <class T> __global__ __launch_bounds__(512, 2) void k_loss_part_long(ProductArgs p) { long_tiles<T, float, false, true>(p); }
@@ -563,8 +567,10 @@ template <int C> __global__ __launch_bounds__(1024) void k_loss_bias(Rows rows, 
     __shared__ float lds[G][C];
     const uint32_t c = threadIdx.x % C, n = blockIdx.x * C + c, g = threadIdx.x / C, groups = (rows.live() + group - 1) / group;
     float sum = 0.0f;
-    if (n < N)
+    if (n < N) {
+#pragma unroll 4
         for (uint32_t i = g; i < groups; i += G) sum += part[i * ld_part + n];
+    }
     lds[g][c] = sum;
     __syncthreads();
     for (int k = G / 2; k > 0; k >>= 1) {
@@ -606,7 +612,7 @@ template <class T> Kind kind_of(const ProductArgs &p, bool tops)
 }
 
 constexpr uint32_t slot_width(Kind k) { return k == kChunks || k == kLong ? 64 : 32; } // columns of a Top
-constexpr uint32_t group_rows(Kind k, bool f32) { return k == kFew ? 16 : k == kAnyhow ? 32 : f32 ? 64 : 128; } // rows of a sum for dbias
+constexpr uint32_t group_rows(Kind k, bool f32) { return k == kFew ? 16 : k == kAnyhow || (k == kNarrow && f32) ? 32 : f32 ? 64 : 128; } // rows of a sum for dbias
 
 // Of dZ.  More has it go through memory twice, less makes dA of more parts: 16384 x 1024 x 65536 bf16, all gradients, with 2^27 .. 2^31 bytes 7.5, 7.2, 6.9, 7.0, 7.0 ms.
 constexpr int64_t kPieceBytes = int64_t(1) << 29;
@@ -734,8 +740,11 @@ DzPlan dz_plan(const Shape &s, bool dA, bool dW, bool dbias, bool weight)
     if (weight) t.off_tops = take(kWeightBlocks * sizeof(float));
     t.off_dz = take((size_t)s.rows * t.ld_dz * e);
     const int64_t tiles_A = (rows + 255) / 256 * ((s.in + 127) / 128), tiles_W = (t.piece + 255) / 256 * ((s.in + 127) / 128);
-    t.splits_A = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(512 / tiles_A, t.piece / 1024));
-    t.splits_W = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(512 / tiles_W, (rows + 255) / 256));
+    // Parts enough for two tiles of 256 x 128 to a compute unit; where tiles of 256 x 256, which would be taken from 256 of them on, were a third empty, fewer than that.
+    const int64_t wide_A = (rows + 255) / 256 * ((s.in + 255) / 256), wide_W = (t.piece + 255) / 256 * ((s.in + 255) / 256);
+    const bool narrow = s.dtype != ZG_F32 && (s.in + 255) / 256 * 256 * 3 >= (s.in + 127) / 128 * 128 * 4;
+    t.splits_A = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(narrow ? std::min(512 / tiles_A, 255 / wide_A) : 512 / tiles_A, t.piece / 1024));
+    t.splits_W = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(narrow ? std::min(512 / tiles_W, 255 / wide_W) : 512 / tiles_W, (rows + 255) / 256));
     const int64_t parts = t.pieces * t.splits_A;
     t.slots_A = (uint32_t)(parts == 1 ? 0 : std::min<int64_t>(parts, t.splits_A + 4));
     if (dA) t.off_part_A = take((size_t)t.slots_A * s.rows * s.in * sizeof(float));
@@ -796,7 +805,7 @@ template <class T> int launch_tops(hipStream_t st, Kind kind, const TopArgs &p)
 {
     if (kind == kFew) return launch(st, k_loss_top_few<T>, grid_of((uint64_t)((p.M + 31) / 32) * ((p.N + 31) / 32)), 256, p);
     if (kind == kAnyhow) return launch(st, k_loss_top_anyhow<T>, tile_grid<64, 64>(p), 256, p);
-    if (kind == kNarrow) return launch(st, k_loss_top_narrow<T>, sizeof(T) == 4 ? tile_grid<128, 64>(p) : tile_grid<256, 64>(p), 256, p);
+    if (kind == kNarrow) return launch(st, k_loss_top_narrow<T>, sizeof(T) == 4 ? tile_grid<64, 64>(p) : tile_grid<256, 64>(p), 256, p);
     if (kind == kRow) {
         const dim3 grid = grid_of(((uint64_t)p.N + 127) / 128);
         const uint32_t row = p.K * sizeof(T);
@@ -814,7 +823,7 @@ template <class T> int launch_dz(hipStream_t st, Kind kind, const DzArgs<T> &p)
 {
     if (kind == kFew) return launch(st, k_loss_dz_few<T>, grid_of((uint64_t)((p.M + 31) / 32) * ((p.N + 31) / 32)), 256, p);
     if (kind == kAnyhow) return launch(st, k_loss_dz_anyhow<T>, tile_grid<64, 64>(p), 256, p);
-    if (kind == kNarrow) return launch(st, k_loss_dz_narrow<T>, sizeof(T) == 4 ? tile_grid<128, 64>(p) : tile_grid<256, 64>(p), 256, p);
+    if (kind == kNarrow) return launch(st, k_loss_dz_narrow<T>, sizeof(T) == 4 ? tile_grid<64, 64>(p) : tile_grid<256, 64>(p), 256, p);
     if constexpr (sizeof(T) == 4) {
         return launch(st, k_loss_dz_chunks<T>, tile_grid<128, 128>(p), 256, p);
     } else {
@@ -1010,7 +1019,13 @@ int zg_linear_cross_entropy_backward(const zg_linear_cross_entropy_grad_args *a,
                         p.splits = 1;
                         p.e.power = power, p.e.type = a->dtype;
                         p.e.Y = a->d_dA, p.e.ld_Y = a->ld_dA;
-                        ZG_TRY(dense_product(st, a->dtype, p));
+                        // (bf16 2304 x 256 of 16 terms: 8.6 us in tiles of 256 x 128, 5.6 in tiles of 64 x 64)
+                        if (tile_blocks<256, 128>(p) < 128 && p.K <= 256) {
+                            p.K = n, p.b_short = 0;
+                            ZG_TRY(launch(st, k_loss_part_anyhow<T>, tile_grid<64, 64>(p), 256, p));
+                        } else {
+                            ZG_TRY(dense_product(st, a->dtype, p));
+                        }
                     } else {
                         Epilogue sum{};
                         sum.factor = 1.0f, sum.type = ZG_F32, sum.Y = part_A, sum.ld_Y = a->in;
