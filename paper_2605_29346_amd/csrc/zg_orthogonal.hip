@@ -297,6 +297,195 @@ template <class T> __global__ __launch_bounds__(256) void k_start_planes(StartAr
     }
 }
 
+// ---- small matrices, whole ----------------------------------------------------------------------------------------------------------
+// Up to 64 x 384 (or turned): one workgroup of eight wavefronts has X, A and B in LDS, planes and all, from the norm to the result: one launch for 2 + 3 steps, each of which would last little more than
+// a launch does.  Sums as in the other kernels (the low products apart).  Five steps of 16 x 16 take 21 us, of 64 x 64 27, 64 x 128 33, 47 x 256 46, 64 x 384 65, against 75 in launches; bound by one compute unit's way
+// from LDS to the matrix instructions and back.
+
+constexpr uint32_t kWholeSmall = 64, kWholeLarge = 384;
+
+struct WholeArgs {
+    StartArgs s; // P, Q and sums are not needed
+    uint64_t inv; // ceil(2^32 / cols): e / cols == (e * inv) >> 32 for the elements of a small matrix
+    bool tall;
+    int32_t steps;
+    float scalars[ZG_MAX_NEWTON_STEPS][5]; // A's, B's and X's alpha, B's and X's beta
+    void *O;
+    int64_t ld_O;
+    int32_t type_O;
+    bool update;
+    float keep;
+};
+
+constexpr uint32_t kWholeX = kWholeLarge + 8, kWholeA = kWholeSmall + 8; // elements to a row in LDS: rows start in other banks
+
+struct Pair {
+    f16 *high, *low; // in LDS
+    __device__ __forceinline__ void put(uint32_t at, float v) const
+    {
+        high[at] = (f16)v;
+        low[at] = (f16)(v - (float)high[at]);
+    }
+    __device__ __forceinline__ float get(uint32_t at) const { return (float)high[at] + (float)low[at]; }
+};
+
+// a lane's eight k of its row, from a plane whose rows lie along k, or across it
+__device__ __forceinline__ u32x4 along_k(const f16 *plane, uint32_t ld, uint32_t row, uint32_t k) { return *reinterpret_cast<const u32x4 *>(plane + row * ld + k); }
+__device__ __forceinline__ u32x4 across_k(const f16 *plane, uint32_t ld, uint32_t row, uint32_t k)
+{
+    const uint32_t lane = threadIdx.x & 15, r = (row & ~15u) + 4 * (lane & 3);
+    u32x4 v;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint64_t two = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(plane + (k + 4 * h + (lane >> 2)) * ld + r)));
+        v[2 * h] = (uint32_t)two, v[2 * h + 1] = (uint32_t)(two >> 32);
+    }
+    return v;
+}
+
+// 32 x 32 cells, k from `first` on, every `stride`th 16 of them: a's rows are the lane's, b's lie side by side
+template <bool ACROSS> __device__ __forceinline__ f32x16 whole_product(const Pair &a, uint32_t ld_a, uint32_t row_a, const Pair &b, uint32_t ld_b, uint32_t row_b, uint32_t first, uint32_t end, uint32_t stride)
+{
+    f32x16 acc = {}, low = {};
+    const uint32_t half = (threadIdx.x & 63) >> 5;
+#pragma unroll 1
+    for (uint32_t k0 = first; k0 < end; k0 += stride) {
+        const uint32_t k = k0 + 8 * half;
+        const u32x4 x = along_k(a.high, ld_a, row_a, k), lx = along_k(a.low, ld_a, row_a, k);
+        const u32x4 y = ACROSS ? across_k(b.high, ld_b, row_b, k) : along_k(b.high, ld_b, row_b, k), ly = ACROSS ? across_k(b.low, ld_b, row_b, k) : along_k(b.low, ld_b, row_b, k);
+        multiply((f16)0, y, lx, low);
+        multiply((f16)0, ly, x, low);
+        multiply((f16)0, y, x, acc);
+    }
+    return acc + low;
+}
+
+template <class T> __global__ __launch_bounds__(512) void k_step_whole(WholeArgs w)
+{
+    __shared__ f16 lds_x[2][kWholeSmall * kWholeX];
+    __shared__ f16 lds_a[2][kWholeSmall * kWholeA];
+    __shared__ __attribute__((aligned(16))) f16 lds_b[2][kWholeSmall * kWholeA];
+    __shared__ double sums[8];
+    static_assert(sizeof lds_b >= 4 * 16 * 64 * sizeof(float), "");
+    const Pair X{lds_x[0], lds_x[1]}, A{lds_a[0], lds_a[1]}, B{lds_b[0], lds_b[1]};
+    float *const half_sums = reinterpret_cast<float *>(lds_b); // (B is not there yet)
+    const StartArgs &s = w.s;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint32_t half = lane >> 5, row = lane & 31;
+    const uint32_t small = w.tall ? s.cols : s.rows, large = w.tall ? s.rows : s.cols;
+    const uint32_t high = (small + 31) / 32, wide = (large + 31) / 32; // tiles of 32
+
+    // the momentum, the norm, and X; zeros around it.  A lane has every 512th element, all of them on their way at once.
+    constexpr int most = kWholeSmall * kWholeLarge / 512;
+    const uint32_t cells = s.rows * s.cols;
+    const auto row_of = [&](uint32_t e) { return (uint32_t)((e * w.inv) >> 32); };
+    float v[most], g[most];
+#pragma unroll
+    for (int i = 0; i < most; ++i) {
+        const uint32_t e = threadIdx.x + 512 * i, r = row_of(e), c = e - r * s.cols;
+        v[i] = g[i] = 0.0f;
+        if (e >= cells) continue;
+        g[i] = (float)static_cast<const T *>(s.g)[r * s.ld_g + c];
+        if (s.m) v[i] = s.m[r * s.ld_m + c];
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < most; ++i) {
+        const uint32_t e = threadIdx.x + 512 * i, r = row_of(e), c = e - r * s.cols;
+        if (s.m) {
+            v[i] = s.momentum * v[i] + g[i];
+            if (e < cells) s.m[r * s.ld_m + c] = v[i];
+            if (s.nesterov) v[i] = s.momentum * v[i] + g[i];
+        } else {
+            v[i] = g[i];
+        }
+        sum += (double)v[i] * (double)v[i];
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    if (lane == 0) sums[wave] = sum;
+    for (uint32_t i = threadIdx.x; i < kWholeSmall * kWholeX / 8; i += 512) {
+        reinterpret_cast<u32x4 *>(X.high)[i] = u32x4{};
+        reinterpret_cast<u32x4 *>(X.low)[i] = u32x4{};
+    }
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += sums[i];
+    const double factor = (double)s.power / (sqrt(sum) + s.eps);
+#pragma unroll
+    for (int i = 0; i < most; ++i) {
+        const uint32_t e = threadIdx.x + 512 * i, r = row_of(e), c = e - r * s.cols;
+        if (e < cells) X.put(w.tall ? c * kWholeX + r : r * kWholeX + c, (float)((double)v[i] * factor));
+    }
+    __syncthreads();
+
+    for (int step = 0; step < w.steps; ++step) {
+        const float *const k = w.scalars[step];
+        asm volatile("" : "+v"(half), "+v"(row)); // (or the addresses of all cells would be made, and kept, ahead of the first step)
+        const uint32_t ti = (wave >> 1 & 1) * 32, tj = (wave & 1) * 32; // a wavefront's tile of A and B; two share A's sums
+        const bool mine = ti < 32 * high && tj < 32 * high;
+        f32x16 acc = {};
+        if (mine) acc = whole_product<false>(X, kWholeX, ti + row, X, kWholeX, tj + row, (wave >> 2) * 16, 32 * wide, 32);
+        if (wave >= 4) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) half_sums[((wave - 4) * 16 + r) * 64 + lane] = acc[r];
+        }
+        __syncthreads();
+        if (wave < 4 && mine) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) A.put((ti + row) * kWholeA + tj + 8 * (r / 4) + 4 * half + r % 4, k[0] * (acc[r] + half_sums[(wave * 16 + r) * 64 + lane]));
+        }
+        __syncthreads();
+        if (wave < 4 && mine) {
+            acc = whole_product<false>(A, kWholeA, ti + row, A, kWholeA, tj + row, 0, 32 * high, 16);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const uint32_t at = (ti + row) * kWholeA + tj + 8 * (r / 4) + 4 * half + r % 4;
+                B.put(at, fmaf(k[3], A.get(at), k[1] * acc[r]));
+            }
+        }
+        __syncthreads();
+        const bool last = step + 1 == w.steps;
+        float next[3][16];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            const uint32_t t = wave + 8 * i, m0 = t % high * 32, n0 = t / high * 32;
+            if (n0 >= 32 * wide) continue;
+            acc = whole_product<true>(B, kWholeA, m0 + row, X, kWholeX, n0 + row, 0, 32 * high, 16);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) next[i][r] = fmaf(k[4], X.get((m0 + row) * kWholeX + n0 + 8 * (r / 4) + 4 * half + r % 4), k[2] * acc[r]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            const uint32_t t = wave + 8 * i, m = t % high * 32 + row, n0 = t / high * 32;
+            if (n0 >= 32 * wide) continue;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const uint32_t n = n0 + 8 * (r / 4) + 4 * half + r % 4;
+                if (!last) {
+                    X.put(m * kWholeX + n, next[i][r]);
+                } else if (m < small && n < large) {
+                    const int64_t at = w.tall ? n * w.ld_O + m : m * w.ld_O + n;
+                    if (w.type_O == ZG_F32) {
+                        float *const o = static_cast<float *>(w.O) + at;
+                        *o = w.update ? fmaf(w.keep, *o, next[i][r]) : next[i][r];
+                    } else if (w.type_O == ZG_F16) {
+                        f16 *const o = static_cast<f16 *>(w.O) + at;
+                        *o = (f16)(w.update ? fmaf(w.keep, (float)*o, next[i][r]) : next[i][r]);
+                    } else {
+                        __bf16 *const o = static_cast<__bf16 *>(w.O) + at;
+                        *o = (__bf16)(w.update ? fmaf(w.keep, (float)*o, next[i][r]) : next[i][r]);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
 // ---- host side --------------------------------------------------------------------------------------------------------------------
 
 // Singular values of at most `top`: what a step makes of them at most, and B's.  Where the derivative is 0 or at the end.
@@ -389,7 +578,7 @@ Way way_of(uint32_t M, uint32_t N, uint32_t K, bool symmetric, bool pairs)
 }
 
 struct StepPlan {
-    bool tall, pairs;
+    bool tall, pairs, whole;
     uint32_t small, large; // the sides: X is [small, large]
     Way way_gram, way_square, way_step;
     bool turned; // X is held turned beside itself
@@ -411,6 +600,11 @@ StepPlan step_plan(const Common &c)
     t.tall = c.rows > c.cols;
     t.small = (uint32_t)std::min(c.rows, c.cols), t.large = (uint32_t)std::max(c.rows, c.cols);
     t.pairs = c.type != ZG_BF16 || t.small < 256 || c.steps > 6;
+    t.whole = t.small <= kWholeSmall && t.large <= kWholeLarge;
+    if (t.whole) {
+        t.total = 256; // (a workspace of nothing would be refused by who asks for one)
+        return t;
+    }
     t.way_gram = way_of(t.small, t.small, t.large, true, t.pairs);
     t.way_square = way_of(t.small, t.small, t.small, true, t.pairs);
     t.way_step = way_of(t.small, t.large, t.small, false, t.pairs);
@@ -510,12 +704,39 @@ template <int SEGMENTS> int run_steps(hipStream_t st, const Common &c, const Ste
     return ZG_OK;
 }
 
+int run_whole(hipStream_t st, const Common &c, const StepPlan &t, const StartArgs &a, const Result &out)
+{
+    WholeArgs w{};
+    w.s = a;
+    w.inv = ((uint64_t(1) << 32) + c.cols - 1) / c.cols;
+    w.tall = t.tall, w.steps = c.steps;
+    double top = 1.0;
+    int ex = exponent_for(top);
+    for (int s = 0; s < c.steps; ++s) {
+        const float *const k = c.coefficients + 3 * s;
+        const Bounds next = bounds_of(top, k);
+        const bool last = s + 1 == c.steps;
+        const double factor = last ? (double)out.factor : 1.0;
+        const int ea = exponent_for(top * top), eb = exponent_for(next.b), en = last ? 0 : exponent_for(next.x);
+        w.scalars[s][0] = std::ldexp(1.0f, ea - 2 * ex);
+        w.scalars[s][1] = std::ldexp(k[2], eb - 2 * ea), w.scalars[s][3] = std::ldexp(k[1], eb - ea);
+        w.scalars[s][2] = (float)std::ldexp(factor, en - eb - ex), w.scalars[s][4] = (float)std::ldexp(factor * k[0], en - ex);
+        top = next.x, ex = en;
+    }
+    w.O = out.O, w.ld_O = out.ld, w.type_O = c.type, w.update = out.update, w.keep = out.keep;
+    if (c.dtype == ZG_F32) return launch(st, k_step_whole<float>, dim3(1), 512, w);
+    if (c.dtype == ZG_F16) return launch(st, k_step_whole<f16>, dim3(1), 512, w);
+    return launch(st, k_step_whole<__bf16>, dim3(1), 512, w);
+}
+
 int run(hipStream_t st, const Common &c, StartArgs a, char *ws, const Result &out)
 {
     const StepPlan t = step_plan(c);
     a.rows = (uint32_t)c.rows, a.cols = (uint32_t)c.cols;
-    a.eps = c.eps, a.sums = reinterpret_cast<double *>(ws + t.off_sums), a.n_sums = t.n_sums;
+    a.eps = c.eps;
     a.power = std::ldexp(1.0f, exponent_for(1.0));
+    if (t.whole) return run_whole(st, c, t, a, out);
+    a.sums = reinterpret_cast<double *>(ws + t.off_sums), a.n_sums = t.n_sums;
     f16 *const X = reinterpret_cast<f16 *>(ws + t.off_X[0]), *const T = t.turned ? reinterpret_cast<f16 *>(ws + t.off_T[0]) : nullptr;
     f16 *const X_low = X + t.plane_X, *const T_low = t.turned && t.pairs ? T + t.plane_T : nullptr;
     a.P = t.tall ? T : X, a.P_low = t.tall ? T_low : X_low, a.ld_P = t.tall ? t.ld_T : t.ld_X;

@@ -60,10 +60,11 @@ def test_every_kernel_is_reached(asked):
     assert sorted(every - reached) == []
 
 
-def test_the_loss_takes_two_launches_or_three_and_an_update_three_a_step(asked):
+def test_the_loss_takes_two_launches_or_three_and_an_update_one_or_three_a_step(asked):
     for what, launched in asked["launched"]:
         own = [n for n in launched if re.search(r"\d+k_(loss|step|start)_", n) and "k_loss_pack" not in n]
         if what[0] == "loss":
             assert len(own) in (2, 3), (what, own)
         elif what[0] == "orthogonalize":
-            assert len(own) == len(launched) == 17, (what, own)
+            small = min(what[2:]) <= 64 and max(what[2:]) <= 384
+            assert len(own) == len(launched) == (1 if small else 17), (what, own)
