@@ -734,8 +734,9 @@ template <class T, int FM, int FN, int CH> struct Part {
 // from LDS.  In front of the last part all wavefronts meet: from there on the step's buffer is free - it is asked to be filled with the step that
 // comes `stages` later - and the next step's is full.  The loads go out one by one between the products: together, right behind the meeting, those
 // of all wavefronts queue up and the products wait behind them; half of them behind the next step's first part.
-template <class T, class A, class B, int FM, int FN, int CH, int stages, class Fetch>
-__device__ __forceinline__ void multiply_steps(f32x16 (&acc)[FM][FN], const u32x4 *lds, int lb_at, uint32_t stage, uint32_t steps, uint32_t am, uint32_t bn,
+// The nth part goes into the (n % SETS)th of `acc`.
+template <class T, class A, class B, int FM, int FN, int CH, int stages, int SETS, class Fetch>
+__device__ __forceinline__ void multiply_steps(f32x16 (&acc)[SETS][FM][FN], const u32x4 *lds, int lb_at, uint32_t stage, uint32_t steps, uint32_t am, uint32_t bn,
                                                uint32_t &now, Fetch &fetch)
 {
     using P = Part<T, FM, FN, CH>;
@@ -760,7 +761,7 @@ __device__ __forceinline__ void multiply_steps(f32x16 (&acc)[FM][FN], const u32x
             P &cur = n % 2 ? two : one, &nxt = n % 2 ? one : two;
             read(nxt, n + 1);
             __builtin_amdgcn_sched_barrier(0);
-            cur.multiply_into(acc, [&](int m) {
+            cur.multiply_into(acc[n % SETS], [&](int m) {
                 if (n == 0) spread(m, half_of, loads);
             });
             __builtin_amdgcn_sched_barrier(0);
@@ -774,7 +775,7 @@ __device__ __forceinline__ void multiply_steps(f32x16 (&acc)[FM][FN], const u32x
         read(one, 0); // (behind the last step, too: nobody looks at it then)
         __builtin_amdgcn_sched_barrier(0);
         fetch.open();
-        two.multiply_into(acc, [&](int m) { spread(m, 0, half_of); });
+        two.multiply_into(acc[last % SETS], [&](int m) { spread(m, 0, half_of); });
     }
 }
 
@@ -866,13 +867,17 @@ template <class T, class O, int BM, int BN, bool A_TURNED, bool B_TURNED, int CH
     };
     if constexpr (Args::segments > 1) a.p += p.plane_a(0), b.p += p.plane_b(0);
     Fetch<A, B, BM * CH, depth, stage, stages, decltype(on)> fetch{a, b, lds, wave, p.K - p.b_short, w.k_first, w.k_end, on};
-    f32x16 acc[FM][FN] = {};
+    // (where registers are left, a pair's sums are made in four, of every fourth pair of chunks: a quarter of the roundings one behind the other)
+    constexpr int sets = Args::segments > 1 && FM * FN == 1 ? CH / 2 : 1;
+    f32x16 all[sets][FM][FN] = {}, (&acc)[FM][FN] = all[0];
     uint32_t now = 0;
     if (steps > 0) {
         fetch.begin();
-        multiply_steps<T, A, B, FM, FN, CH, stages>(acc, lds, BM * CH, stage, steps, am, bn, now, fetch);
+        multiply_steps<T, A, B, FM, FN, CH, stages>(all, lds, BM * CH, stage, steps, am, bn, now, fetch);
         wait_loads<0>();
     }
+#pragma unroll
+    for (int i = 1; i < sets; ++i) acc[0][0] += all[i][0][0];
     __syncthreads(); // the buffers are free
     if constexpr (GROUPS > 1) { // the groups' sums, in order
         float *const cells = reinterpret_cast<float *>(all_lds);
@@ -936,9 +941,9 @@ template <class T, class O, bool A_TURNED, bool B_TURNED, int WAVES = 8, class A
     Place w;
     uint32_t now = 0;
     while (tiles.take(w)) {
-        f32x16 acc[FM][FN] = {};
+        f32x16 all[1][FM][FN] = {}, (&acc)[FM][FN] = all[0];
         const uint32_t steps = (w.k_end - w.k_first + depth - 1) / depth * Args::segments;
-        if (steps > 0) multiply_steps<T, A, B, FM, FN, CH, stages>(acc, lds, BM * CH, stage, steps, am, bn, now, fetch);
+        if (steps > 0) multiply_steps<T, A, B, FM, FN, CH, stages>(all, lds, BM * CH, stage, steps, am, bn, now, fetch);
         Out<Args>::template narrow<O, B_TURNED>(p, acc, reinterpret_cast<f32x4 *>(lds) + stages * stage + wave * 256, w.m0 + wm, w.n0 + wn, tiles.M, w.split);
     }
     wait_loads<0>();
@@ -994,7 +999,7 @@ template <class T, class Args> __device__ __forceinline__ void few_tile(const Ar
         }
     } else { // pairs: the high planes at p, the low ones behind
         Along<T> la = a, lb = b;
-        f32x16 low = {};
+        f32x16 low = {}, other = {}; // (every other chunk's: half the roundings one behind the other)
         la.row = reinterpret_cast<const T *>(reinterpret_cast<const char *>(a.row) + p.plane_a(0));
         lb.row = reinterpret_cast<const T *>(reinterpret_cast<const char *>(b.row) + p.plane_b(1));
         for (uint32_t k0 = wave * 2 * K; k0 < p.K; k0 += ahead * 8 * K) {
@@ -1009,9 +1014,10 @@ template <class T, class Args> __device__ __forceinline__ void few_tile(const Ar
             for (int i = 0; i < ahead; ++i) {
                 multiply(T(), y[i], lx[i], low);
                 multiply(T(), ly[i], x[i], low);
-                multiply(T(), y[i], x[i], acc);
+                multiply(T(), y[i], x[i], i % 2 ? other : acc);
             }
         }
+        acc += other;
         acc += low;
     }
 #pragma unroll
