@@ -902,15 +902,15 @@ template <class T, class O, int BM, int BN, bool A_TURNED, bool B_TURNED, int CH
 // Eight wavefronts, 256 x 256 cells, one workgroup to a compute unit, which takes one tile after the other; two buffers of eight chunks (128 bytes) of k.  For 16-bit types.  The next tile's
 // first steps are on their way while this one's cells are handed over, through LDS of their own.  Bound by what is between the matrix
 // instructions (counters: they run for 0.38 to 0.43 of the time over 1024 terms): bf16 65536 x 1024 x 1024 162 us, 850 TFLOP/s, 4096 x 16384 x 4096 433 us, 1270.
-template <class T, class O, bool A_TURNED, bool B_TURNED, int WAVES = 8, class Args> __device__ __forceinline__ void long_tiles(const Args &p)
+template <class T, class O, bool A_TURNED, bool B_TURNED, class Args> __device__ __forceinline__ void long_tiles(const Args &p)
 {
-    constexpr int BM = 256, BN = 256, FM = 4, FN = WAVES == 8 ? 2 : 4, CH = 8, stages = 2, stage = (BM + BN) * CH;
-    using A = Feed<T, BM, WAVES, CH, A_TURNED>;
-    using B = Feed<T, BN, WAVES, CH, B_TURNED>;
+    constexpr int BM = 256, BN = 256, FM = 4, FN = 2, CH = 8, stages = 2, stage = (BM + BN) * CH;
+    using A = Feed<T, BM, 8, CH, A_TURNED>;
+    using B = Feed<T, BN, 8, CH, B_TURNED>;
     constexpr int depth = CH * A::K;
     __shared__ u32x4 lds[stages * stage + 8 * 256];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t wm = (wave >> (WAVES == 8 ? 2 : 1)) * 128, wn = (wave & (WAVES == 8 ? 3 : 1)) * 32 * FN, am = wm + (lane & 31), bn = wn + (lane & 31);
+    const uint32_t wm = (wave >> 2) * 128, wn = (wave & 3) * 64, am = wm + (lane & 31), bn = wn + (lane & 31);
     Tiles<BM, BN, Args::symmetric, Args::high> tiles(p, depth), ahead = tiles;
     A a{}; // (a workgroup without a tile asks for zeros)
     B b{};
