@@ -538,7 +538,7 @@ template <class T> struct Out<DzArgs<T>> {
             for (int k = 0; k < 8; ++k)
 #pragma unroll
                 for (int d = 4; d < 64; d <<= 1) v[k] += __shfl_xor(v[k], d);
-            if ((threadIdx.x & 63) < 4 && c.left > 0) store8(p.bias_part + m / 16 * p.ld_part + c.n, 8, v);
+            if ((threadIdx.x & 63) < 4 && m < live && c.left > 0) store8(p.bias_part + m / 16 * p.ld_part + c.n, 8, v); // (m: the wavefront's first row, of the tile's second half there may be none)
         }
     };
 };
