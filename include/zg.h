@@ -514,7 +514,7 @@ int zg_rms_norm_backward(const zg_norm_grad_args *a, void *d_workspace, size_t w
 
 /* Softmax cross entropy of the logits Z = A W^T + bias, which are not kept:
  *   lse[i] = log sum over c of exp(Z[i,c]),   row_loss[i] = lse[i] - Z[i, label[i]],   total = sum of weight[i],   loss = (sum of weight[i] row_loss[i]) / total,
- * the sums over the rows that count: those with a label in 0..out-1 (any other value: the row has none, its row_loss is 0) and a weight that is not 0.  loss = 0 where no row counts.
+ * the sums over the rows that count: those with a label in 0..out-1 (any other value: the row has none, its row_loss is 0) and a weight that is not 0.  loss = 0 where no row counts (or total is 0).
  * A: [rows, in], W: [out, in] of type dtype; bias: [out] or NULL (-infinity takes a class out); labels: [rows] of type label_dtype (ZG_I32 or ZG_I64); weight: [rows] or
  * NULL (ones).  out <= ZG_MAX_CLASSES.  Logits and all that is made of them are fp32 whatever dtype is, the sums over the rows 64 bits.  A row whose logits hold a NaN or +infinity, or
  * nothing but -infinity, has the NaN or infinity that the formula gives, and so has the loss if the row counts.  lse (what the gradients need of this pass) is written for every live row. */
@@ -566,6 +566,7 @@ typedef struct {
     int64_t ld_dW;
     float *d_dbias;
 } zg_linear_cross_entropy_grad_args;
+/* Workspace bytes of the call with this very struct: up to 2^29 bytes of dZ (4096 classes of it, where that is more), parts of the sums, and copies as above.  Host only. */
 int zg_linear_cross_entropy_backward_workspace(const zg_linear_cross_entropy_grad_args *a, size_t *bytes);
 int zg_linear_cross_entropy_backward(const zg_linear_cross_entropy_grad_args *a, void *d_workspace, size_t workspace_bytes, void *stream);
 
@@ -588,6 +589,7 @@ typedef struct {
     void *d_O;
     int64_t ld_O;
 } zg_orthogonalize_args;
+/* Workspace bytes of the call (of these sizes and types).  Host only. */
 int zg_orthogonalize_workspace(const zg_orthogonalize_args *a, size_t *bytes);
 int zg_orthogonalize(const zg_orthogonalize_args *a, void *d_workspace, size_t workspace_bytes, void *stream);
 

@@ -585,12 +585,12 @@ template <int C> __global__ __launch_bounds__(1024) void k_loss_bias(Rows rows, 
 
 // ---- operands that lie anyhow -----------------------------------------------------------------------------------------------------
 
-// A copy whose rows are whole chunks: [rows, cols] to [rows, ld_to], zeros behind the columns.
-template <class T> __global__ __launch_bounds__(256) void k_loss_pack(const T *from, int64_t ld_from, uint32_t rows, uint32_t cols, T *to, uint32_t groups)
+// A copy whose rows are whole chunks, zeros behind the columns; `groups` of eight columns to a row.
+template <class T> __global__ __launch_bounds__(256) void k_loss_pack(const T *from, int64_t ld_from, Rows rows, uint32_t cols, T *to, uint32_t groups)
 {
     const uint64_t i = (uint64_t)block_number() * 256 + threadIdx.x, r = i / groups;
     const uint32_t g = (uint32_t)(i - r * groups);
-    if (r >= rows) return;
+    if (r >= rows.live()) return;
     float v[8];
     load8(from + r * ld_from + 8 * g, (int)cols - 8 * (int)g, v);
     store8(to + (r * groups + g) * 8, 8, v);
@@ -661,12 +661,12 @@ template <class F> int with_wide_type(int32_t type, F &&f)
     return f((__bf16)0);
 }
 
-int launch_pack(hipStream_t st, int32_t dtype, const void *from, int64_t ld, int64_t rows, int32_t cols, void *to)
+int launch_pack(hipStream_t st, int32_t dtype, const void *from, int64_t ld, Rows rows, int32_t cols, void *to)
 {
     const uint32_t groups = ((uint32_t)cols + 7) / 8;
     return with_wide_type(dtype, [&](auto t) {
         using T = decltype(t);
-        return launch(st, k_loss_pack<T>, grid_of(((uint64_t)rows * groups + 255) / 256), 256, static_cast<const T *>(from), ld, (uint32_t)rows, (uint32_t)cols, static_cast<T *>(to), groups);
+        return launch(st, k_loss_pack<T>, grid_of(((uint64_t)rows.cap * groups + 255) / 256), 256, static_cast<const T *>(from), ld, rows, (uint32_t)cols, static_cast<T *>(to), groups);
     });
 }
 
@@ -794,11 +794,11 @@ template <class A> Shape shape_of(const A *a) { return {a->rows, a->in, a->out, 
 template <class A> int launch_packs(hipStream_t st, const A *a, char *ws, const size_t (&off)[2], Packed &pk)
 {
     if (pk.copy_A) {
-        ZG_TRY(launch_pack(st, a->dtype, a->d_A, a->ld_A, a->rows, a->in, ws + off[0]));
+        ZG_TRY(launch_pack(st, a->dtype, a->d_A, a->ld_A, Rows{a->d_rows, (uint32_t)a->rows}, a->in, ws + off[0]));
         pk.a.p = ws + off[0];
     }
     if (pk.copy_W) {
-        ZG_TRY(launch_pack(st, a->dtype, a->d_W, a->ld_W, a->out, a->in, ws + off[1]));
+        ZG_TRY(launch_pack(st, a->dtype, a->d_W, a->ld_W, Rows{nullptr, (uint32_t)a->out}, a->in, ws + off[1]));
         pk.w.p = ws + off[1];
     }
     return ZG_OK;

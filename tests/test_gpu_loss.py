@@ -347,3 +347,21 @@ def test_no_rows():
     assert float(r.loss) == 0 and float(r.total) == 0 and r.lse.numel() == 0
     da, dw, db = layers.linear_cross_entropy_backward(torch.empty(0, 16, device="cuda"), w, torch.empty(0, dtype=torch.int64, device="cuda"), r.lse, total=r.total)
     assert da.shape == (0, 16) and not dw.any() and not db.any()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_rows_beyond_the_count_of_operands_that_lie_anyhow(kind):
+    """At a size where such operands are copied first: what lies behind the count, in A and in the workspace, is nobody's operand."""
+    rows, k, n, live = 3001, 301, 1303, 2777
+    g = _gen("anyhow", str(kind))
+    a, w, labels, bias, weight = _inputs(g, rows, k, n, kind, 3)
+    a[live:] = float("nan")
+    weight[live:] = float("nan")
+    dev = torch.tensor([live], dtype=torch.int32, device="cuda")
+    full = torch.full((1 << 24,), float("nan"), device="cuda")  # (torch's next allocations of this size are likely to have these values)
+    del full
+    r = layers.linear_cross_entropy(a, w, labels, bias=bias, weight=weight, rows=dev, row_loss=True)
+    _check_loss(r, L.loss(a, w, labels, bias, weight, live), live)
+    got = layers.linear_cross_entropy_backward(a, w, labels, r.lse, bias=bias, weight=weight, total=r.total, rows=dev)
+    for x, (y, bound), what in zip((got[0][:live], got[1], got[2]), L.gradients(a, w, labels, kind, bias, weight, live), ("da", "dw", "dbias")):
+        R.check(x, y, bound, what)
