@@ -435,7 +435,10 @@ template <class T> struct DzArgs : ProductArgs {
     int64_t ld_part;
 };
 
-// Eight cells of a row; what is beyond the last class is 0.  Mostly a cell takes the bias, a multiplication and addition in one, an exponential and the factor; what else there may be, in any row of the
+// A probability.  Logits of millions are off by ones, and here they may be added up in another order than for lse: exp(Z - lse) could be any number, and an fp16 dZ infinite.  Not-a-number stays that.
+__device__ __forceinline__ float at_most_one(float p) { return __builtin_elementwise_minimum(p, 1.0f); }
+
+// Eight cells of a row; what is beyond the last class is 0.  Mostly a cell takes the bias, a multiplication and addition in one, an exponential, a minimum and the factor; what else there may be, in any row of the
 // wavefront, is looked after in a branch of its own.
 __device__ __forceinline__ void dz8(const Columns &c, const RowFactor &f, uint32_t first, bool bias, float (&v)[8])
 {
@@ -447,19 +450,19 @@ __device__ __forceinline__ void dz8(const Columns &c, const RowFactor &f, uint32
     if (__any(at < 8 || f.factor == 0.0f || c.left < 8 || !(fabsf(f.lse) < kPlainTop))) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            v[j] = f.factor * power_of(v[j], f.lse);
+            v[j] = f.factor * at_most_one(power_of(v[j], f.lse));
             v[j] -= at == (uint32_t)j ? f.factor : 0.0f;
             v[j] = f.factor != 0.0f && j < c.left ? v[j] : 0.0f;
         }
     } else {
         const float base2 = f.lse * kLog2e; // (its rounding is that of a logit of lse's size)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = f.factor * __builtin_amdgcn_exp2f(fmaf(v[j], kLog2e, -base2));
+        for (int j = 0; j < 8; ++j) v[j] = f.factor * at_most_one(__builtin_amdgcn_exp2f(fmaf(v[j], kLog2e, -base2)));
     }
 }
 
 // The hand-over through LDS of 4 KB, as for other products' cells: 32 x 32 cells at a time, four lanes have 32 columns of a row.  bf16 16384 x 1024 x 16384 629 us, 870 TFLOP/s (the same product's statistics take 450): the way through LDS,
-// and 9 vector instructions a cell.
+// and 10 vector instructions a cell.
 template <class T, int FM, int FN> __device__ __forceinline__ void hand_over_dz(const DzArgs<T> &p, f32x16 (&acc)[FM][FN], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M)
 {
     const uint32_t lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31, g = lane & 3;

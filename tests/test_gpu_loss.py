@@ -365,3 +365,20 @@ def test_rows_beyond_the_count_of_operands_that_lie_anyhow(kind):
     got = layers.linear_cross_entropy_backward(a, w, labels, r.lse, bias=bias, weight=weight, total=r.total, rows=dev)
     for x, (y, bound), what in zip((got[0][:live], got[1], got[2]), L.gradients(a, w, labels, kind, bias, weight, live), ("da", "dw", "dbias")):
         R.check(x, y, bound, what)
+
+
+@pytest.mark.parametrize("rows", [1, 3, 200])
+@pytest.mark.parametrize("kind", KINDS)
+def test_probabilities_stay_probabilities(rows, kind):
+    """Logits of millions, off by ones: the loss and its gradients need not add them up in one order, and exp(Z - lse) could be any power of e.  It is held to one: no gradient is infinite, none of a
+    bias larger than the rows' number.  lse itself may be given, too, with the rounding of another kernel."""
+    g = _gen("probabilities", rows)
+    a, w = (torch.randn(m, 1024, device="cuda", generator=g).mul(300).to(kind) for m in (rows, 900))
+    labels = torch.randint(0, 900, (rows,), device="cuda", generator=g)
+    lse = layers.linear_cross_entropy(a, w, labels).lse
+    for off in (0.0, 5.0):
+        da, dw, db = layers.linear_cross_entropy_backward(a, w, labels, lse - off)
+        assert bool(torch.isfinite(da).all()) and bool(torch.isfinite(dw).all())
+        assert float(db.abs().max()) <= rows
+    small = layers.linear_cross_entropy(a * 2.0**-10, w, labels).lse  # (of thousands)
+    assert float(layers.linear_cross_entropy_backward(a * 2.0**-10, w, labels, small - 5.0)[2].abs().max()) <= rows
