@@ -461,7 +461,7 @@ __device__ __forceinline__ void dz8(const Columns &c, const RowFactor &f, uint32
     }
 }
 
-// The hand-over through LDS of 4 KB, as for other products' cells: 32 x 32 cells at a time, four lanes have 32 columns of a row.  bf16 16384 x 1024 x 16384 629 us, 870 TFLOP/s (the same product's statistics take 450): the way through LDS,
+// The hand-over through LDS of 4 KB, as for other products' cells: 32 x 32 cells at a time, four lanes have 32 columns of a row.  bf16 16384 x 1024 x 16384 634 us, 867 TFLOP/s (the same product's statistics take 450): the way through LDS,
 // and 10 vector instructions a cell.
 template <class T, int FM, int FN> __device__ __forceinline__ void hand_over_dz(const DzArgs<T> &p, f32x16 (&acc)[FM][FN], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M)
 {
@@ -622,6 +622,9 @@ constexpr uint32_t group_rows(Kind k, bool f32) { return k == kFew ? 16 : k == k
 
 // Of dZ.  More has it go through memory twice, less makes dA of more parts: 16384 x 1024 x 65536 bf16, all gradients, with 2^27 .. 2^31 bytes 7.5, 7.2, 6.9, 7.0, 7.0 ms.
 constexpr int64_t kPieceBytes = int64_t(1) << 29;
+// Classes to a part of dA's sum, at least: few rows and columns are few tiles, and a part's steps come one behind the other.  The parts' kernel with 1024 / 256 / 128 / 64: f32 1 x 638 x 9054 97 / 32 / 23 / 18 us,
+// 771 x 34 x 2012 132 / 23 / 15 / 13, 300 x 256 x 5000 88 / 24 / 18 / 20, bf16 2000 x 64 x 10000 35 / 19 / 19 / 19, 300 x 256 x 5000 39 / 14 / 12 / 16; the join takes 1 to 4 us more with 64 parts than with 8.
+constexpr int64_t kPartTerms = 128;
 constexpr double kPackFlops = 2e9;                // products from here on are worth a copy of operands that lie anyhow
 
 struct Shape {
@@ -749,7 +752,7 @@ DzPlan dz_plan(const Shape &s, bool dA, bool dW, bool dbias, bool weight)
     // Parts enough for two tiles of 256 x 128 to a compute unit; where tiles of 256 x 256, which would be taken from 256 of them on, were a third empty, fewer than that.
     const int64_t wide_A = (rows + 255) / 256 * ((s.in + 255) / 256), wide_W = (t.piece + 255) / 256 * ((s.in + 255) / 256);
     const bool narrow = s.dtype != ZG_F32 && (s.in + 255) / 256 * 256 * 3 >= (s.in + 127) / 128 * 128 * 4;
-    t.splits_A = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(narrow ? std::min(512 / tiles_A, 255 / wide_A) : 512 / tiles_A, t.piece / 1024));
+    t.splits_A = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(narrow ? std::min(512 / tiles_A, 255 / wide_A) : 512 / tiles_A, t.piece / kPartTerms));
     t.splits_W = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(narrow ? std::min(512 / tiles_W, 255 / wide_W) : 512 / tiles_W, (rows + 255) / 256));
     const int64_t parts = t.pieces * t.splits_A;
     t.slots_A = (uint32_t)(parts == 1 ? 0 : std::min<int64_t>(parts, t.splits_A + 4));
