@@ -516,8 +516,8 @@ int zg_rms_norm_backward(const zg_norm_grad_args *a, void *d_workspace, size_t w
  *   lse[i] = log sum over c of exp(Z[i,c]),   row_loss[i] = lse[i] - Z[i, label[i]],   total = sum of weight[i],   loss = (sum of weight[i] row_loss[i]) / total,
  * the sums over the rows that count: those with a label in 0..out-1 (any other value: the row has none, its row_loss is 0) and a weight that is not 0.  loss = 0 where no row counts (or total is 0).
  * A: [rows, in], W: [out, in] of type dtype; bias: [out] or NULL (-infinity takes a class out); labels: [rows] of type label_dtype (ZG_I32 or ZG_I64); weight: [rows] or
- * NULL (ones).  out <= ZG_MAX_CLASSES.  Logits and all that is made of them are fp32 whatever dtype is, the sums over the rows 64 bits.  A row whose logits hold a NaN or +infinity, or
- * nothing but -infinity, has the NaN or infinity that the formula gives, and so has the loss if the row counts.  lse (what the gradients need of this pass) is written for every live row. */
+ * NULL (ones).  out <= ZG_MAX_CLASSES.  Logits and all that is made of them are fp32 whatever dtype is, the sums over the rows 64 bits.  A row whose logits hold a NaN has an lse of NaN, else one with a
+ * +infinity one of +infinity, and one of nothing but -infinity one of -infinity; row_loss is what the formula makes of that, and so is the loss if the row counts.  lse (what the gradients need of this pass) is written for every live row. */
 typedef struct {
     int64_t rows;
     const uint32_t *d_rows;

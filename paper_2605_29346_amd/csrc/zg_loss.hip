@@ -33,8 +33,8 @@ struct Top {
 
 __device__ __forceinline__ float power_of(float v, float top) { return __builtin_amdgcn_exp2f((v - top) * kLog2e); }
 
-// Where all logits are -infinity, they count from 0; not-a-number and +infinity end in a sum that is not a number.
-__device__ __forceinline__ float base_of(float top) { return top == -INFINITY ? 0.0f : top; }
+// What exponentials are made below: the top, or 0 where that is infinite.  The sum of a row with a +infinity is +infinity then, that of nothing but -infinity 0, and one with a not-a-number stays that.
+__device__ __forceinline__ float base_of(float top) { return fabsf(top) == INFINITY ? 0.0f : top; }
 
 // Up to here z log2 e is far inside fp32; beyond, exp(z - top) is made from the difference.
 constexpr float kPlainTop = 1e30f;
