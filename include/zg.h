@@ -544,7 +544,7 @@ int zg_linear_cross_entropy(const zg_linear_cross_entropy_args *a, void *d_works
  * g = *d_dloss (NULL: 1), total = *d_total (NULL: 1, the gradients of the sum; 0: all gradients are 0).  d_dA, d_dW and d_dbias may be NULL.  The logits are made again,
  * a piece of the classes at a time; dZ is held in dtype (rounded once, the products' operand), without g / total, which is applied behind the sums, and
  * where there are weights, or dtype is ZG_F16, beside a power of two that brings the largest |weight| to 2^14.  dbias is summed from dZ's fp32 values.  exp(Z - lse) is made from lse as fp32 holds it, off by
- * 2^-24 |lse| of itself, and at most 1.  A row that does not count is still an operand of dW (as a zero times what A holds there). */
+ * 2^-23 |lse| of itself, and at most 1.  A row that does not count is still an operand of dW (as a zero times what A holds there). */
 typedef struct {
     int64_t rows;
     const uint32_t *d_rows;

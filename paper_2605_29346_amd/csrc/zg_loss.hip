@@ -103,7 +103,7 @@ template <int FM, int FN> __device__ __forceinline__ void tops(const TopArgs &p,
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, v[j][r]);
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float base = base_of(top), base2 = base * kLog2e; // (base2's rounding is that of a logit of base's size)
+        const float base = base_of(top), base2 = base * kLog2e;
         float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < FN; ++j)
@@ -111,18 +111,21 @@ template <int FM, int FN> __device__ __forceinline__ void tops(const TopArgs &p,
             for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(fmaf(v[j][r], kLog2e, -base2));
         const bool far = fabsf(base) > kPlainTop;
         if (__any(at < 32 * FN || far)) { // what is rare
-            float z = 0.0f, far_sum = 0.0f;
+            float z = 0.0f, below = 0.0f;
 #pragma unroll
             for (int j = 0; j < FN; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     z = at == 32 * j + 8 * (r / 4) + 4 * half + r % 4 ? v[j][r] : z;
-                    far_sum += power_of(v[j][r], base);
+                    below += power_of(v[j][r], base);
                 }
             if (at < 32 * FN && (at >> 2 & 1) == half) p.at_label[m] = z;
-            sum = far ? far_sum : sum;
+            sum = far ? below : sum;
         }
         sum += __shfl_xor(sum, 32);
+        // base2's rounding, that of a logit of base's size, is a factor of all terms; and one of them is 1
+        if (!far) sum *= __builtin_amdgcn_exp2f(fmaf(-base, kLog2e, base2));
+        if (fabsf(top) < INFINITY) sum = __builtin_elementwise_maximum(sum, 1.0f);
         if (half == 0 && m < M) part[m] = Top{top, sum};
     }
 }
