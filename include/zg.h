@@ -576,7 +576,9 @@ int zg_linear_cross_entropy_backward(const zg_linear_cross_entropy_grad_args *a,
  * G: [rows, cols] of type dtype, O: of type out_dtype (may be G); rows, cols: 1..ZG_MAX_WIDTH.  coefficients is host memory, read before the call returns; coefficients under which the
  * largest singular value, 1 at first, may grow beyond 1024 in a step are refused.  The norm is summed in 64 bits.
  * Between the products X and what they are made of is held in 22 significant bits (two fp16 planes, relative to the largest value there can be), and the products are made of those, their sums being fp32.
- * A ZG_BF16 result of at least 256 rows and columns and at most 6 steps has its products' operands rounded to fp16 (X itself stays in 22 bits): 1.0e-3 .. 1.8e-3 of the result's length, its own rounding being 1.7e-3. */
+ * A ZG_BF16 result of at least 256 rows and columns may have its products' operands rounded to fp16 (X itself stays in 22 bits), where what that leaves, as estimated from the coefficients, is at most 4.0e-3 of the length of a
+ * matrix whose singular values are ones: so in five steps of the triple above (1.0e-3 .. 1.8e-3 for noise and for some strong directions, up to 3.2e-3 where all singular values are alike; the result's own rounding is
+ * 1.7e-3).  Six steps of it, and others that let errors grow as much, take all 22 bits. */
 #define ZG_MAX_NEWTON_STEPS 32
 typedef struct {
     int32_t rows, cols;

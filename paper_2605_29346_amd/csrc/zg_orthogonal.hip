@@ -1,8 +1,8 @@
 // A matrix whose singular values are brought near one by Newton-Schulz products, and the weights' update that uses it.
 //
 // X = G / (|G| + eps), turned where G is tall; a step is A = X X^T, B = b A + c A^2, X = a X + B X: singular values s become a s + b s^3 + c s^5.
-// Between the products X, A and B are held as fp16 planes (x = high + low: 22 bits) at a power of two; X always has both, as it is added to what the products make of it.  A bfloat16 result is made with the
-// high planes as operands (one rounding of 2^-12 of each); others with both planes of both operands, three products: low x high, high x low and high x high.  A and B are symmetric: only
+// Between the products X, A and B are held as fp16 planes (x = high + low: 22 bits) at a power of two; X always has both, as it is added to what the products make of it.  A bfloat16 result of large sides is made with the
+// high planes as operands (one rounding of 2^-12 of each) where the steps let that be (high_planes_do); others with both planes of both operands, three products: low x high, high x low and high x high.  A and B are symmetric: only
 // the tiles that reach down to the diagonal are made, and go out mirrored.  The sums of B X run across the rows of X: tiles of 256 x 256 turn them as they are read from LDS, smaller ones, which that would
 // hold up (1024 x 4096: 24 -> 30 us; pairs of 1024 x 2048 in tiles of 64 x 64: 27 -> 48), have X turned beside it.
 #include "zg_product.h"
@@ -577,6 +577,34 @@ Way way_of(uint32_t M, uint32_t N, uint32_t K, bool symmetric, bool pairs)
     return best;
 }
 
+// Whether the steps' products may be made of the high planes alone.  What their rounding leaves grows in the steps behind it: an error along a singular value s by the step's slope there, one that turns its direction by
+// p(s) / s, whichever is larger, and each step adds about s (3 (b s^2)^2 + 6 (c s^4)^2 + 2 (b s^2 + c s^4)^2)^(1/2) of its own; the square of that is carried from 128 values of s through all steps.  Values above 1/16 are fewer than
+// 256, over which errors of the operands spread out: what is left among the few falls with their number's root, s / 16.  The usual triple has 8, 21, 32 and 52 in 3 to 6 steps.  By this arithmetic in 64 bits, some 200 sets of triples
+// between 10 and 35, sides of 256 to 600, matrices of noise, of singular values all alike, and both, were off by no more than 1.04e-4 of this (3.5e-3 in all) times the length of as many ones; sets of 75 to 240, made to converge fast,
+// by up to 6e-3.  A step that makes small singular values smaller leaves results that an error of that size would hide.
+bool high_planes_do(const float *k, int32_t steps)
+{
+    constexpr int points = 128;
+    constexpr float limit = 35.0f, ratio = 0.93003f; // 10^(-4 / 127)
+    for (int s = 0; s < steps; ++s)
+        if (std::fabs(k[3 * s]) < 1.0f) return false;
+    float v[points], off[points] = {};
+    v[0] = 1.0f;
+    for (int i = 1; i < points; ++i) v[i] = v[i - 1] * ratio;
+    for (int s = 0; s < steps; ++s)
+        for (int i = 0; i < points; ++i) { // (side by side: 2 us in all)
+            const float a = k[3 * s], t = v[i] * v[i], bt = k[3 * s + 1] * t, ct = k[3 * s + 2] * t * t, slope = a + 3.0f * bt + 5.0f * ct, turn = a + bt + ct;
+            off[i] = std::max(slope * slope, turn * turn) * off[i] + t * (3.0f * bt * bt + 6.0f * ct * ct + 2.0f * (bt + ct) * (bt + ct));
+            v[i] *= turn;
+        }
+    float from = 1.0f;
+    for (int i = 0; i < points; ++i, from *= ratio) {
+        const float most = limit * std::max(1.0f, 16.0f * from);
+        if (!(off[i] <= most * most)) return false;
+    }
+    return true;
+}
+
 struct StepPlan {
     bool tall, pairs, whole;
     uint32_t small, large; // the sides: X is [small, large]
@@ -588,7 +616,7 @@ struct StepPlan {
     int64_t plane_X, plane_T, plane_A; // elements
 };
 
-StepPlan step_plan(const Common &c)
+StepPlan plan_of(const Common &c, bool pairs)
 {
     StepPlan t{};
     const auto take = [&](size_t bytes) {
@@ -599,7 +627,7 @@ StepPlan step_plan(const Common &c)
     const auto up = [](int64_t n) { return (n + 7) / 8 * 8; };
     t.tall = c.rows > c.cols;
     t.small = (uint32_t)std::min(c.rows, c.cols), t.large = (uint32_t)std::max(c.rows, c.cols);
-    t.pairs = c.type != ZG_BF16 || t.small < 256 || c.steps > 6;
+    t.pairs = pairs;
     t.whole = t.small <= kWholeSmall && t.large <= kWholeLarge;
     if (t.whole) {
         t.total = 256; // (a workspace of nothing would be refused by who asks for one)
@@ -620,6 +648,17 @@ StepPlan step_plan(const Common &c)
     t.off_A = take((size_t)t.plane_A * (t.pairs ? 2 : 1) * sizeof(f16));
     t.off_B = take((size_t)t.plane_A * (t.pairs ? 2 : 1) * sizeof(f16));
     return t;
+}
+
+bool may_be_single(const Common &c) { return c.type == ZG_BF16 && std::min(c.rows, c.cols) >= 256; }
+
+StepPlan step_plan(const Common &c) { return plan_of(c, !may_be_single(c) || c.steps > 6 || !high_planes_do(c.coefficients, c.steps)); }
+
+// goes by the matrix, not by the steps
+size_t workspace_of(const Common &c)
+{
+    const size_t pairs = plan_of(c, true).total;
+    return may_be_single(c) ? std::max(pairs, plan_of(c, false).total) : pairs;
 }
 
 template <int SEGMENTS, int KIND> int launch_step(hipStream_t st, Way way, const StepArgs<SEGMENTS, KIND> &p)
@@ -779,7 +818,7 @@ int zg_orthogonalize_workspace(const zg_orthogonalize_args *a, size_t *bytes)
         Common c;
         ZG_TRY(check_orthogonalize(a, c));
         if (!bytes) return fail(ZG_EINVAL, "null argument");
-        *bytes = step_plan(c).total;
+        *bytes = workspace_of(c);
         return ZG_OK;
     });
 }
@@ -792,7 +831,7 @@ int zg_orthogonalize(const zg_orthogonalize_args *a, void *d_workspace, size_t w
         ZG_TRY(check_matrix("d_G", a->d_G, a->ld_G, a->cols, a->dtype));
         ZG_TRY(check_matrix("d_O", a->d_O, a->ld_O, a->cols, a->out_dtype));
         ZG_TRY(check_apart(matrix_span("d_O", a->d_O, a->rows, a->ld_O, a->cols, a->out_dtype), {}, {matrix_span("d_G", a->d_G, a->rows, a->ld_G, a->cols, a->dtype)}));
-        ZG_TRY(check_workspace(d_workspace, workspace_bytes, step_plan(c).total));
+        ZG_TRY(check_workspace(d_workspace, workspace_bytes, workspace_of(c)));
         StartArgs s{};
         s.g = a->d_G, s.ld_g = a->ld_G;
         return run(static_cast<hipStream_t>(stream), c, s, static_cast<char *>(d_workspace), {a->d_O, a->ld_O, false, 0.0f, 1.0f});
@@ -805,7 +844,7 @@ int zg_muon_step_workspace(const zg_muon_args *a, size_t *bytes)
         Common c;
         ZG_TRY(check_muon(a, c));
         if (!bytes) return fail(ZG_EINVAL, "null argument");
-        *bytes = step_plan(c).total;
+        *bytes = workspace_of(c);
         return ZG_OK;
     });
 }
@@ -824,7 +863,7 @@ int zg_muon_step(const zg_muon_args *a, void *d_workspace, size_t workspace_byte
             ZG_TRY(check_apart(M, {G, W}));
             ZG_TRY(check_apart(W, {G}));
         }
-        ZG_TRY(check_workspace(d_workspace, workspace_bytes, step_plan(c).total));
+        ZG_TRY(check_workspace(d_workspace, workspace_bytes, workspace_of(c)));
         StartArgs s{};
         s.g = a->d_G, s.ld_g = a->ld_G, s.m = a->d_M, s.ld_m = a->ld_M, s.momentum = a->momentum, s.nesterov = a->nesterov != 0;
         const float keep = (float)(1.0 - (double)a->lr * (double)a->decay), factor = (float)(-(double)a->lr * (double)a->scale);

@@ -357,8 +357,8 @@ def _steps(coefficients, steps):
 
 def orthogonalize(g, *, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, out_dtype=None, out=None, stream=None):
     """g / (|g| + eps) after `steps` Newton-Schulz steps x <- a x + b (x x^T) x + c (x x^T)^2 x, which bring its singular values near one; `coefficients`: (a, b, c), or a triple
-    for each step.  Result of `out_dtype` (default: g's type); `out` may be g.  Products are made of 22 significant bits (fp16 operands for a bfloat16 result of 256 rows and columns or more in at
-    most 6 steps), their sums in 32."""
+    for each step.  Result of `out_dtype` (default: g's type); `out` may be g.  Products are made of 22 significant bits (fp16 operands for a bfloat16 result of 256 rows and columns or more
+    whose steps keep what that leaves small, as five of the default do), their sums in 32."""
     _no_history(g)
     (m, n), device = _shape(g, "g")
     dtype = g.dtype
