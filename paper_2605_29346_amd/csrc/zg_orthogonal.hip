@@ -513,8 +513,8 @@ Bounds bounds_of(double top, const float *k)
     return r;
 }
 
-// the exponent that values of at most `top` are held with in fp16, whose range ends at 65504
-int exponent_for(double top) { return top > 0.0 ? std::min(24, 14 - (int)std::ceil(std::log2(top))) : 24; }
+// The exponent that values of at most `top` are held with in fp16, whose range ends at 65504.  Up to 100 the products' factors, differences of three of these, are numbers of fp32, or of no account beside what they are added to.
+int exponent_for(double top) { return top > 0.0 ? std::min(100, 14 - (int)std::ceil(std::log2(top))) : 0; }
 
 constexpr double kMostTop = 1024.0; // singular values that a step may reach
 
