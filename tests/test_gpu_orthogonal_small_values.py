@@ -19,10 +19,10 @@ def _need_gpu():
     zg.lib()
 
 
-SMALL = [[(1e-5, 0.0, 0.0), (1e5, -5e14, 0.0)], [(0.0, 0.0, 1e-4), (1e4, -3e11, 0.0), (3.0, -3.0, 1.0)]]
+SMALL = [[(1e-5, 0.0, 0.0), (1e5, -5e14, 0.0)], [(1e-7, 0.0, 0.0), (1e7, -5e20, 0.0), (1.5, -0.5, 0.0)], [(0.0, 0.0, 1e-4), (1e4, -3e11, 0.0), (3.0, -3.0, 1.0)]]
 
 
-@pytest.mark.parametrize("k", SMALL, ids=["1e-5", "1e-4 of the fifth"])
+@pytest.mark.parametrize("k", SMALL, ids=["1e-5", "1e-7", "1e-4 of the fifth"])
 @pytest.mark.parametrize("kind", [F32, BF16], ids=str)
 @pytest.mark.parametrize("size", [(40, 60), (300, 260)], ids=str)
 def test_steps_through_very_small_values(size, kind, k):
