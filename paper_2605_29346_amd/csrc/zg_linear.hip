@@ -24,7 +24,7 @@ template <class T, class O, bool A_TURNED, bool B_TURNED> __global__ __launch_bo
 template <class T> __global__ __launch_bounds__(256) void k_few(ProductArgs p) { few_tile<T>(p); }
 
 // The sum over the parts, and what happens to it (16 parts of 1024 x 1024: 12 us, 5.6 TB/s; 256 of 256 x 200: 12 us): groups of eight cells, each with `lanes` lanes (a power of two up to 32) that have every so
-// manieth part each; then the lanes in order.  Up to 32 parts are added one after the other whatever the lanes are.
+// manieth part each; then the lanes in order.  One lane, or as many as parts, add them one after the other; beyond 32 parts there are 32 lanes: the order goes by the number of parts alone (dense_join).
 struct JoinArgs {
     const float *part;
     uint32_t M, N, splits, lanes;
@@ -295,10 +295,11 @@ int dense_product(hipStream_t st, int32_t type, const ProductArgs &p, float *par
 
 int dense_join(hipStream_t st, const float *part, uint32_t M, uint32_t N, uint32_t splits, const Epilogue &e, Rows rows)
 {
-    // Lanes enough to fill the chip, no more than there are parts: 2 parts of 16384 x 1024 with one lane 36 us, with 32 212.
+    // One lane, or one for each part (32 beyond that): sums whose order goes by the result's size would give other bits for other sizes.  us with one / each / lanes in between: 2048 x 1024 of 16 parts 23.9 / 28.6,
+    // 1024 x 1024 of 16 12.2 / 12.7 / 12.4, 1024 x 512 of 16 8.9 / 9.2 / 7.7, 512 x 512 of 32 13.3 / 10.1 / 7.8, 256 x 256 of 32 11.5 / 6.4.
     const uint64_t groups = (uint64_t)M * ((N + 7) / 8);
     uint32_t lanes = 1;
-    while (lanes < 32 && lanes < splits && (groups * lanes < (1 << 18) || splits > 32)) lanes *= 2;
+    while (lanes < 32 && lanes < splits && (splits > 32 || groups < 65536)) lanes *= 2;
     return launch(st, k_join, grid_of((groups * lanes + 255) / 256), 256, JoinArgs{part, M, N, splits, lanes, e, rows});
 }
 
