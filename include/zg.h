@@ -542,7 +542,7 @@ int zg_linear_cross_entropy(const zg_linear_cross_entropy_args *a, void *d_works
 /* Gradients of zg_linear_cross_entropy's loss: with dZ[i,c] = g weight[i] / total (exp(Z[i,c] - lse[i]) - [c = label[i]]) for the rows that count, 0 for the others,
  *   dA = dZ W,  dW = dZ^T A,  dbias = sum of dZ over the rows.
  * g = *d_dloss (NULL: 1), total = *d_total (NULL: 1, the gradients of the sum; 0: all gradients are 0).  d_dA, d_dW and d_dbias may be NULL.  The logits are made again,
- * a piece of the classes at a time; dZ is held in dtype (rounded once, the products' operand), without g / total, which is applied behind the sums, and
+ * a piece of them at a time (dW and dbias are sums over pieces of the rows in fp32 where there are some); dZ is held in dtype (rounded once, the products' operand), without g / total, which is applied behind the sums, and
  * where there are weights, or dtype is ZG_F16, beside a power of two that brings the largest |weight| to 2^14.  dbias is summed from dZ's fp32 values.  exp(Z - lse) is made from lse as fp32 holds it, off by
  * 2^-23 |lse| of itself, and at most 1.  A row that does not count is still an operand of dW (as a zero times what A holds there). */
 typedef struct {
@@ -566,7 +566,9 @@ typedef struct {
     int64_t ld_dW;
     float *d_dbias;
 } zg_linear_cross_entropy_grad_args;
-/* Workspace bytes of the call with this very struct: up to 2^29 bytes of dZ (4096 classes of it, where that is more), parts of the sums, and copies as above.  Host only. */
+/* Workspace bytes of the call with this very struct: dZ a piece of the classes, or of rows and classes, at a time, parts of the sums, and copies as above (of a piece of A's rows).  Up to 7 x 2^28 bytes; where that does
+ * not do, the least of some choices of pieces, beside those copies never more than the logits would take in dtype, an eighth of that and 2^28 bytes, and where they are large in the main a sum at 32 bits of the smaller of rows and classes
+ * by `in`.  Host only. */
 int zg_linear_cross_entropy_backward_workspace(const zg_linear_cross_entropy_grad_args *a, size_t *bytes);
 int zg_linear_cross_entropy_backward(const zg_linear_cross_entropy_grad_args *a, void *d_workspace, size_t workspace_bytes, void *stream);
 

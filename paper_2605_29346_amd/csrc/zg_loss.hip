@@ -569,8 +569,8 @@ template <class T> __global__ __launch_bounds__(256, 2) void k_loss_part_chunks(
 template <> __global__ __launch_bounds__(256, 3) void k_loss_part_chunks<float>(ProductArgs p) { chunks_tile<float, float, 128, 128, false, true>(p); }
 template <class T> __global__ __launch_bounds__(512, 2) void k_loss_part_long(ProductArgs p) { long_tiles<T, float, false, true>(p); }
 
-// dbias = power x the sum over the groups of rows: C classes to a workgroup, 1024 / C groups side by side, then in order.
-template <int C> __global__ __launch_bounds__(1024) void k_loss_bias(Rows rows, uint32_t group, uint32_t N, const float *part, int64_t ld_part, const float *power, float *out)
+// dbias = power x the sum over the groups of rows: C classes to a workgroup, 1024 / C groups side by side, then in order.  `more`: these rows are not the first.
+template <int C> __global__ __launch_bounds__(1024) void k_loss_bias(Rows rows, uint32_t group, uint32_t N, const float *part, int64_t ld_part, const float *power, float *out, bool more)
 {
     constexpr int G = 1024 / C;
     __shared__ float lds[G][C];
@@ -586,7 +586,14 @@ template <int C> __global__ __launch_bounds__(1024) void k_loss_bias(Rows rows, 
         if (g < (uint32_t)k) lds[g][c] += lds[g + k][c];
         __syncthreads();
     }
-    if (g == 0 && n < N) out[n] = lds[0][c] * *power;
+    if (g == 0 && n < N) out[n] = fmaf(lds[0][c], *power, more ? out[n] : 0.0f);
+}
+
+// how many rows of each piece of `step` rows there are
+__global__ __launch_bounds__(256) void k_row_counts(Rows rows, uint32_t step, uint32_t pieces, uint32_t *counts)
+{
+    const uint64_t i = (uint64_t)block_number() * 256 + threadIdx.x, first = i * step, live = rows.live();
+    if (i < pieces) counts[i] = (uint32_t)(first < live ? min(live - first, (uint64_t)step) : 0);
 }
 
 // ---- operands that lie anyhow -----------------------------------------------------------------------------------------------------
@@ -625,6 +632,8 @@ constexpr uint32_t group_rows(Kind k, bool f32) { return k == kFew ? 16 : k == k
 
 // Of dZ.  More has it go through memory twice, less makes dA of more parts: 16384 x 1024 x 65536 bf16, all gradients, with 2^27 .. 2^31 bytes 7.5, 7.2, 6.9, 7.0, 7.0 ms.
 constexpr int64_t kPieceBytes = int64_t(1) << 29;
+constexpr int64_t kPartBytes = int64_t(1) << 30;  // of parts of dA that wait for their join, if more than it takes at least
+constexpr int64_t kShareBytes = int64_t(7) << 28; // a workspace that is always fine: the two above and parts of dW and dbias
 // Classes to a part of dA's sum, at least: few rows and columns are few tiles, and a part's steps come one behind the other.  The parts' kernel with 1024 / 256 / 128 / 64: f32 1 x 638 x 9054 97 / 32 / 23 / 18 us,
 // 771 x 34 x 2012 132 / 23 / 15 / 13, 300 x 256 x 5000 88 / 24 / 18 / 20, bf16 2000 x 64 x 10000 35 / 19 / 19 / 19, 300 x 256 x 5000 39 / 14 / 12 / 16; the join takes 1 to 4 us more with 64 parts than with 8.
 constexpr int64_t kPartTerms = 128;
@@ -730,40 +739,66 @@ TopPlan top_plan(const Shape &s)
 struct DzPlan {
     Packed pk;
     Kind kind;
-    int64_t piece, pieces, ld_dz;
-    uint32_t splits_A, slots_A, splits_W; // parts of a piece's sum for dA, parts that there is room for, parts of dW's
-    size_t off_pack[2], off_power, off_tops, off_dz, off_part_A, off_part_W, off_bias, total;
+    int64_t step, steps, piece, pieces, ld_dz; // rows and classes of a piece of dZ
+    uint32_t splits_A, slots_A, splits_W;      // parts of a piece's sum for dA, parts that there is room for, parts of dW's
+    size_t off_pack[2], off_power, off_tops, off_counts, off_dz, off_part_A, off_part_W, off_sum_W, off_bias, total;
 };
 
-DzPlan dz_plan(const Shape &s, bool dA, bool dW, bool dbias, bool weight)
+struct Wanted {
+    bool dA, dW, dbias, weight;
+};
+
+DzPlan dz_layout(const Shape &s, const Wanted &w, int64_t step, int64_t piece)
 {
     DzPlan t{};
     const Taker take{t.total};
-    const int64_t e = (int64_t)type_size(s.dtype), rows = std::max<int64_t>(1, s.rows);
-    t.pk = packed_plan(s, take, t.off_pack);
-    t.piece = std::max<int64_t>(4096, kPieceBytes / (rows * e) / 256 * 256);
-    if (t.piece >= s.out) t.piece = s.out;
-    t.pieces = (s.out + t.piece - 1) / t.piece;
-    t.ld_dz = (t.piece + 7) / 8 * 8;
-    Shape one = s;
-    one.out = (int32_t)t.piece;
-    t.kind = logits_kind(s.dtype, logits_product(one, t.pk, nullptr), false);
+    const int64_t e = (int64_t)type_size(s.dtype), rows = std::max<int64_t>(1, step);
+    Shape some = s;
+    some.rows = step;
+    t.pk = packed_plan(some, take, t.off_pack);
+    t.step = step, t.steps = (std::max<int64_t>(1, s.rows) + rows - 1) / rows;
+    t.piece = piece, t.pieces = (s.out + piece - 1) / piece;
+    t.ld_dz = (piece + 7) / 8 * 8;
+    some.out = (int32_t)piece;
+    t.kind = logits_kind(s.dtype, logits_product(some, t.pk, nullptr), false);
     t.off_power = take(sizeof(float));
-    if (weight) t.off_tops = take(kWeightBlocks * sizeof(float));
-    t.off_dz = take((size_t)s.rows * t.ld_dz * e);
-    const int64_t tiles_A = (rows + 255) / 256 * ((s.in + 127) / 128), tiles_W = (t.piece + 255) / 256 * ((s.in + 127) / 128);
+    if (w.weight) t.off_tops = take(kWeightBlocks * sizeof(float));
+    if (t.steps > 1) t.off_counts = take((size_t)t.steps * sizeof(uint32_t));
+    t.off_dz = take((size_t)step * t.ld_dz * e);
+    const int64_t tiles_A = (rows + 255) / 256 * ((s.in + 127) / 128), tiles_W = (piece + 255) / 256 * ((s.in + 127) / 128);
     // Parts enough for two tiles of 256 x 128 to a compute unit; where tiles of 256 x 256, which would be taken from 256 of them on, were a third empty, fewer than that.
-    const int64_t wide_A = (rows + 255) / 256 * ((s.in + 255) / 256), wide_W = (t.piece + 255) / 256 * ((s.in + 255) / 256);
+    const int64_t wide_A = (rows + 255) / 256 * ((s.in + 255) / 256), wide_W = (piece + 255) / 256 * ((s.in + 255) / 256);
     const bool narrow = s.dtype != ZG_F32 && (s.in + 255) / 256 * 256 * 3 >= (s.in + 127) / 128 * 128 * 4;
-    t.splits_A = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(narrow ? std::min(512 / tiles_A, 255 / wide_A) : 512 / tiles_A, t.piece / kPartTerms));
+    t.splits_A = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(narrow ? std::min(512 / tiles_A, 255 / wide_A) : 512 / tiles_A, piece / kPartTerms));
     t.splits_W = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(narrow ? std::min(512 / tiles_W, 255 / wide_W) : 512 / tiles_W, (rows + 255) / 256));
-    const int64_t parts = t.pieces * t.splits_A;
-    t.slots_A = (uint32_t)(parts == 1 ? 0 : std::min<int64_t>(parts, t.splits_A + 4));
-    if (dA) t.off_part_A = take((size_t)t.slots_A * s.rows * s.in * sizeof(float));
-    if (dW && t.splits_W > 1) t.off_part_W = take((size_t)t.splits_W * t.piece * s.in * sizeof(float));
+    const int64_t parts = t.pieces * t.splits_A, room = kPartBytes / (rows * s.in * (int64_t)sizeof(float));
+    t.slots_A = (uint32_t)(parts == 1 ? 0 : std::min(parts, t.splits_A + std::min<int64_t>(4, std::max<int64_t>(1, room - t.splits_A))));
+    if (w.dA) t.off_part_A = take((size_t)t.slots_A * step * s.in * sizeof(float));
+    if (w.dW && (t.splits_W > 1 || t.steps > 1)) t.off_part_W = take((size_t)t.splits_W * piece * s.in * sizeof(float));
+    if (w.dW && t.steps > 1) t.off_sum_W = take((size_t)s.out * s.in * sizeof(float));
     const uint32_t group = group_rows(t.kind, s.dtype == ZG_F32);
-    if (dbias) t.off_bias = take((size_t)((s.rows + group - 1) / group) * t.ld_dz * sizeof(float));
+    if (w.dbias) t.off_bias = take((size_t)((step + group - 1) / group) * t.ld_dz * sizeof(float));
     return t;
+}
+
+// Pieces of the classes, 4096 at least, of all rows; where dZ whole takes less than such a piece and the parts of dA that they leave, whole; and where neither is small, pieces of the rows too, the
+// largest that are: then dW is a sum over those, in fp32.
+DzPlan dz_plan(const Shape &s, const Wanted &w)
+{
+    const auto classes = [&](int64_t rows) {
+        const int64_t most = kPieceBytes / (std::max<int64_t>(1, rows) * (int64_t)type_size(s.dtype)) / 256 * 256;
+        return std::min<int64_t>(s.out, std::max<int64_t>(4096, most));
+    };
+    DzPlan best = dz_layout(s, w, s.rows, classes(s.rows));
+    const auto better = [&](int64_t step, int64_t piece) {
+        const DzPlan t = dz_layout(s, w, step, piece);
+        if (t.total < best.total) best = t;
+    };
+    if (best.pieces > 1) better(s.rows, s.out);
+    const int64_t whole = kPieceBytes / ((s.out + 7) / 8 * 8 * (int64_t)type_size(s.dtype)) / 256 * 256; // rows of all classes
+    for (int64_t step = std::max<int64_t>(65536, whole); step >= 4096 && best.total > (size_t)kShareBytes; step = step > 65536 ? 65536 : step / 2)
+        if (step < s.rows) better(step, classes(step));
+    return best;
 }
 
 int check_labels(const char *what, const void *p, int32_t type)
@@ -798,19 +833,23 @@ template <class A> int check_common(const A *a)
     return ZG_OK;
 }
 
+Wanted wanted_of(const zg_linear_cross_entropy_grad_args *a) { return {a->d_dA != nullptr, a->d_dW != nullptr, a->d_dbias != nullptr, a->d_weight != nullptr}; }
+
 template <class A> Shape shape_of(const A *a) { return {a->rows, a->in, a->out, a->dtype, a->d_A, a->d_W, a->ld_A, a->ld_W}; }
 
-template <class A> int launch_packs(hipStream_t st, const A *a, char *ws, const size_t (&off)[2], Packed &pk)
+// the copies of W, and of the rows of A from `first` on (`rows` of them)
+template <class A> int pack_W(hipStream_t st, const A *a, char *ws, const size_t (&off)[2], Packed &pk)
 {
-    if (pk.copy_A) {
-        ZG_TRY(launch_pack(st, a->dtype, a->d_A, a->ld_A, Rows{a->d_rows, (uint32_t)a->rows}, a->in, ws + off[0]));
-        pk.a.p = ws + off[0];
-    }
-    if (pk.copy_W) {
-        ZG_TRY(launch_pack(st, a->dtype, a->d_W, a->ld_W, Rows{nullptr, (uint32_t)a->out}, a->in, ws + off[1]));
-        pk.w.p = ws + off[1];
-    }
-    return ZG_OK;
+    if (!pk.copy_W) return ZG_OK;
+    pk.w.p = ws + off[1];
+    return launch_pack(st, a->dtype, a->d_W, a->ld_W, Rows{nullptr, (uint32_t)a->out}, a->in, ws + off[1]);
+}
+
+template <class A> int pack_A(hipStream_t st, const A *a, char *ws, const size_t (&off)[2], Packed &pk, int64_t first, Rows rows)
+{
+    const char *const from = static_cast<const char *>(a->d_A) + first * a->ld_A * (int64_t)type_size(a->dtype);
+    pk.a.p = pk.copy_A ? ws + off[0] : from;
+    return pk.copy_A ? launch_pack(st, a->dtype, from, a->ld_A, rows, a->in, ws + off[0]) : ZG_OK;
 }
 
 template <class T> int launch_tops(hipStream_t st, Kind kind, const TopArgs &p)
@@ -897,7 +936,8 @@ int zg_linear_cross_entropy(const zg_linear_cross_entropy_args *a, void *d_works
         Top *const part = reinterpret_cast<Top *>(ws + t.off_part);
         float *const at = reinterpret_cast<float *>(ws + t.off_at);
         if (a->rows > 0) {
-            ZG_TRY(launch_packs(st, a, ws, t.off_pack, t.pk));
+            ZG_TRY(pack_W(st, a, ws, t.off_pack, t.pk));
+            ZG_TRY(pack_A(st, a, ws, t.off_pack, t.pk, 0, Rows{a->d_rows, (uint32_t)a->rows}));
             TopArgs p{};
             static_cast<ProductArgs &>(p) = logits_product(shape_of(a), t.pk, a->d_rows);
             p.e.bias = a->d_bias;
@@ -925,7 +965,7 @@ int zg_linear_cross_entropy_backward_workspace(const zg_linear_cross_entropy_gra
     return entry([&]() -> int {
         ZG_TRY(check_common(a));
         if (!bytes) return fail(ZG_EINVAL, "null argument");
-        *bytes = dz_plan(shape_of(a), a->d_dA, a->d_dW, a->d_dbias, a->d_weight).total;
+        *bytes = dz_plan(shape_of(a), wanted_of(a)).total;
         return ZG_OK;
     });
 }
@@ -948,17 +988,17 @@ int zg_linear_cross_entropy_backward(const zg_linear_cross_entropy_grad_args *a,
             ZG_TRY(check_apart(dW, {A, W, bias, labels, weight, count, lse, total, dloss, dA}));
             ZG_TRY(check_apart(dbias, {A, W, bias, labels, weight, count, lse, total, dloss, dA, dW}));
         }
-        const bool want_A = a->d_dA, want_W = a->d_dW, want_b = a->d_dbias;
-        DzPlan t = dz_plan(shape_of(a), want_A, want_W, want_b, a->d_weight);
+        const Wanted want = wanted_of(a);
+        DzPlan t = dz_plan(shape_of(a), want);
         ZG_TRY(check_workspace(d_workspace, workspace_bytes, t.total));
-        if (!want_A && !want_W && !want_b) return ZG_OK;
+        if (!want.dA && !want.dW && !want.dbias) return ZG_OK;
         const hipStream_t st = static_cast<hipStream_t>(stream);
         char *const ws = static_cast<char *>(d_workspace);
-        const Rows rows{a->d_rows, (uint32_t)a->rows};
+        const Rows all{a->d_rows, (uint32_t)a->rows};
         float *const power = reinterpret_cast<float *>(ws + t.off_power);
-        if (a->rows > 0) ZG_TRY(launch_packs(st, a, ws, t.off_pack, t.pk));
+        if (a->rows > 0) ZG_TRY(pack_W(st, a, ws, t.off_pack, t.pk));
         FactorArgs f{};
-        f.rows = rows;
+        f.rows = all;
         f.lse = a->d_lse, f.weight = a->d_weight, f.total = a->d_total, f.dloss = a->d_dloss;
         f.labels = {a->d_labels, a->label_dtype == ZG_I64, (uint32_t)a->out};
         // fp16's range does not hold a softmax over many classes as it is: |dZ| <= 1 is brought to the top of it.  Weights may be of any size: the largest is brought there, whatever the type.
@@ -970,93 +1010,113 @@ int zg_linear_cross_entropy_backward(const zg_linear_cross_entropy_grad_args *a,
             ZG_TRY(launch(st, k_loss_weight_top, dim3(kWeightBlocks), 256, f, tops));
         }
         if (a->rows == 0) ZG_TRY(launch(st, k_loss_power, dim3(1), 64, f));
+        uint32_t *const counts = t.steps > 1 && a->d_rows ? reinterpret_cast<uint32_t *>(ws + t.off_counts) : nullptr;
+        if (counts) ZG_TRY(launch(st, k_row_counts, grid_of(((uint64_t)t.steps + 255) / 256), 256, all, (uint32_t)t.step, (uint32_t)t.steps, counts));
         const auto run = [&](auto zero) -> int {
             using T = decltype(zero);
             T *const dz = reinterpret_cast<T *>(ws + t.off_dz);
             float *const part_A = reinterpret_cast<float *>(ws + t.off_part_A), *const bias_part = reinterpret_cast<float *>(ws + t.off_bias);
+            float *const part_W = reinterpret_cast<float *>(ws + t.off_part_W), *const sum_W = reinterpret_cast<float *>(ws + t.off_sum_W);
             const bool parts_A = t.pieces * t.splits_A > 1;
-            const int64_t cells_A = a->rows * a->in;
-            uint32_t filled = 0; // parts of dA that are there
-            for (int64_t first = 0; first < a->out; first += t.piece) {
-                const uint32_t n = (uint32_t)std::min<int64_t>(t.piece, a->out - first), n8 = (n + 7) / 8 * 8;
-                Operand w = t.pk.w;
-                w.p = static_cast<const T *>(w.p) + first * w.ld;
-                if (a->rows > 0) {
-                    Shape s = shape_of(a);
-                    s.out = (int32_t)n;
-                    DzArgs<T> p{};
-                    static_cast<ProductArgs &>(p) = logits_product(s, t.pk, a->d_rows);
-                    p.b = w;
-                    p.e.bias = a->d_bias ? a->d_bias + first : nullptr;
-                    p.e.Y = dz, p.e.ld_Y = t.ld_dz;
-                    p.f = f, p.first = (uint32_t)first;
-                    p.bias_part = want_b ? bias_part : nullptr, p.ld_part = t.ld_dz;
-                    ZG_TRY(launch_dz(st, t.kind, p));
-                }
-                if (want_b) {
-                    const uint32_t group = group_rows(t.kind, sizeof(T) == 4);
-                    if (n < 1024) ZG_TRY(launch(st, k_loss_bias<8>, dim3((n + 7) / 8), 1024, rows, group, n, bias_part, t.ld_dz, power, a->d_dbias + first));
-                    else ZG_TRY(launch(st, k_loss_bias<32>, dim3((n + 31) / 32), 1024, rows, group, n, bias_part, t.ld_dz, power, a->d_dbias + first));
-                }
-                if (want_W) {
-                    ProductArgs p{};
-                    p.a = {dz, t.ld_dz, true, true};
-                    p.b = t.pk.a, p.b.turned = true;
-                    p.M = n, p.N = (uint32_t)a->in, p.K = (uint32_t)a->rows;
-                    p.rows = rows, p.rows_are_k = 1;
-                    p.splits = t.splits_W;
-                    p.e.factor = 1.0f, p.e.power = power, p.e.type = a->dtype;
-                    p.e.Y = static_cast<T *>(a->d_dW) + first * a->ld_dW, p.e.ld_Y = a->ld_dW;
-                    float *const part = reinterpret_cast<float *>(ws + t.off_part_W);
-                    if (sizeof(T) == 4 && n <= 64 && p.splits > 1 && in_chunks<T>(p.b, p.N, p.K)) {
-                        const Epilogue result = p.e;
-                        p.e = Epilogue{};
-                        p.e.factor = 1.0f, p.e.type = ZG_F32, p.e.Y = part, p.e.ld_Y = p.N, p.e.part = (int64_t)p.M * p.N;
-                        ZG_TRY(launch(st, k_loss_part_narrow, tile_grid<64, 128>(p), 256, p));
-                        ZG_TRY(dense_join(st, part, p.M, p.N, p.splits, result, {nullptr, p.M}));
-                    } else {
-                        ZG_TRY(dense_product(st, a->dtype, p, part));
+            Epilogue result_W{};
+            result_W.factor = 1.0f, result_W.power = power, result_W.type = a->dtype, result_W.Y = a->d_dW, result_W.ld_Y = a->ld_dW;
+            for (int64_t step = 0; step < t.steps; ++step) {
+                const int64_t m0 = step * t.step, m = std::min(t.step, a->rows - m0), cells_A = m * a->in;
+                const Rows rows{counts ? counts + step : t.steps > 1 ? nullptr : a->d_rows, (uint32_t)m};
+                FactorArgs here = f;
+                here.lse += m0;
+                if (here.weight) here.weight += m0;
+                here.labels.p = static_cast<const char *>(f.labels.p) + m0 * (f.labels.wide ? 8 : 4);
+                ZG_TRY(pack_A(st, a, ws, t.off_pack, t.pk, m0, rows));
+                uint32_t filled = 0; // parts of dA that are there
+                for (int64_t first = 0; first < a->out; first += t.piece) {
+                    const uint32_t n = (uint32_t)std::min<int64_t>(t.piece, a->out - first), n8 = (n + 7) / 8 * 8;
+                    Operand w = t.pk.w;
+                    w.p = static_cast<const T *>(w.p) + first * w.ld;
+                    if (m > 0) {
+                        Shape s = shape_of(a);
+                        s.rows = m, s.out = (int32_t)n;
+                        DzArgs<T> p{};
+                        static_cast<ProductArgs &>(p) = logits_product(s, t.pk, rows.d_rows);
+                        p.b = w;
+                        p.e.bias = a->d_bias ? a->d_bias + first : nullptr;
+                        p.e.Y = dz, p.e.ld_Y = t.ld_dz;
+                        p.f = here, p.first = (uint32_t)first;
+                        p.bias_part = want.dbias ? bias_part : nullptr, p.ld_part = t.ld_dz;
+                        ZG_TRY(launch_dz(st, t.kind, p));
                     }
-                }
-                if (want_A && a->rows > 0) {
-                    ProductArgs p{};
-                    p.a = {dz, t.ld_dz, false, true};
-                    p.b = w, p.b.turned = true;
-                    p.M = (uint32_t)a->rows, p.N = (uint32_t)a->in;
-                    const bool chunks = in_chunks<T>(p.b, p.N, n8); // (dZ is)
-                    p.K = chunks ? n8 : n, p.b_short = chunks ? n8 - n : 0;
-                    p.rows = rows;
-                    p.e.factor = 1.0f;
-                    if (!parts_A) {
-                        p.splits = 1;
-                        p.e.power = power, p.e.type = a->dtype;
-                        p.e.Y = a->d_dA, p.e.ld_Y = a->ld_dA;
-                        // (bf16 2304 x 256 of 16 terms: 8.6 us in tiles of 256 x 128, 5.6 in tiles of 64 x 64)
-                        if (tile_blocks<256, 128>(p) < 128 && p.K <= 256) {
-                            p.K = n, p.b_short = 0;
-                            ZG_TRY(launch(st, k_loss_part_anyhow<T>, tile_grid<64, 64>(p), 256, p));
+                    if (want.dbias) {
+                        const uint32_t group = group_rows(t.kind, sizeof(T) == 4);
+                        if (n < 1024) ZG_TRY(launch(st, k_loss_bias<8>, dim3((n + 7) / 8), 1024, rows, group, n, bias_part, t.ld_dz, power, a->d_dbias + first, step > 0));
+                        else ZG_TRY(launch(st, k_loss_bias<32>, dim3((n + 31) / 32), 1024, rows, group, n, bias_part, t.ld_dz, power, a->d_dbias + first, step > 0));
+                    }
+                    if (want.dW) {
+                        ProductArgs p{};
+                        p.a = {dz, t.ld_dz, true, true};
+                        p.b = t.pk.a, p.b.turned = true;
+                        p.M = n, p.N = (uint32_t)a->in, p.K = (uint32_t)m;
+                        p.rows = rows, p.rows_are_k = 1;
+                        p.splits = t.splits_W;
+                        Epilogue to = result_W; // or onto the sums of the rows in front of these
+                        to.Y = static_cast<T *>(a->d_dW) + first * a->ld_dW;
+                        if (t.steps > 1) {
+                            to = Epilogue{};
+                            to.factor = 1.0f, to.type = ZG_F32, to.Y = sum_W + first * a->in, to.ld_Y = a->in;
+                            if (step > 0) to.R = to.Y, to.ld_R = a->in;
+                        }
+                        const bool narrow = sizeof(T) == 4 && n <= 64 && p.splits > 1 && in_chunks<T>(p.b, p.N, p.K);
+                        if (!narrow && (p.splits > 1 || t.steps == 1)) {
+                            p.e = to;
+                            ZG_TRY(dense_product(st, a->dtype, p, part_W));
                         } else {
-                            ZG_TRY(dense_product(st, a->dtype, p));
+                            p.e.factor = 1.0f, p.e.type = ZG_F32, p.e.Y = part_W, p.e.ld_Y = p.N, p.e.part = (int64_t)p.M * p.N;
+                            ZG_TRY(narrow ? launch(st, k_loss_part_narrow, tile_grid<64, 128>(p), 256, static_cast<const ProductArgs &>(p)) : dense_product(st, a->dtype, p));
+                            ZG_TRY(dense_join(st, part_W, p.M, p.N, p.splits, to, {nullptr, p.M}));
                         }
-                    } else {
-                        Epilogue sum{};
-                        sum.factor = 1.0f, sum.type = ZG_F32, sum.Y = part_A, sum.ld_Y = a->in;
-                        if (filled + t.splits_A > t.slots_A) { // no room: what is there becomes the first part
-                            ZG_TRY(dense_join(st, part_A, p.M, p.N, filled, sum, rows));
-                            filled = 1;
+                    }
+                    if (want.dA && m > 0) {
+                        ProductArgs p{};
+                        p.a = {dz, t.ld_dz, false, true};
+                        p.b = w, p.b.turned = true;
+                        p.M = (uint32_t)m, p.N = (uint32_t)a->in;
+                        // dZ lies in chunks, and the rows of a tile, 256 or as many as there are, in reach of each other: more than 2^29 bytes of it are there only where a row has 4096 classes, or where all of
+                        // them take no more than two rows of dA at 32 bits do, 2^18 bytes.
+                        const bool chunks = in_chunks<T>(p.b, p.N, n8);
+                        p.K = chunks ? n8 : n, p.b_short = chunks ? n8 - n : 0;
+                        p.rows = rows;
+                        p.e.factor = 1.0f;
+                        if (!parts_A) {
+                            p.splits = 1;
+                            p.e.power = power, p.e.type = a->dtype;
+                            p.e.Y = static_cast<T *>(a->d_dA) + m0 * a->ld_dA, p.e.ld_Y = a->ld_dA;
+                            // (bf16 2304 x 256 of 16 terms: 8.6 us in tiles of 256 x 128, 5.6 in tiles of 64 x 64)
+                            if (tile_blocks<256, 128>(p) < 128 && p.K <= 256) {
+                                p.K = n, p.b_short = 0;
+                                ZG_TRY(launch(st, k_loss_part_anyhow<T>, tile_grid<64, 64>(p), 256, p));
+                            } else {
+                                ZG_TRY(dense_product(st, a->dtype, p));
+                            }
+                        } else {
+                            Epilogue sum{};
+                            sum.factor = 1.0f, sum.type = ZG_F32, sum.Y = part_A, sum.ld_Y = a->in;
+                            if (filled + t.splits_A > t.slots_A) { // no room: what is there becomes the first part
+                                ZG_TRY(dense_join(st, part_A, p.M, p.N, filled, sum, rows));
+                                filled = 1;
+                            }
+                            p.splits = t.splits_A;
+                            p.e.type = ZG_F32, p.e.Y = part_A + filled * cells_A, p.e.ld_Y = a->in, p.e.part = cells_A;
+                            ZG_TRY(launch_parts<T>(st, p, chunks));
+                            filled += t.splits_A;
                         }
-                        p.splits = t.splits_A;
-                        p.e.type = ZG_F32, p.e.Y = part_A + filled * cells_A, p.e.ld_Y = a->in, p.e.part = cells_A;
-                        ZG_TRY(launch_parts<T>(st, p, chunks));
-                        filled += t.splits_A;
                     }
                 }
+                if (want.dA && parts_A && m > 0) {
+                    Epilogue e{};
+                    e.factor = 1.0f, e.power = power, e.type = a->dtype, e.Y = static_cast<T *>(a->d_dA) + m0 * a->ld_dA, e.ld_Y = a->ld_dA;
+                    ZG_TRY(dense_join(st, part_A, (uint32_t)m, (uint32_t)a->in, filled, e, rows));
+                }
             }
-            if (want_A && parts_A && a->rows > 0) {
-                Epilogue e{};
-                e.factor = 1.0f, e.power = power, e.type = a->dtype, e.Y = a->d_dA, e.ld_Y = a->ld_dA;
-                ZG_TRY(dense_join(st, part_A, (uint32_t)a->rows, (uint32_t)a->in, filled, e, rows));
-            }
+            if (want.dW && t.steps > 1) return dense_join(st, sum_W, (uint32_t)a->out, (uint32_t)a->in, 1, result_W, {nullptr, (uint32_t)a->out});
             return ZG_OK;
         };
         return with_wide_type(a->dtype, run);
