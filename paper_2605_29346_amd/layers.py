@@ -114,6 +114,7 @@ def _vector(t, what, n, dtype, device):
 def _out(t, what, m, n, dtype, device, made, like=None):
     """(tensor, address, row stride) of an output: what the caller gave, or a new one"""
     if t is not None:
+        made.append((t,))
         return (t, *_matrix(t, what, m, n, dtype, device))
     t = torch.empty_like(like) if like is not None and like.is_contiguous() else torch.empty((m, n), dtype=dtype, device=device)
     made.append(t)
@@ -123,6 +124,7 @@ def _out(t, what, m, n, dtype, device, made, like=None):
 def _out_vector(t, what, n, device, made):
     """(tensor, address) of an output of float32"""
     if t is not None:
+        made.append((t,))
         return t, _vector(t, what, n, _F32, device)
     t = torch.empty(n, dtype=_F32, device=device)
     made.append(t)
@@ -156,16 +158,10 @@ def _mask(d, rows, device):
     return d.p, d.key & 0xFFFFFFFFFFFFFFFF, d.layer & 0xFFFFFFFF, 0, _vector(d.ids, "the dropout's ids", rows, _I32, device)
 
 
-def _written(given):
-    """Counts what a call wrote into tensors that the caller gave (or None) as changes in place: autograd refuses a backward pass that saved one before."""
-    given = [t for t in given if t is not None]
-    if given:
-        torch._C._increment_version(given)
-
-
 def _run(name, args, device, stream, made=(), workspace=False):
     """Enqueues the call on `stream`.  `made`: tensors that were allocated for it - on torch's current stream, whose earlier work another
-    stream has to wait for, and whose memory must not be handed out again before that other stream is done with it."""
+    stream has to wait for, and whose memory must not be handed out again before that other stream is done with it; and in a tuple each what the caller gave
+    to be written: a change in place, so that autograd refuses a backward pass that saved it before."""
     current = torch._C._cuda_getCurrentRawStream(device.index)
     handle = current if stream is None else zg._stream_ptr(stream)
     foreign = None
@@ -186,14 +182,19 @@ def _enqueue(name, args, device, handle, foreign, made, workspace):
             raise zg.ZgError(status)
         ws = torch.empty(need.value, dtype=torch.uint8, device=device)
         made = (*made, ws)
-    if foreign is not None and made:
-        foreign.wait_stream(torch.cuda.current_stream(device))
+    if foreign is not None:
+        new = [t for t in made if type(t) is not tuple]
+        if new:
+            foreign.wait_stream(torch.cuda.current_stream(device))
     status = _entry(name)(args, ws.data_ptr(), need.value, handle) if workspace else _entry(name)(args, handle)
     if foreign is not None:
-        for t in made:
+        for t in new:
             t.record_stream(foreign)
     if status:
         raise zg.ZgError(status)
+    for t in made:
+        if type(t) is tuple:
+            torch._C._increment_version(t)
 
 
 def linear(a, w, *, bias=None, act="none", dropout: Optional[Dropout] = None, residual=None, scale_a=None, scale_w=None, out_dtype=None,
@@ -205,7 +206,6 @@ def linear(a, w, *, bias=None, act="none", dropout: Optional[Dropout] = None, re
     (m, k), device = _shape(a, "a")
     n, dtype = w.shape[0], a.dtype
     kind = out_dtype or (torch.bfloat16 if dtype == torch.float8_e4m3fn else dtype)
-    given = out, preact
     made = []
     out, y, ld_y = _out(out, "out", m, n, kind, device, made, a if k == n and kind is dtype else None)
     preact, z, ld_z = _out(preact, "preact", m, n, kind, device, made) if save or preact is not None else _NONE3
@@ -214,7 +214,6 @@ def linear(a, w, *, bias=None, act="none", dropout: Optional[Dropout] = None, re
                        *_matrix(w, "w", n, k, dtype, device), _vector(scale_w, "scale_w", n, _F32, device), _vector(bias, "bias", n, _F32, device),
                        *(_matrix(residual, "residual", m, n, kind, device) if residual is not None else (0, 0)),
                        y, ld_y, z, ld_z, *_mask(dropout, m, device)), device, stream, made)
-    _written(given)
     return (out, preact) if preact is not None else out
 
 
@@ -225,7 +224,6 @@ def linear_backward(dy, a, w, *, preact=None, act="none", dropout: Optional[Drop
     _no_history(dy, a, w, preact)
     (m, n), device = _shape(dy, "dy")
     k, dtype, kind = w.shape[1], a.dtype, dy.dtype
-    given = da, dw, dbias
     made = []
     da, da_at, ld_da = _out(da, "da", m, k, dtype, device, made) if need[0] or da is not None else _NONE3
     dw, dw_at, ld_dw = _out(dw, "dw", n, k, dtype, device, made) if need[1] or dw is not None else _NONE3
@@ -235,7 +233,6 @@ def linear_backward(dy, a, w, *, preact=None, act="none", dropout: Optional[Drop
                                 *(_matrix(preact, "preact", m, n, kind, device) if preact is not None else (0, 0)),
                                 *_matrix(a, "a", m, k, dtype, device), *_matrix(w, "w", n, k, dtype, device),
                                 da_at, ld_da, dw_at, ld_dw, db_at, *_mask(dropout, m, device)), device, stream, made, workspace=True)
-    _written(given)
     return da, dw, dbias
 
 
@@ -243,13 +240,11 @@ def dropout(x, mask: Optional[Dropout], *, residual=None, rows=None, out=None, s
     """drop(x) + residual; the gradient of x is the same call on the gradient of the result.  `out` may be x or the residual."""
     _no_history(x, residual)
     (m, n), device = _shape(x, "x")
-    given = out,
     dtype, made = x.dtype, []
     out, y, ld_y = _out(out, "out", m, n, dtype, device, made, x)
     _run("zg_dropout", (m, _vector(rows, "rows", 1, _I32, device), n, _type(dtype, "x"), *_matrix(x, "x", m, n, dtype, device),
                         *(_matrix(residual, "residual", m, n, dtype, device) if residual is not None else (0, 0)),
                         y, ld_y, *_mask(mask, m, device)), device, stream, made)
-    _written(given)
     return out
 
 
@@ -262,7 +257,6 @@ def rms_norm(x, *, gain=None, eps=1e-6, residual=None, dropout: Optional[Dropout
     (m, n), device = _shape(x, "x")
     dtype = x.dtype
     kind = out_dtype or dtype
-    given = y, h, rstd, scale
     made = []
     y, y_at, ld_y = _out(y, "y", m, n, kind, device, made, x if kind is dtype else None)
     summed = residual is not None or (dropout is not None and dropout.p > 0)
@@ -274,7 +268,6 @@ def rms_norm(x, *, gain=None, eps=1e-6, residual=None, dropout: Optional[Dropout
                          *(_matrix(residual, "residual", m, n, dtype, device) if residual is not None else (0, 0)),
                          _vector(gain, "gain", n, _F32, device), h_at, ld_h, y_at, ld_y, scale_at, rstd_at,
                          *_mask(dropout, m, device)), device, stream, made)
-    _written(given)
     return NormResult(y, h, rstd, scale)
 
 
@@ -286,7 +279,6 @@ def rms_norm_backward(dy, h, rstd, *, gain=None, dh=None, dropout: Optional[Drop
     _no_history(dy, h, rstd, gain, dh)
     (m, n), device = _shape(dy, "dy")
     dtype = dy.dtype
-    given = dx, dr, dgain
     made = []
     dx, dx_at, ld_dx = _out(dx, "dx", m, n, dtype, device, made, dy)
     two = dr is not None or (need_dr and dropout is not None and dropout.p > 0)
@@ -297,7 +289,6 @@ def rms_norm_backward(dy, h, rstd, *, gain=None, dh=None, dropout: Optional[Drop
                                   *(_matrix(dh, "dh", m, n, dtype, device) if dh is not None else (0, 0)),
                                   dx_at, ld_dx, dr_at, ld_dr, dg_at, *_mask(dropout, m, device)),
          device, stream, made, workspace=True)
-    _written(given)
     return dx, dr, dgain
 
 
@@ -316,7 +307,6 @@ def linear_cross_entropy(a, w, labels, *, bias=None, weight=None, rows=None, los
     _no_history(a, w, bias, weight)
     (m, k), device = _shape(a, "a")
     n, dtype = w.shape[0], a.dtype
-    given = loss, total, lse, row_loss if isinstance(row_loss, torch.Tensor) else None
     made = []
     if loss is None and total is None:
         both = torch.empty(2, dtype=_F32, device=device)
@@ -333,7 +323,6 @@ def linear_cross_entropy(a, w, labels, *, bias=None, weight=None, rows=None, los
     _run("zg_linear_cross_entropy", (m, _vector(rows, "rows", 1, _I32, device), k, n, _type(dtype, "a"), kind, *_matrix(a, "a", m, k, dtype, device),
                                      *_matrix(w, "w", n, k, dtype, device), _vector(bias, "bias", n, _F32, device), labels_at,
                                      _vector(weight, "weight", m, _F32, device), loss_at, total_at, lse_at, each_at), device, stream, made, workspace=True)
-    _written(given)
     return LossResult(loss, total, lse, row_loss)
 
 
@@ -344,7 +333,6 @@ def linear_cross_entropy_backward(a, w, labels, lse, *, bias=None, weight=None, 
     _no_history(a, w, bias, weight, lse, total, dloss)
     (m, k), device = _shape(a, "a")
     n, dtype = w.shape[0], a.dtype
-    given = da, dw, dbias
     made = []
     da, da_at, ld_da = _out(da, "da", m, k, dtype, device, made) if need[0] or da is not None else _NONE3
     dw, dw_at, ld_dw = _out(dw, "dw", n, k, dtype, device, made) if need[1] or dw is not None else _NONE3
@@ -354,7 +342,6 @@ def linear_cross_entropy_backward(a, w, labels, lse, *, bias=None, weight=None, 
                                               *_matrix(w, "w", n, k, dtype, device), _vector(bias, "bias", n, _F32, device), labels_at,
                                               _vector(weight, "weight", m, _F32, device), _vector(lse, "lse", m, _F32, device), _vector(total, "total", 1, _F32, device),
                                               _vector(dloss, "dloss", 1, _F32, device), da_at, ld_da, dw_at, ld_dw, db_at), device, stream, made, workspace=True)
-    _written(given)
     return da, dw, dbias
 
 
@@ -386,12 +373,10 @@ def orthogonalize(g, *, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, out_dtype
     dtype = g.dtype
     kind = out_dtype or (out.dtype if out is not None else dtype)
     k = _steps(coefficients, steps)
-    given = out,
     made = []
     out, at, ld = _out(out, "out", m, n, kind, device, made, g if kind is dtype else None)
     _run("zg_orthogonalize", (m, n, _type(dtype, "g"), _type(kind, "out_dtype"), steps, eps, C.addressof(k), *_matrix(g, "g", m, n, dtype, device), at, ld), device, stream, made,
          workspace=True)
-    _written(given)
     return out
 
 
@@ -405,6 +390,5 @@ def muon_step(w, m, g, *, lr, momentum=0.95, nesterov=True, decay=0.0, scale=Non
         scale = max(1.0, rows / cols) ** 0.5
     _run("zg_muon_step", (rows, cols, _type(w.dtype, "w"), _type(g.dtype, "g"), steps, int(nesterov), lr, momentum, decay, scale, eps, 0.0, C.addressof(k),
                           *_matrix(g, "g", rows, cols, g.dtype, device), *_matrix(m, "m", rows, cols, _F32, device), *_matrix(w, "w", rows, cols, w.dtype, device)),
-         device, stream, workspace=True)
-    _written((w, m))
+         device, stream, ((w,), (m,)), workspace=True)
     return w
