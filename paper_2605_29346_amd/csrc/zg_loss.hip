@@ -1,7 +1,7 @@
 // Softmax cross entropy of a linear layer: the loss over many classes without keeping the logits, and its gradients.
 //
 // z = A W^T + bias.  The product's tiles keep, of every row of their cells, the largest z and the sum of exp(z - largest) - 8 bytes for 32 or 64 logits -, which a
-// second launch joins to lse = log sum exp z.  The gradients make the logits again, a piece of the classes at a time: dZ = f (exp(z - lse) - [class is the label]) leaves the
+// second launch joins to lse = log sum exp z.  The gradients make the logits again, a piece of the classes (and of the rows, where there are many) at a time: dZ = f (exp(z - lse) - [class is the label]) leaves the
 // product's tiles in the operands' type, f being the row's weight, and goes into the products dW = dZ^T A and dA += dZ W; what all rows have in common (1 / the sum of weights, and what the
 // loss' own gradient is) is applied behind the sums.
 #include "zg_product.h"
@@ -464,6 +464,8 @@ __device__ __forceinline__ void dz8(const Columns &c, const RowFactor &f, uint32
     }
 }
 
+// dZ is rounded to the operands' type here, once: dW and dA are products of that type's matrix instructions (fp32's have an eighth of the rate), and half the bytes go out and come back.  Off 64 bits that makes bf16 gradients
+// 1.84e-3 instead of the 1.66e-3 of their own rounding, fp16 ones 3.0e-4 instead of 2.1e-4.
 // The hand-over through LDS of 4 KB, as for other products' cells: 32 x 32 cells at a time, four lanes have 32 columns of a row.  bf16 16384 x 1024 x 16384 634 us, 867 TFLOP/s (the same product's statistics take 450): the way through LDS,
 // and 10 vector instructions a cell.
 template <class T, int FM, int FN> __device__ __forceinline__ void hand_over_dz(const DzArgs<T> &p, f32x16 (&acc)[FM][FN], f32x4 *mine, uint32_t m_wave, uint32_t n_wave, uint32_t M)
